@@ -247,6 +247,139 @@ int nacl_evict_noalloc(const nacl_problem* p, const void* q, const void* k, cons
 int nacl_attention(const nacl_problem* p, const void* q, const void* k, const void* v, void* out,
                    float* lse, float* lse_proxy, void* stream);
 
+/* ------------------------------------------------------------------------
+ * The decoding step between two evictions (Algorithm 1, generation phase):
+ * the new tokens' queries and keys are normalised and rotated and join the
+ * cache (nacl_rotate_append), attend to it and to a prefix that a group of
+ * sequences shares (nacl_prefix_attention), and the next token is drawn from
+ * the model's logits (nacl_sample).  The problem describes the cache, as for
+ * nacl_append: B, H, L rows per head, D, dtype, q_group, sm_scale, k_stride
+ * and v_stride; its proxies and q_stride are validated and not used.
+ * ------------------------------------------------------------------------ */
+
+/* The new tokens of one step: T per sequence, a prompt's or a decoding
+ * step's.  Token t of sequence b belongs in row row0 + lens[b] + t of each of
+ * the sequence's heads. */
+typedef struct nacl_step {
+  int32_t T;               /* 1..NACL_MAX_L */
+  int32_t row0;            /* >= 0; added to every length */
+  const int32_t* lens;     /* optional DEVICE [B]: rows each sequence holds before the step (NULL: 0) */
+  const int32_t* n_new;    /* optional DEVICE [B]: of sequence b's T tokens the first n_new[b] are
+                              real, the others padding (NULL: all real) */
+  int64_t q_stride[3];     /* element strides of the new tokens' Q for b, query head, t */
+  int64_t k_stride[3];     /* and of their K and V for b, h, t (nacl_rotate_append) */
+  int64_t v_stride[3];
+  int64_t q_out_stride[3]; /* of nacl_rotate_append's rotated Q */
+} nacl_step;
+
+/* Norm and rotation of nacl_rotate_append. */
+typedef struct nacl_rotation {
+  int32_t rot;             /* the leading entries of a head that are rotated: a multiple of 16, 0..D */
+  int32_t interleaved;     /* 0: entry i pairs with i + rot/2; 1: entry 2i with 2i + 1 */
+  float eps;               /* >= 0, added to the mean square */
+  const void* q_weight;    /* optional DEVICE [D] of the problem's dtype: the norm's weights (NULL: no norm) */
+  const void* k_weight;
+  const float* inv_freq;   /* DEVICE [rot/2]: radians per position of each pair (unused if rot is 0) */
+  int64_t pos_stride;      /* elements between two sequences' positions (0: shared by the batch) */
+} nacl_rotation;
+
+/* The step's queries and keys, each head normalised by its root mean square
+ * and the weights (where given), then rotated by the token's position, and the
+ * keys and values written into the cache:
+ *   y = x / sqrt(mean(x^2) + eps) * weight           (y = x without weights)
+ *   (y_a, y_b) -> (y_a cos - y_b sin, y_b cos + y_a sin),
+ *   angle = positions[b, t] * inv_freq[pair]
+ *   q_out = Q',  cache K row row0 + lens[b] + t = K',  cache V row = V (bit copy)
+ * in fp32 (the angle in fp64, so far positions keep their accuracy), rounded
+ * once to the dtype.  An evicted cache holds fewer rows than the sequence has
+ * tokens, so positions are given apart from the rows.
+ * q_new: device [B, H*q_group, T, D], k_new, v_new: device [B,H,T,D], with the
+ * step's strides (one projection's [B, T, (H*q_group + 2 H) D] output, say).
+ * positions: device int32, T consecutive entries per sequence (NULL only if
+ * rot is 0).  q_out: device, [B, H*q_group, T, D] with q_out_stride; it may be
+ * q_new with the same strides (in place), and overlaps nothing else.  k, v: the
+ * cache, [B,H,L,D] with the problem's strides, K and V disjoint and apart from
+ * the new tokens.  Padding tokens (t >= n_new[b]) are not
+ * read, and q_out and the cache keep what they hold in their places.  A
+ * token whose row lies outside [0, L) joins no cache (its q_out is written).
+ * Sequences may not share cache rows.  Base pointers 16-byte aligned, strides
+ * multiples of 16 bytes, B * T below 2^28. */
+int nacl_rotate_append(const nacl_problem* p, const nacl_step* s, const nacl_rotation* r, const int32_t* positions,
+                       const void* q_new, const void* k_new, const void* v_new, void* q_out, void* k, void* v,
+                       void* stream);
+
+/* A prefix that groups of sequences share: B / G consecutive sequences read
+ * the same rows, sequence b those of group b / (B / G). */
+typedef struct nacl_prefix {
+  int32_t G;               /* groups, a divisor of B */
+  int32_t L;               /* rows per head of the prefix buffers, 1..NACL_MAX_L */
+  int64_t k_stride[3];     /* element strides for group, h, row; row strides of at least D */
+  int64_t v_stride[3];
+  const void* k;           /* DEVICE [G,H,L,D], of the problem's dtype */
+  const void* v;
+  const int32_t* lens;     /* optional DEVICE [G]: rows in use (NULL: L); clamped to [0, L] */
+} nacl_prefix;
+
+/* Workspace bytes of nacl_prefix_attention (0 on invalid input).  Device
+ * memory, 256-byte aligned; its contents need no initialisation. */
+size_t nacl_prefix_workspace_bytes(const nacl_problem* p, const nacl_step* s, const nacl_prefix* x);
+
+/* Attention of the step's queries to the cache and the shared prefix: query
+ * row (b, hq, t) sees the rows in use of its group's prefix (none if x is
+ * NULL) and its sequence's cache rows j < row0 + lens[b] + t + 1 (at most L),
+ * so the step's own tokens causally.  B * H * q_group * T below 2^26.
+ * The prefix's K and V are read once for all the group's rows.
+ * q: device [B, H*q_group, T, D] with the step's q_stride (16-byte aligned
+ * base, strides multiples of 16 bytes); k, v: the cache, row strides at least
+ * D; query head hq reads K/V head hq / q_group.
+ * out: device [B, H*q_group, T, D] contiguous, of the problem's dtype: the
+ * softmax of sm_scale <q, k_j> over the visible rows times their values (fp32
+ * accumulation; for bf16 the probabilities are rounded to bf16 for the value
+ * product as in nacl_attention, the row once).  lse: optional device fp32
+ * [B, H*q_group, T], the natural log-sum-exp of the row's scaled logits; for
+ * T = 1 it is the lse argument of nacl_score with the current token as the
+ * proxy.  A row that sees nothing (padding among them, which sees nothing) and
+ * a row whose logits are all -infinity get zeros and lse -infinity.  Rows of
+ * the cache or prefix that a query does not see do not touch its result,
+ * whatever they hold.  out, lse and ws overlap nothing else. */
+int nacl_prefix_attention(const nacl_problem* p, const nacl_step* s, const nacl_prefix* x, const void* q,
+                          const void* k, const void* v, void* out, float* lse, void* ws, size_t ws_bytes,
+                          void* stream);
+
+/* Settings of nacl_sample; each array is optional DEVICE [N]. */
+typedef struct nacl_draw {
+  int32_t N, V;            /* rows, 1..65535, and tokens of the vocabulary, 1..NACL_MAX_V */
+  int32_t dtype;           /* nacl_dtype of the logits */
+  int64_t stride;          /* elements between rows, at least V */
+  const float* temperature; /* <= 0 or NaN: greedy, the first largest logit (NULL: 1) */
+  const int32_t* top_k;    /* <= 0: no limit (NULL: none) */
+  const float* top_p;      /* >= 1 or NaN: no limit (NULL: none); <= 0: the first largest */
+  const float* min_p;      /* <= 0 or NaN: no limit (NULL: none); > 1 counts as 1 */
+} nacl_draw;
+#define NACL_MAX_V (1 << 20)
+
+/* Workspace bytes of nacl_sample (0 on invalid input).  Device memory, 256-byte
+ * aligned; its contents need no initialisation. */
+size_t nacl_sample_workspace_bytes(const nacl_draw* d);
+
+/* The next token of every row of logits [N, V] (row stride d->stride, element
+ * alignment) from given uniform numbers u [N] in [0, 1):
+ *   w_i = exp((x_i - max x) / temperature); tokens in order of falling logit,
+ *   equal logits by index; kept are the first top_k, of these the fewest
+ *   leading ones whose weights reach top_p of the weights' sum (at least one),
+ *   and of these those with w_i >= min_p;
+ *   tokens[n] = the first kept i, in order of index, at which the kept weights
+ *   up to and with i exceed u times their sum.
+ * logprobs (optional): ln of the probability it was drawn with, w_i over the
+ * kept weights' sum.  A NaN logit counts as -infinity; infinite logits share a row
+ * evenly; a row without a logit above -infinity gives token -1 and logprob -infinity.  Weights
+ * are fp32 exponentials summed as 64-bit integers in units of 2^-43 of the
+ * largest, so that the result does not depend on the order of the sums: a
+ * weight below half a unit counts as nothing.
+ * tokens: device int32 [N]; logprobs: device fp32 [N]. */
+int nacl_sample(const nacl_draw* d, const void* logits, const float* u, int32_t* tokens, float* logprobs, void* ws,
+                size_t ws_bytes, void* stream);
+
 /* Static text for a status code. */
 const char* nacl_status_string(int status);
 

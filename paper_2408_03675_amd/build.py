@@ -19,7 +19,8 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libnacl.so")
 ARCH = "gfx950"
 
-SOURCES = ["score.hip", "select.hip", "compact.hip", "attention.hip", "api.cpp", "noalloc.hip"]
+SOURCES = ["score.hip", "select.hip", "compact.hip", "attention.hip", "rotate.hip", "prefix.hip", "sample.hip",
+           "api.cpp", "step.cpp", "noalloc.hip"]
 
 # Packed fp32 arithmetic stays off: the kernels are written for plain fp32
 # VALU ops.
@@ -30,7 +31,7 @@ HIP_FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
 # for accumulation registers: the logits feed vector instructions at once, and
 # copies out of accumulation registers would cost as much as the exponentials'
 # FMAs.
-SOURCE_FLAGS = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for src in ("attention.hip", "score.hip")}
+SOURCE_FLAGS = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for src in ("attention.hip", "prefix.hip", "score.hip")}
 
 
 def _hipcc():

@@ -511,6 +511,9 @@ int run_compact_slots(const nacl_problem* p, void* k, void* v, const int32_t* ke
 
 }  // namespace
 
+int nacl::validate_problem(const nacl_problem* p) { return check_problem(p); }
+void nacl::clear_detail() { g_detail[0] = 0; }
+
 extern "C" {
 
 size_t nacl_workspace_bytes(const nacl_problem* p) {

@@ -6,6 +6,8 @@
 
 #include <algorithm>
 
+#include "../../include/nacl.h"
+
 namespace nacl {
 
 // Sets the thread-local error text of the C ABI and returns status.
@@ -149,6 +151,11 @@ __host__ __device__ inline int select_slices(int L) { return (L + kSelSlice - 1)
 constexpr int kSelRegMaxL = 32 * kSelThreads;
 inline bool select_uses_slices(int L) { return L > kSelRegMaxL; }
 
+// The checks of nacl_problem that every entry point makes (api.cpp): a status,
+// with the failure's text set; the text of this thread's last failure cleared.
+int validate_problem(const nacl_problem* p);
+void clear_detail();
+
 struct SelectLaunch {
   int B, H, L, P, n_protect, C, Cp, Cr, sampling;
   uint64_t seed;
@@ -214,5 +221,71 @@ struct AttnLaunch {
 // Also writes lse_proxy[b, hq, p] = lse[b, hq, pos[p]] when lse_proxy is set.
 hipError_t launch_attention(const AttnLaunch& a, int D, const int32_t* pos, int P, float* lse_proxy,
                             hipStream_t stream);
+
+// New tokens' Q and K, normalised and rotated, and V into the cache (rotate.hip).
+struct RotateLaunch {
+  int B, H, G, T, L, row0;
+  int rot, interleaved;
+  float eps;
+  int heads_per_run;             // set by the launcher
+  int64_t qs[3], kns[3], vns[3], qos[3], ks[3], vs[3];  // element strides
+  int64_t pos_stride;
+  const int32_t* lens;           // [B] or nullptr
+  const int32_t* n_new;          // [B] or nullptr
+  const int32_t* pos;
+  const float* inv_freq;
+  const void* q_weight;          // [D] or nullptr
+  const void* k_weight;
+  const void* q;
+  const void* k_new;
+  const void* v_new;
+  void* q_out;
+  void* k;
+  void* v;
+};
+hipError_t launch_rotate_append(RotateLaunch a, int dtype, int D, int cus, hipStream_t stream);
+
+// Attention of a step's queries to the cache and a shared prefix (prefix.hip).
+constexpr int kPrefixMinChunk = 128;  // keys per chunk at least
+struct PrefixLaunch {
+  int B, H, G, T, L, row0;
+  int Lp, per_group;             // rows per head of the prefix (0: none), sequences per group
+  int block_rows;                // rows per work-group
+  int prefix_blocks, prefix_split, prefix_items;  // row blocks per (group, head), most chunks, work-groups
+  int own_blocks, own_split, own_items;           // the same per (sequence, head)
+  int direct;                    // one chunk in all: no partials
+  float c2;                      // logit scale times log2(e)
+  int64_t qs[3], ks[3], vs[3], pks[3], pvs[3];  // element strides
+  const int32_t* lens;
+  const int32_t* n_new;
+  const int32_t* plens;
+  const void* q;
+  const void* k;
+  const void* v;
+  const void* pk;
+  const void* pv;
+  void* out;
+  float* lse;                    // or nullptr
+  float* part_o;                 // workspace [rows, prefix_split + own_split, D]
+  float2* part_ml;               // workspace [rows, prefix_split + own_split]: maximum (base 2), sum
+};
+hipError_t launch_prefix(const PrefixLaunch& a, int dtype, int D, hipStream_t stream);
+
+// The next token of each row of logits (sample.hip).
+struct SampleLaunch {
+  int N, V;
+  int64_t stride;
+  const float* temperature;
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  const void* logits;
+  const float* u;
+  int32_t* tokens;
+  float* logprobs;               // or nullptr
+  void* ws;
+};
+size_t sample_workspace(int N, int V, int dtype);
+hipError_t launch_sample(const SampleLaunch& a, int dtype, hipStream_t stream);
 
 }  // namespace nacl

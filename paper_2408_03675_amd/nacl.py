@@ -29,7 +29,8 @@ SAMPLE_UNIFORM = 2
 
 EXPORTED = ("nacl_workspace_bytes", "nacl_score", "nacl_select", "nacl_compact", "nacl_compact_slots",
             "nacl_append", "nacl_evict", "nacl_evict_slots", "nacl_evict_noalloc", "nacl_attention",
-            "nacl_status_string",
+            "nacl_rotate_append", "nacl_prefix_workspace_bytes", "nacl_prefix_attention",
+            "nacl_sample_workspace_bytes", "nacl_sample", "nacl_status_string",
             "nacl_last_error_detail", "nacl_version")
 
 
@@ -50,6 +51,37 @@ class _Problem(ctypes.Structure):
         ("proxy_pos", ctypes.POINTER(ctypes.c_int32)),
         ("proxy_pos_dev", ctypes.c_void_p),
         ("q_group", ctypes.c_int32),
+    ]
+
+
+class _Step(ctypes.Structure):
+    _fields_ = [
+        ("T", ctypes.c_int32), ("row0", ctypes.c_int32), ("lens", ctypes.c_void_p), ("n_new", ctypes.c_void_p),
+        ("q_stride", ctypes.c_int64 * 3), ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3),
+        ("q_out_stride", ctypes.c_int64 * 3),
+    ]
+
+
+class _Rotation(ctypes.Structure):
+    _fields_ = [
+        ("rot", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("eps", ctypes.c_float),
+        ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("inv_freq", ctypes.c_void_p),
+        ("pos_stride", ctypes.c_int64),
+    ]
+
+
+class _Prefix(ctypes.Structure):
+    _fields_ = [
+        ("G", ctypes.c_int32), ("L", ctypes.c_int32), ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3),
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+    ]
+
+
+class _Draw(ctypes.Structure):
+    _fields_ = [
+        ("N", ctypes.c_int32), ("V", ctypes.c_int32), ("dtype", ctypes.c_int32), ("stride", ctypes.c_int64),
+        ("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p), ("top_p", ctypes.c_void_p),
+        ("min_p", ctypes.c_void_p),
     ]
 
 
@@ -86,6 +118,17 @@ def load_library(path=LIB_PATH):
     lib.nacl_evict_noalloc.restype = ctypes.c_int
     lib.nacl_attention.argtypes = [P, vp, vp, vp, vp, vp, vp, vp]
     lib.nacl_attention.restype = ctypes.c_int
+    S, R, X, W = (ctypes.POINTER(t) for t in (_Step, _Rotation, _Prefix, _Draw))
+    lib.nacl_rotate_append.argtypes = [P, S, R, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.nacl_rotate_append.restype = ctypes.c_int
+    lib.nacl_prefix_workspace_bytes.argtypes = [P, S, X]
+    lib.nacl_prefix_workspace_bytes.restype = sz
+    lib.nacl_prefix_attention.argtypes = [P, S, X, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.nacl_prefix_attention.restype = ctypes.c_int
+    lib.nacl_sample_workspace_bytes.argtypes = [W]
+    lib.nacl_sample_workspace_bytes.restype = sz
+    lib.nacl_sample.argtypes = [W, vp, vp, vp, vp, vp, sz, vp]
+    lib.nacl_sample.restype = ctypes.c_int
     lib.nacl_status_string.argtypes = [ctypes.c_int]
     lib.nacl_status_string.restype = ctypes.c_char_p
     lib.nacl_last_error_detail.argtypes = []
@@ -448,3 +491,234 @@ def evict_noalloc(prob, q, k, v, C, Cr, sampling=SAMPLE_SOFTMAX, seed=0, layer=0
                                   int(seed), int(layer), _ptr(scores), _ptr(keep_idx), _ptr(k_out),
                                   _ptr(v_out), _ptr(health), _stream(dev)))
     return scores, keep_idx, k_out, v_out
+
+
+# The decoding step between two evictions (Algorithm 1, generation phase).
+
+class _On:
+    """Makes a tensor's device the current one for a launch on its stream."""
+
+    def __init__(self, dev):
+        self.guard = torch.cuda.device(dev) if dev.index != torch.cuda.current_device() else None
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _rows4(t, name, dev, shape, dtype):
+    """A [., ., ., D] tensor with a contiguous last dimension; its strides."""
+    _gpu(t, name, dev, shape, dtype)
+    if t.stride(3) != 1:
+        raise ValueError(f"{name} must have a contiguous last dimension")
+    return t.stride()[:3]
+
+
+class Step:
+    """nacl_step: T new tokens per sequence, token t of sequence b in cache row
+    row0 + lens[b] + t.  lens, n_new: optional int32 [B] GPU tensors, read when
+    the calls run (a program may advance them in place)."""
+
+    def __init__(self, prob, T=1, lens=None, row0=0, n_new=None):
+        for t, name in ((lens, "lens"), (n_new, "n_new")):
+            if t is not None:
+                _gpu(t, name, t.device, (prob.B,), torch.int32, contiguous=True)
+        self.T, self.lens, self.n_new = int(T), lens, n_new
+        s = _Step()
+        s.T, s.row0 = self.T, int(row0)
+        s.lens = None if lens is None else lens.data_ptr()
+        s.n_new = None if n_new is None else n_new.data_ptr()
+        dense = (prob.H * prob.q_group * self.T * prob.D, self.T * prob.D, prob.D)
+        s.q_stride[:] = s.q_out_stride[:] = dense
+        s.k_stride[:] = s.v_stride[:] = (prob.H * self.T * prob.D, self.T * prob.D, prob.D)
+        self.c = s
+
+    def on(self, dev):
+        for t, name in ((self.lens, "lens"), (self.n_new, "n_new")):
+            if t is not None and t.device != dev:
+                raise ValueError(f"the step's {name} is on {t.device}, the call runs on {dev}")
+
+
+class Rotation:
+    """nacl_rotation: the angles' frequencies, inv_freq fp32 [rot / 2] (None: no
+    rotation), the optional norm weights [D] of the problem's dtype, and how
+    entries pair (interleaved: 2i with 2i + 1, else i with i + rot / 2)."""
+
+    def __init__(self, prob, inv_freq=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False):
+        if inv_freq is not None:
+            _gpu(inv_freq, "inv_freq", inv_freq.device, dtype=torch.float32, contiguous=True)
+            if inv_freq.dim() != 1:
+                raise ValueError("inv_freq must be one-dimensional")
+        for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+            if t is not None:
+                _gpu(t, name, t.device, (prob.D,), prob.torch_dtype, contiguous=True)
+        self.tensors = tuple(t for t in (inv_freq, q_weight, k_weight) if t is not None)
+        r = _Rotation()
+        r.rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+        r.interleaved, r.eps = int(bool(interleaved)), float(eps)
+        r.q_weight = None if q_weight is None else q_weight.data_ptr()
+        r.k_weight = None if k_weight is None else k_weight.data_ptr()
+        r.inv_freq = None if inv_freq is None else inv_freq.data_ptr()
+        self.c = r
+
+    def on(self, dev):
+        for t in self.tensors:
+            if t.device != dev:
+                raise ValueError(f"the rotation's tensors are on {t.device}, the call runs on {dev}")
+
+
+class Prefix:
+    """nacl_prefix: k, v [G, H, L, D], shared by B / G consecutive sequences
+    each; lens: optional int32 [G] rows in use."""
+
+    def __init__(self, prob, k, v, lens=None):
+        if not isinstance(k, torch.Tensor) or k.dim() != 4:
+            raise ValueError("the prefix's k must be [G, H, L, D]")
+        G, _, L, _ = k.shape
+        x = _Prefix()
+        x.G, x.L = G, L
+        self.dev = _gpu(k, "the prefix's k", k.device).device
+        x.k_stride[:] = _rows4(k, "the prefix's k", self.dev, (G, prob.H, L, prob.D), prob.torch_dtype)
+        x.v_stride[:] = _rows4(v, "the prefix's v", self.dev, (G, prob.H, L, prob.D), prob.torch_dtype)
+        if lens is not None:
+            _gpu(lens, "the prefix's lens", self.dev, (G,), torch.int32, contiguous=True)
+        self.k, self.v, self.lens = k, v, lens
+        x.k, x.v = k.data_ptr(), v.data_ptr()
+        x.lens = None if lens is None else lens.data_ptr()
+        self.c = x
+
+
+def rotate_append(prob, step, rotation, positions, q_new, k_new, v_new, k, v, q_out=None):
+    """The new tokens' queries and keys normalised and rotated, keys and values
+    written into the cache k, v (include/nacl.h: nacl_rotate_append).  q_new
+    [B, H*q_group, T, D], k_new, v_new [B, H, T, D] of any strides; positions
+    int32 [B, T], or [T] shared by the batch.  Returns q_out (a new tensor, or
+    the given one, which may be q_new)."""
+    lib = load_library()
+    dev = _gpu(k, "k", k.device).device
+    prob.qkv(k, "k", dev, "k")
+    prob.qkv(v, "v", dev, "v")
+    step.on(dev)
+    rotation.on(dev)
+    rows, dt = (prob.B, prob.H * prob.q_group, step.T, prob.D), prob.torch_dtype
+    s = _Step.from_buffer_copy(step.c)
+    s.q_stride[:] = _rows4(q_new, "q_new", dev, rows, dt)
+    new = (prob.B, prob.H, step.T, prob.D)
+    s.k_stride[:] = _rows4(k_new, "k_new", dev, new, dt)
+    s.v_stride[:] = _rows4(v_new, "v_new", dev, new, dt)
+    if q_out is None:
+        q_out = torch.empty(rows, dtype=dt, device=dev)
+    s.q_out_stride[:] = _rows4(q_out, "q_out", dev, rows, dt)
+    r = rotation.c
+    if positions is not None:
+        _gpu(positions, "positions", dev, dtype=torch.int32, contiguous=True)
+        if tuple(positions.shape) not in ((prob.B, step.T), (step.T,)):
+            raise ValueError(f"positions has shape {tuple(positions.shape)}, expected [B, T] or [T]")
+        r = _Rotation.from_buffer_copy(r)
+        r.pos_stride = step.T if positions.dim() == 2 else 0
+    with _On(dev):
+        _check(lib.nacl_rotate_append(prob.ref(), ctypes.byref(s), ctypes.byref(r), _ptr(positions), _ptr(q_new),
+                                      _ptr(k_new), _ptr(v_new), _ptr(q_out), _ptr(k), _ptr(v), _stream(dev)))
+    return q_out
+
+
+def prefix_workspace(prob, step, prefix=None, device="cuda"):
+    """A workspace for prefix_attention calls of these sizes."""
+    lib = load_library()
+    n = int(lib.nacl_prefix_workspace_bytes(prob.ref(), ctypes.byref(step.c),
+                                            None if prefix is None else ctypes.byref(prefix.c)))
+    if n == 0:
+        raise NaclError(NACL_ERR_INVALID_ARG, lib.nacl_last_error_detail().decode())
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def prefix_attention(prob, step, q, k, v, prefix=None, out=None, lse=None, ws=None):
+    """Attention of the step's queries q [B, H*q_group, T, D] to the cache k, v
+    (which holds the step's own tokens already) and to the prefix that groups of
+    sequences share (include/nacl.h: nacl_prefix_attention).  Returns (out
+    [B, H*q_group, T, D], lse [B, H*q_group, T] fp32); lse=False: no lse."""
+    lib = load_library()
+    dev = _gpu(k, "k", k.device).device
+    prob.qkv(k, "k", dev, "k")
+    prob.qkv(v, "v", dev, "v")
+    step.on(dev)
+    if prefix is not None and prefix.dev != dev:
+        raise ValueError(f"the prefix is on {prefix.dev}, the call runs on {dev}")
+    rows, dt = (prob.B, prob.H * prob.q_group, step.T, prob.D), prob.torch_dtype
+    s = _Step.from_buffer_copy(step.c)
+    s.q_stride[:] = _rows4(q, "q", dev, rows, dt)
+    if out is None:
+        out = torch.empty(rows, dtype=dt, device=dev)
+    _gpu(out, "out", dev, rows, dt, contiguous=True)
+    if lse is None:
+        lse = torch.empty(rows[:3], dtype=torch.float32, device=dev)
+    elif lse is False:
+        lse = None
+    if lse is not None:
+        _gpu(lse, "lse", dev, rows[:3], torch.float32, contiguous=True)
+    if ws is None:
+        ws = prefix_workspace(prob, step, prefix, dev)
+    _gpu(ws, "ws", dev, dtype=torch.uint8, contiguous=True)
+    with _On(dev):
+        _check(lib.nacl_prefix_attention(prob.ref(), ctypes.byref(s), None if prefix is None else ctypes.byref(prefix.c),
+                                         _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), _ptr(ws), ws.numel(),
+                                         _stream(dev)))
+    return out, lse
+
+
+def _draw(N, V, dtype=torch.float32, stride=None):
+    d = _Draw()
+    d.N, d.V, d.dtype = int(N), int(V), NACL_F32 if dtype == torch.float32 else NACL_BF16
+    d.stride = d.V if stride is None else int(stride)
+    return d
+
+
+def sample_workspace(N, V, device="cuda"):
+    """A workspace for sample calls of N rows over a vocabulary of V, of either dtype."""
+    lib = load_library()
+    n = max(int(lib.nacl_sample_workspace_bytes(ctypes.byref(_draw(N, V, t)))) for t in (torch.float32, torch.bfloat16))
+    if n == 0:
+        raise NaclError(NACL_ERR_INVALID_ARG, lib.nacl_last_error_detail().decode())
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None, logprobs=None, ws=None):
+    """The next token of every row of logits [N, V] (fp32 or bf16, any row stride)
+    from uniform numbers u [N] in [0, 1) (include/nacl.h: nacl_sample).  The
+    settings are [N] GPU tensors, top_k int32 and the others fp32.  Returns
+    (tokens int32 [N], logprobs fp32 [N]); logprobs=False: no logprobs."""
+    lib = load_library()
+    dev = _gpu(logits, "logits", logits.device).device
+    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("logits must be [N, V] of fp32 or bf16")
+    N, V = logits.shape
+    if V > 1 and logits.stride(1) != 1:
+        raise ValueError("logits must have a contiguous last dimension")
+    _gpu(u, "u", dev, (N,), torch.float32, contiguous=True)
+    d = _draw(N, V, logits.dtype, max(V, logits.stride(0)) if N > 1 else V)
+    if N > 1 and logits.stride(0) < V:
+        raise ValueError("rows of logits must not overlap")
+    for t, name, dt in ((temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32),
+                        (top_p, "top_p", torch.float32), (min_p, "min_p", torch.float32)):
+        if t is not None:
+            setattr(d, name, _gpu(t, name, dev, (N,), dt, contiguous=True).data_ptr())
+    if tokens is None:
+        tokens = torch.empty((N,), dtype=torch.int32, device=dev)
+    _gpu(tokens, "tokens", dev, (N,), torch.int32, contiguous=True)
+    if logprobs is None:
+        logprobs = torch.empty((N,), dtype=torch.float32, device=dev)
+    elif logprobs is False:
+        logprobs = None
+    if logprobs is not None:
+        _gpu(logprobs, "logprobs", dev, (N,), torch.float32, contiguous=True)
+    if ws is None:
+        ws = sample_workspace(N, V, dev)
+    _gpu(ws, "ws", dev, dtype=torch.uint8, contiguous=True)
+    with _On(dev):
+        _check(lib.nacl_sample(ctypes.byref(d), _ptr(logits), _ptr(u), _ptr(tokens), _ptr(logprobs), _ptr(ws), ws.numel(),
+                               _stream(dev)))
+    return tokens, logprobs

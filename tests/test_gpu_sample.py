@@ -1,0 +1,152 @@
+"""nacl_sample against the definition: exact where the weights are powers of
+two, and within the borders' rounding elsewhere."""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+nacl = pytest.importorskip("paper_2408_03675_amd.nacl")
+from oracle.step import draw_token
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+LOG2E = float(np.float32(1.44269504))  # a temperature of log2(e): weights are powers of two
+
+
+def _col(x, dtype=torch.float32):
+    return torch.tensor(x, dtype=dtype, device=DEV)
+
+
+def _sample(x, u, t, k, p, m, **kw):
+    tok, lp = nacl.sample(x, _col(u), temperature=_col(t), top_k=_col(k, torch.int32), top_p=_col(p), min_p=_col(m), **kw)
+    torch.cuda.synchronize()
+    return tok.cpu().tolist(), lp.cpu().tolist()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [1, 2, 63, 1000, 1025, 8191, 50257])
+def test_exact_draws(V, dtype):
+    """Whole-number logits and a temperature of log2(e): every weight, sum and
+    border is exact, ties abound, and so tokens have to be equal.  (u and top_p
+    are multiples of 1/64 and 1/128, so their products with the sums are exact.)"""
+    rng = np.random.default_rng(V)
+    N = 24
+    x = rng.integers(-9, 1, (N, V)).astype(np.float32)
+    x[::3] += rng.integers(0, 4, (len(x[::3]), V)) * (rng.random((len(x[::3]), V)) < 0.01)
+    x[1, :V // 2] = -math.inf
+    x[2, V // 3:] = math.nan
+    if V > 2:
+        x[2, 0] = 1.0
+    else:
+        x[2, 0] = 0.0
+    u = [float(i) for i in rng.integers(0, 64, N) / 64]
+    k = [int(i) for i in rng.choice([0, 1, 2, 5, 40, V, V + 7], N)]
+    p = [float(i) for i in rng.choice([1.0, 2.0, 0.0, 0.5, 0.875, 125 / 128], N)]
+    m = [float(i) for i in rng.choice([0.0, 0.0, 2.0 ** -5, 0.25, 1.0, 3.0], N)]
+    t = [LOG2E] * N
+    t[5] = 0.0
+    got, lps = _sample(torch.tensor(x).to(dtype).to(DEV), u, t, k, p, m)
+    for n in range(N):
+        want, lp = draw_token(x[n], u[n], t[n], k[n], p[n], m[n], weight=lambda d, t: 2.0 ** d)
+        assert got[n] == want, (n, k[n], p[n], m[n], u[n])
+        # one fp32 rounding and the logarithm's own
+        assert abs(lps[n] - lp) <= 2.0 ** -22 * (1 + abs(lp))
+
+
+def _allowed(x, u, t, k, p, m):
+    """Tokens within rounding of the borders, and ln of each one's probability.
+    A weight's exponent is a product rounded to fp32, so it is off by |ln w|
+    2^-22 at most and the sums by their weighted mean of it, below ln V 2^-22 <
+    2^-18; fixed-point units add V 2^-44."""
+    d = 2.0 ** -18
+    return dict(draw_token(x, min(max(u + du, 0.0), 1.0), t, k, p if p >= 1 else max(p + dp, 0.0), m)
+                for du in (-d, 0, d) for dp in (-d, 0, d))
+
+
+@pytest.mark.parametrize("N,V,dtype", [(1, 32000, torch.float32), (7, 50257, torch.bfloat16), (40, 4099, torch.float32),
+                                       (3, 262144, torch.bfloat16), (2, 131071, torch.float32), (300, 777, torch.bfloat16)])
+def test_draws(N, V, dtype):
+    """Gaussian logits with peaks, every combination of settings, rows a view of
+    a larger buffer (odd strides and offsets)."""
+    g = torch.Generator().manual_seed(N)
+    rng = np.random.default_rng(V)
+    buf = torch.randn((N, V + 5), generator=g) * 2.5
+    buf[:, ::97] += 6 * torch.rand(buf[:, ::97].shape, generator=g)
+    x = buf.to(dtype).to(DEV)[:, 3:3 + V]
+    ref = x.cpu().double().numpy()
+    u = [float(np.float32(i)) for i in rng.random(N)]
+    t = [float(np.float32(i)) for i in rng.choice([0.0, 0.3, 0.7, 1.0, 2.0, 1e6], N, p=[.1, .1, .3, .3, .1, .1])]
+    k = [int(i) for i in rng.choice([0, 1, 50, 1000], N, p=[.4, .1, .4, .1])]
+    p = [float(np.float32(i)) for i in rng.choice([1.0, 0.9, 0.99, 0.3], N)]
+    m = [float(np.float32(i)) for i in rng.choice([0.0, 0.01, 0.2], N, p=[.6, .2, .2])]
+    got, lps = _sample(x, u, t, k, p, m)
+    for n in range(min(N, 40)):
+        ok = _allowed(ref[n], u[n], t[n], k[n], p[n], m[n])
+        assert got[n] in ok, (n, got[n], ok, t[n], k[n], p[n], m[n])
+        assert abs(lps[n] - ok[got[n]]) <= 1e-4 + 2.0 ** -22 * abs(lps[n])
+
+
+def test_odd_rows():
+    """All hidden; infinities; NaN; u of 0 and 1 and beyond; NaN settings."""
+    inf, nan = math.inf, math.nan
+    x = torch.full((9, 40), -inf)
+    x[1, 7] = -3.0                                       # one token left
+    x[2, 5], x[2, 9], x[2, 20] = inf, 3.0, inf           # infinite logits share
+    x[3] = nan
+    x[4, 10:12] = 1.0
+    x[5, 10:12] = 1.0
+    x[6, 10:13] = 1.0
+    x[7, 3:5] = torch.tensor([0.0, -0.0])                # equal, the first by index
+    x[8, 3:5] = torch.tensor([-0.0, 0.0])
+    u = [0.3, 0.9, 0.75, 0.5, 1.0, -1.0, nan, 0.9, 0.9]
+    t = [1.0, 1.0, 1.0, 1.0, 1.0, 1.0, 1.0, 0.0, nan]
+    p = [1.0, nan, 1.0, 0.5, 1.0, 1.0, 1.0, 1.0, 1.0]
+    m = [0.0, nan, 0.0, 0.5, 0.0, 0.0, 0.0, 0.0, 0.0]
+    got, lps = _sample(x.to(DEV), u, t, [0] * 9, p, m)
+    assert got == [-1, 7, 20, -1, 11, 10, 10, 3, 3]
+    assert lps[0] == -inf and lps[3] == -inf and lps[1] == 0
+    assert abs(lps[2] - math.log(0.5)) < 1e-6 and abs(lps[4] - math.log(0.5)) < 1e-6
+
+
+def test_extreme_temperatures():
+    x = torch.tensor([[1.0, 2.0, 3.0, -math.inf]] * 3).to(DEV)
+    got, lps = _sample(x, [0.5, 0.99, 0.9], [1e-40, 1e-30, math.inf], [0] * 3, [1.0] * 3, [0.0] * 3)
+    assert got == [2, 2, 2]
+    assert lps[0] == 0 and lps[1] == 0 and abs(lps[2] - math.log(1 / 3)) < 1e-6
+
+
+def test_settings_are_optional_and_results_repeat():
+    g = torch.Generator().manual_seed(1)
+    x = (torch.randn((33, 7001), generator=g) * 3).to(DEV)
+    u = torch.rand((33,), generator=g).to(DEV)
+    tok, lp = nacl.sample(x, u)
+    full, flp = nacl.sample(x, u, torch.ones(33, device=DEV), torch.zeros(33, dtype=torch.int32, device=DEV),
+                            torch.ones(33, device=DEV), torch.zeros(33, device=DEV))
+    assert torch.equal(tok, full) and torch.equal(lp, flp)
+    for n in range(33):  # a row's draw does not depend on the batch it is in
+        one, olp = nacl.sample(x[n:n + 1], u[n:n + 1])
+        assert int(one) == int(tok[n]) and float(olp) == float(lp[n])
+    only, none = nacl.sample(x, u, logprobs=False)
+    assert none is None and torch.equal(only, tok)
+
+
+def test_graph_replays():
+    g = torch.Generator().manual_seed(2)
+    x = (torch.randn((5, 40000), generator=g) * 3).to(DEV)
+    u = torch.rand((5,), generator=g).to(DEV)
+    p = torch.full((5,), 0.9, device=DEV)
+    ws = nacl.sample_workspace(5, 40000, DEV)
+    tok, lp = nacl.sample(x, u, top_p=p, ws=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        nacl.sample(x, u, top_p=p, tokens=tok, logprobs=lp, ws=ws)
+    for i in range(5):
+        u.copy_(torch.rand((5,), generator=g))
+        x[:, i::7] += 0.5
+        graph.replay()
+        want, wlp = nacl.sample(x, u, top_p=p)
+        torch.cuda.synchronize()
+        assert torch.equal(tok, want) and torch.equal(lp, wlp)
