@@ -372,10 +372,9 @@ size_t nacl_sample_workspace_bytes(const nacl_draw* d);
  *   up to and with i exceed u times their sum.
  * logprobs (optional): ln of the probability it was drawn with, w_i over the
  * kept weights' sum.  A NaN logit counts as -infinity; infinite logits share a row
- * evenly; a row without a logit above -infinity gives token -1 and logprob -infinity.  Weights
- * are fp32 exponentials summed as 64-bit integers in units of 2^-43 of the
- * largest, so that the result does not depend on the order of the sums: a
- * weight below half a unit counts as nothing.
+ * evenly; a row without a logit above -infinity gives token -1 and logprob -infinity.   Weights
+ * are fp32 exponentials; their sums are 64-bit integers or fp64 in an order
+ * that V fixes, so a row's result depends on the row and its settings alone.
  * tokens: device int32 [N]; logprobs: device fp32 [N]. */
 int nacl_sample(const nacl_draw* d, const void* logits, const float* u, int32_t* tokens, float* logprobs, void* ws,
                 size_t ws_bytes, void* stream);
