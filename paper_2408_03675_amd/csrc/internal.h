@@ -247,10 +247,11 @@ hipError_t launch_rotate_append(RotateLaunch a, int dtype, int D, int cus, hipSt
 
 // Attention of a step's queries to the cache and a shared prefix (prefix.hip).
 constexpr int kPrefixMinChunk = 128;  // keys per chunk at least
+constexpr int kPrefixTileRows = 128;
 struct PrefixLaunch {
   int B, H, G, T, L, row0;
   int Lp, per_group;             // rows per head of the prefix (0: none), sequences per group
-  int block_rows;                // rows per work-group
+  int prefix_rows, own_rows;     // rows per work-group: 16, 32 or (bf16) kPrefixTileRows
   int prefix_blocks, prefix_split, prefix_items;  // row blocks per (group, head), most chunks, work-groups
   int own_blocks, own_split, own_items;           // the same per (sequence, head)
   int direct;                    // one chunk in all: no partials

@@ -11,6 +11,8 @@
 // waves' results are joined in LDS and either are the output (one chunk in all)
 // or go to the workspace, where merge_kernel joins a row's chunks.
 
+#include <type_traits>
+
 #include "device_common.h"
 #include "internal.h"
 
@@ -18,8 +20,9 @@ namespace nacl {
 
 namespace {
 
-constexpr int kStreamWaves = 4;
-constexpr int kStreamThreads = 64 * kStreamWaves;
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kTileRows = kPrefixTileRows, kTileKeys = 64;
 constexpr int kRsrcWord3 = 0x00020000;
 
 __device__ __forceinline__ float group_max(float x) {
@@ -37,7 +40,6 @@ __device__ __forceinline__ float group_sum(float x) {
 
 // Own cache rows that query token t of sequence b sees.
 __device__ __forceinline__ int own_limit(const PrefixLaunch& a, int b, int t) {
-  if (a.n_new && t >= a.n_new[b]) return 0;
   const int64_t n = (int64_t)a.row0 + (a.lens ? a.lens[b] : 0) + t + 1;
   return (int)(n < 0 ? 0 : n > a.L ? a.L : n);
 }
@@ -56,10 +58,12 @@ __device__ __forceinline__ int chunk_of(int n, int n_split) {
   return max(kPrefixMinChunk, (c + 31) & ~31);
 }
 
-// A query row of a block: its (sequence, query head, token), the keys it sees.
+// A query row of a block: its (sequence, query head, token), the keys it sees
+// (of padding, anything: its results are not taken).
 struct RowAt {
   int b, hq, t, limit;
 };
+__device__ __forceinline__ bool padding(const PrefixLaunch& a, const RowAt& x) { return a.n_new && x.t >= a.n_new[x.b]; }
 __device__ __forceinline__ RowAt row_at(const PrefixLaunch& a, bool prefix, int owner, int h, int row) {
   RowAt r;
   if (prefix) {
@@ -68,7 +72,7 @@ __device__ __forceinline__ RowAt row_at(const PrefixLaunch& a, bool prefix, int 
     r.b = owner * a.per_group + i;
     r.hq = h * a.G + u / a.T;
     r.t = u % a.T;
-    r.limit = a.n_new && r.t >= a.n_new[r.b] ? 0 : prefix_len(a, owner);
+    r.limit = prefix_len(a, owner);
   } else {
     r.b = owner;
     r.t = row / a.G;
@@ -169,7 +173,7 @@ struct Frag<__bf16, D> {
       for (int q = 0; q < R; ++q) acc[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[q], acc[q][dt], 0, 0, 0);
     }
   }
-  // Whether a value of the lane's key (e, i) is infinite or NaN; dropping it.
+  // Whether a value of the lane's key (e, i) is infinite or NaN.
   __device__ __forceinline__ bool odd(int e, int i) const {
     bool x = false;
 #pragma unroll
@@ -178,10 +182,6 @@ struct Frag<__bf16, D> {
       x |= (w & 0x7F800000u) == 0x7F800000u || (w & 0x7F80u) == 0x7F80u;
     }
     return x;
-  }
-  __device__ __forceinline__ void drop(int e, int i) {
-#pragma unroll
-    for (int c = 0; c < kDt / 2; ++c) vw[4 * e + i][c] = 0;
   }
 };
 
@@ -246,84 +246,172 @@ struct Frag<float, D> {
     for (int dt = 0; dt < kDt; ++dt) x |= !(__builtin_fabsf(vw[i][dt]) < INFINITY);
     return x;
   }
-  __device__ __forceinline__ void drop(int, int i) {
-#pragma unroll
-    for (int dt = 0; dt < kDt; ++dt) vw[i][dt] = 0.f;
-  }
 };
 
-template <typename T>
-__device__ __forceinline__ T to_out(float x) {
-  return (T)x;
-}
-
-// One block of 16 R rows by one chunk of keys; see above.
-template <typename T, int D, int R>
-__global__ __launch_bounds__(kStreamThreads, 2) void prefix_stream_kernel(PrefixLaunch a) {
-  using F = Frag<T, D>;
-  constexpr int kE = F::kKeys / 16, kDt = F::kDt;
-  constexpr int kRows = 16 * R;
-  constexpr int kPad = 4;  // floats after each row in LDS: lanes of one column hit distinct banks
-  __shared__ float so[kStreamWaves][kRows][D + kPad];
-  __shared__ float sm[kStreamWaves][kRows], sl[kStreamWaves][kRows];
-
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int g = lane >> 4, r = lane & 15;
-
-  // The item: prefix items first (the longer ones), then the sequences' own.
-  int item = blockIdx.x;
-  const bool prefix = item < a.prefix_items;
-  if (!prefix) item -= a.prefix_items;
+// A work-group's share: a block of rows and a chunk of the keys they read.
+struct Item {
+  bool prefix;
+  int owner, h, row0, row1;      // group or sequence, K/V head, rows of it
+  int split, key_lo, key_hi;
+  __device__ __forceinline__ bool nothing(const PrefixLaunch& a) const { return key_lo >= key_hi && !(a.direct && split == 0); }
+};
+__device__ __forceinline__ Item item_of(const PrefixLaunch& a, bool prefix, int i, int rows) {
+  Item it;
+  it.prefix = prefix;
   const int n_split = prefix ? a.prefix_split : a.own_split;
   const int n_blocks = prefix ? a.prefix_blocks : a.own_blocks;
   const int n_rows = prefix ? a.per_group * a.G * a.T : a.G * a.T;
-  const int split = item % n_split;
-  item /= n_split;
-  const int block = item % n_blocks;
-  item /= n_blocks;
-  const int h = item % a.H, owner = item / a.H;
-  const int row0 = block * kRows, row1 = min(n_rows, row0 + kRows);
-
+  it.split = i % n_split;
+  i /= n_split;
+  const int block = i % n_blocks;
+  i /= n_blocks;
+  it.h = i % a.H;
+  it.owner = i / a.H;
+  it.row0 = block * rows;
+  it.row1 = min(n_rows, it.row0 + rows);
   // Keys of the block: those its last real row sees.
   int n;
   if (prefix) {
-    n = prefix_len(a, owner);
+    n = prefix_len(a, it.owner);
   } else {
-    const int t0 = row0 / a.G, t1 = last_real(a, owner, t0, (row1 - 1) / a.G);
-    n = t1 < t0 ? 0 : own_limit(a, owner, t1);
+    const int t0 = it.row0 / a.G, t1 = last_real(a, it.owner, t0, (it.row1 - 1) / a.G);
+    n = t1 < t0 ? 0 : own_limit(a, it.owner, t1);
   }
   const int chunk = chunk_of(n, n_split);
-  const int key_lo = split * chunk, key_hi = min(n, key_lo + chunk);
-  if (key_lo >= key_hi && !(a.direct && split == 0)) return;
+  it.key_lo = it.split * chunk;
+  it.key_hi = min(n, it.key_lo + chunk);
+  return it;
+}
+
+// One head's K or V rows below `rows`; what lies past them reads as zeros.
+template <typename T>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const void* base, const int64_t (&st)[3], const Item& it, int rows) {
+  const T* p = reinterpret_cast<const T*>(base) + (int64_t)it.owner * st[0] + (int64_t)it.h * st[1];
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(p), (short)0, (int)((uint32_t)rows * ((uint32_t)st[2] * sizeof(T))),
+                                           kRsrcWord3);
+}
+template <typename T>
+__device__ __forceinline__ const T* query_of(const PrefixLaunch& a, const RowAt& x) {
+  return reinterpret_cast<const T*>(a.q) + (int64_t)x.b * a.qs[0] + (int64_t)x.hq * a.qs[1] + (int64_t)x.t * a.qs[2];
+}
+
+// Takes N neighbouring entries from d0 of a row's unnormalised output, with its
+// maximum (base 2) and sum, to the output or the workspace.
+template <typename T, int D, int N>
+__device__ __forceinline__ void put(const PrefixLaunch& a, const Item& it, const RowAt& x, float m, float l, int d0,
+                                    const float (&o)[N]) {
+  const int64_t at = ((int64_t)x.b * a.H * a.G + x.hq) * a.T + x.t;
+  if (a.direct) {
+    const bool empty = l == 0.f || padding(a, x);
+    const float inv = 1.f / l;
+    T* dst = reinterpret_cast<T*>(a.out) + at * D + d0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) dst[i] = (T)(empty ? 0.f : o[i] * inv);
+    if (a.lse && d0 == 0) a.lse[at] = empty ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+  } else {
+    const int64_t slot = at * (a.prefix_split + a.own_split) + (it.prefix ? it.split : a.prefix_split + it.split);
+    float* dst = a.part_o + slot * D + d0;
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < N; i += 4) *reinterpret_cast<f32x4*>(dst + i) = f32x4{o[i], o[i + 1], o[i + 2], o[i + 3]};
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) dst[i] = o[i];
+    }
+    if (d0 == 0) a.part_ml[slot] = float2{m, l};
+  }
+}
+
+// An item one row after the other, reading the keys that the row sees and no
+// others: for chunks of which some rows see a part and in which a value is
+// infinite or NaN.  The matrix products above give a hidden key the probability
+// 0, which times such a value would still be NaN.  A wave per row: 64 keys at a
+// time, a lane each for the logits, then each lane D / 64 entries of the output.
+template <typename T, int D>
+__device__ __forceinline__ void odd_item(const PrefixLaunch& a, const Item& it) {
+  constexpr int kPer = D / 64;
+  const int lane = threadIdx.x & 63;
+  const int64_t* ks = it.prefix ? a.pks : a.ks;
+  const int64_t* vs = it.prefix ? a.pvs : a.vs;
+  const T* kh = reinterpret_cast<const T*>(it.prefix ? a.pk : a.k) + (int64_t)it.owner * ks[0] + (int64_t)it.h * ks[1];
+  const T* vh = reinterpret_cast<const T*>(it.prefix ? a.pv : a.v) + (int64_t)it.owner * vs[0] + (int64_t)it.h * vs[1];
+  for (int row = it.row0 + (threadIdx.x >> 6); row < it.row1; row += kWaves) {
+    const RowAt x = row_at(a, it.prefix, it.owner, it.h, row);
+    const T* q = query_of<T>(a, x);
+    const int end = min(x.limit, it.key_hi);
+    float m = -INFINITY, l = 0.f, o[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) o[i] = 0.f;
+    for (int key0 = it.key_lo; key0 < end; key0 += 64) {
+      float s = -INFINITY;
+      if (key0 + lane < end) {
+        s = 0.f;
+        const T* k = kh + (int64_t)(key0 + lane) * ks[2];
+        for (int d = 0; d < D; ++d) s = __builtin_fmaf((float)k[d], (float)q[d], s);
+      }
+      float mn = s;
+#pragma unroll
+      for (int i = 1; i < 64; i *= 2) mn = fmaxf(mn, __shfl_xor(mn, i));
+      mn = fmaxf(m, mn * a.c2);
+      const float ref = mn == -INFINITY ? 0.f : mn;
+      const float alpha = __builtin_amdgcn_exp2f(m - ref);
+      m = mn;
+      const float p = key0 + lane < end ? __builtin_amdgcn_exp2f(__builtin_fmaf(s, a.c2, -ref)) : 0.f;
+      l = l * alpha + p;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) o[i] *= alpha;
+      for (int j = 0; j < min(64, end - key0); ++j) {
+        const float pj = __shfl(p, j);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) o[i] = __builtin_fmaf(pj, (float)vh[(int64_t)(key0 + j) * vs[2] + kPer * lane + i], o[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 1; i < 64; i *= 2) l += __shfl_xor(l, i);
+    put<T, D, kPer>(a, it, x, m, l, kPer * lane, o);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Few rows: 16 R per work-group, whose waves take the chunk's tiles in turn,
+// each with a softmax of its own; K and V go from memory to the fragments' registers.
+
+template <int D, int R>
+struct StreamShared {
+  static constexpr int kPad = 4;  // floats after each row: lanes of one column hit distinct banks
+  float o[kWaves][16 * R][D + kPad];
+  float m[kWaves][16 * R], l[kWaves][16 * R];
+};
+
+template <typename T, int D, int R>
+__device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& it, StreamShared<D, R>& sh) {
+  using F = Frag<T, D>;
+  constexpr int kE = F::kKeys / 16, kDt = F::kDt;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int g = lane >> 4, r = lane & 15;
+  const int key_lo = it.key_lo, key_hi = it.key_hi;
 
   typename F::Query qf[R];
   int limit[R];
   bool plain = true;  // every row of the block sees every key of the chunk
 #pragma unroll
   for (int q = 0; q < R; ++q) {
-    const int row = row0 + 16 * q + r;
-    limit[q] = 0;
+    const int row = it.row0 + 16 * q + r;
+    limit[q] = key_hi;
     qf[q].zero();
-    if (row < row1) {
-      const RowAt x = row_at(a, prefix, owner, h, row);
-      limit[q] = x.limit;
-      qf[q].load(reinterpret_cast<const T*>(a.q) + (int64_t)x.b * a.qs[0] + (int64_t)x.hq * a.qs[1] + (int64_t)x.t * a.qs[2],
-                 g);
+    if (row < it.row1) {
+      const RowAt x = row_at(a, it.prefix, it.owner, it.h, row);
+      limit[q] = min(x.limit, key_hi);
+      qf[q].load(query_of<T>(a, x), g);
     }
-    plain = plain && (row >= row1 || limit[q] >= key_hi);
+    plain = plain && limit[q] >= key_hi;
   }
   plain = __all(plain);
 
-  const int64_t* ks = prefix ? a.pks : a.ks;
-  const int64_t* vs = prefix ? a.pvs : a.vs;
-  const T* kh = reinterpret_cast<const T*>(prefix ? a.pk : a.k) + (int64_t)owner * ks[0] + (int64_t)h * ks[1];
-  const T* vh = reinterpret_cast<const T*>(prefix ? a.pv : a.v) + (int64_t)owner * vs[0] + (int64_t)h * vs[1];
-  const uint32_t krow = (uint32_t)ks[2] * sizeof(T), vrow = (uint32_t)vs[2] * sizeof(T);
-  // Rows at or past the chunk's end read as zeros.
-  const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(kh), (short)0,
-                                                                      (int)((uint32_t)key_hi * krow), kRsrcWord3);
-  const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(vh), (short)0,
-                                                                      (int)((uint32_t)key_hi * vrow), kRsrcWord3);
+  const __amdgpu_buffer_rsrc_t kr = it.prefix ? rows_of<T>(a.pk, a.pks, it, key_hi) : rows_of<T>(a.k, a.ks, it, key_hi);
+  const __amdgpu_buffer_rsrc_t vr = it.prefix ? rows_of<T>(a.pv, a.pvs, it, key_hi) : rows_of<T>(a.v, a.vs, it, key_hi);
+  const uint32_t krow = (uint32_t)(it.prefix ? a.pks[2] : a.ks[2]) * sizeof(T);
+  const uint32_t vrow = (uint32_t)(it.prefix ? a.pvs[2] : a.vs[2]) * sizeof(T);
 
   f32x4 acc[R][kDt];
   float m[R], l[R];
@@ -336,21 +424,22 @@ __global__ __launch_bounds__(kStreamThreads, 2) void prefix_stream_kernel(Prefix
   }
 
   F f;
+  bool odd = false;  // an infinite or NaN value in a chunk that some rows see a part of
   int key0 = key_lo + wave * F::kKeys;
   if (key0 < key_hi) {
     f.load_k(kr, krow, key0, g, r);
     f.load_v(vr, vrow, key0, g, r);
   }
-  for (; key0 < key_hi; key0 += kStreamWaves * F::kKeys) {
+  for (; key0 < key_hi; key0 += kWaves * F::kKeys) {
     f32x4 s[R][kE];
 #pragma unroll
     for (int q = 0; q < R; ++q) f.logits(qf[q], s[q]);
-    const int next = key0 + kStreamWaves * F::kKeys;
+    const int next = key0 + kWaves * F::kKeys;
     if (next < key_hi) f.load_k(kr, krow, next, g, r);
 #pragma unroll
     for (int q = 0; q < R; ++q) {
       if (!plain || key0 + F::kKeys > key_hi) {
-        const int lim = min(limit[q], key_hi) - key0 - 4 * g;
+        const int lim = limit[q] - key0 - 4 * g;
 #pragma unroll
         for (int e = 0; e < kE; ++e)
 #pragma unroll
@@ -382,58 +471,18 @@ __global__ __launch_bounds__(kStreamThreads, 2) void prefix_stream_kernel(Prefix
       }
     }
     if (!plain) {
-      // Some rows do not see all keys.  A hidden key has probability 0, which
-      // times an infinite or NaN value would still be NaN: where there is such a
-      // value, the product is taken row by row of the causal order, each with
-      // the keys it sees.
-      bool odd = false;
 #pragma unroll
       for (int e = 0; e < kE; ++e)
 #pragma unroll
         for (int i = 0; i < 4; ++i) odd = odd || f.odd(e, i);
-      if (__any(odd)) {
-        int from = 0;  // rows with this limit or less are done
-        while (true) {
-          int lim = 0x7FFFFFFF;  // the smallest limit left
-#pragma unroll
-          for (int q = 0; q < R; ++q)
-            if (limit[q] > from) lim = min(lim, limit[q]);
-#pragma unroll
-          for (int x = 1; x < 16; x *= 2) lim = min(lim, __shfl_xor(lim, x));
-          if (lim == 0x7FFFFFFF) break;
-          F part = f;
-          f32x4 p[R][kE];
-#pragma unroll
-          for (int q = 0; q < R; ++q)
-#pragma unroll
-            for (int e = 0; e < kE; ++e)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) p[q][e][i] = limit[q] == lim ? s[q][e][i] : 0.f;
-#pragma unroll
-          for (int e = 0; e < kE; ++e)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (key0 + 16 * e + 4 * g + i >= lim) part.drop(e, i);
-          f32x4 add[R][kDt];
-#pragma unroll
-          for (int q = 0; q < R; ++q)
-#pragma unroll
-            for (int dt = 0; dt < kDt; ++dt) add[q][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-          part.template value<R>(p, add);
-#pragma unroll
-          for (int q = 0; q < R; ++q)
-            if (limit[q] == lim) {
-#pragma unroll
-              for (int dt = 0; dt < kDt; ++dt) acc[q][dt] += add[q][dt];
-            }
-          from = lim;
-        }
-        if (next < key_hi) f.load_v(vr, vrow, next, g, r);
-        continue;
-      }
     }
     f.template value<R>(s, acc);
     if (next < key_hi) f.load_v(vr, vrow, next, g, r);
+  }
+
+  if (!plain && __syncthreads_or(odd)) {
+    odd_item<T, D>(a, it);
+    return;
   }
 
   // Join the waves: rows in LDS, each thread a run of entries of one row.
@@ -441,60 +490,272 @@ __global__ __launch_bounds__(kStreamThreads, 2) void prefix_stream_kernel(Prefix
   for (int q = 0; q < R; ++q) {
     const float lq = group_sum(l[q]);
     if (g == 0) {
-      sm[wave][16 * q + r] = m[q];
-      sl[wave][16 * q + r] = lq;
+      sh.m[wave][16 * q + r] = m[q];
+      sh.l[wave][16 * q + r] = lq;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int dt = 0; dt < kDt; dt += 4)
-        *reinterpret_cast<f32x4*>(&so[wave][16 * q + r][kDt * (4 * g + i) + dt]) =
+        *reinterpret_cast<f32x4*>(&sh.o[wave][16 * q + r][kDt * (4 * g + i) + dt]) =
             f32x4{acc[q][dt][i], acc[q][dt + 1][i], acc[q][dt + 2][i], acc[q][dt + 3][i]};
   }
   __syncthreads();
   constexpr int kPer = 8;  // entries per thread
-  for (int u = tid; u < (row1 - row0) * (D / kPer); u += kStreamThreads) {
+  for (int u = tid; u < (it.row1 - it.row0) * (D / kPer); u += kThreads) {
     const int lr = u / (D / kPer), d0 = (u % (D / kPer)) * kPer;
     float mt = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < kStreamWaves; ++w) mt = fmaxf(mt, sm[w][lr]);
+    for (int w = 0; w < kWaves; ++w) mt = fmaxf(mt, sh.m[w][lr]);
     const float ref = mt == -INFINITY ? 0.f : mt;
     float lt = 0.f, o[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) o[i] = 0.f;
 #pragma unroll
-    for (int w = 0; w < kStreamWaves; ++w) {
-      const float c = __builtin_amdgcn_exp2f(sm[w][lr] - ref);
-      lt += c * sl[w][lr];
+    for (int w = 0; w < kWaves; ++w) {
+      const float c = __builtin_amdgcn_exp2f(sh.m[w][lr] - ref);
+      lt += c * sh.l[w][lr];
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) o[i] += c * so[w][lr][d0 + i];
+      for (int i = 0; i < kPer; ++i) o[i] += c * sh.o[w][lr][d0 + i];
     }
-    const RowAt x = row_at(a, prefix, owner, h, row0 + lr);
-    const int64_t at = ((int64_t)x.b * a.H * a.G + x.hq) * a.T + x.t;
-    if (a.direct) {
-      const float inv = lt == 0.f ? 0.f : 1.f / lt;
-      T* dst = reinterpret_cast<T*>(a.out) + at * D + d0;
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) dst[i] = (T)(o[i] * inv);
-      if (a.lse && d0 == 0) a.lse[at] = lt == 0.f ? -INFINITY : (mt + log2f(lt)) * 0.69314718055994531f;
-    } else {
-      const int64_t slot = at * (a.prefix_split + a.own_split) + (prefix ? split : a.prefix_split + split);
-      float* dst = a.part_o + slot * D + d0;
-#pragma unroll
-      for (int i = 0; i < kPer; i += 4) *reinterpret_cast<f32x4*>(dst + i) = f32x4{o[i], o[i + 1], o[i + 2], o[i + 3]};
-      if (d0 == 0) a.part_ml[slot] = float2{mt, lt};
-    }
+    put<T, D, kPer>(a, it, row_at(a, it.prefix, it.owner, it.h, it.row0 + lr), mt, lt, d0, o);
   }
 }
 
-// A row's chunks joined: one wave per row.
+// ---------------------------------------------------------------------------
+// Many rows (bf16): 32 per wave, 128 per work-group, whose waves share tiles of
+// 64 keys in LDS (two of each of K and V, one barrier per tile; the next tile's
+// rows wait in registers while the one in hand is used).  v_mfma_f32_32x32x16_bf16
+// with the roles as above: lane (hl, n) = (lane / 32, lane mod 32) holds logits of
+// query n, keys 8 (i / 4) + 4 hl + i mod 4, and the output's entries likewise.
+// K's 16-byte pieces are swizzled by row so that a fragment's 32 rows fall on
+// distinct banks; V stays in rows and is read transposed (ds_read_b64_tr_b16).
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+template <int D>
+struct TileShared {
+  unsigned char k[2][kTileKeys * D * 2], v[2][kTileKeys * D * 2];
+};
+
+template <int D>
+__device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it, TileShared<D>& sh) {
+  constexpr int kRowBytes = D * 2, kChunks = kRowBytes / 16, kSwz = kChunks - 1;
+  constexpr int kC = D / 16, kDt = D / 32;
+  constexpr int kUnits = kTileKeys * kChunks / kThreads;  // 16-byte pieces of a tile per thread
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int hl = lane >> 5, n = lane & 31;
+  const int key_lo = it.key_lo, key_hi = it.key_hi;
+
+  bf16x8 qf[kC];
+  int limit = key_hi;
+  const int row = it.row0 + 32 * wave + n;
+  const bool real = row < it.row1;
+  RowAt at{};
+  if (real) {
+    at = row_at(a, it.prefix, it.owner, it.h, row);
+    limit = min(at.limit, key_hi);
+  }
+#pragma unroll
+  for (int c = 0; c < kC; ++c)
+    qf[c] = real ? __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(query_of<__bf16>(a, at) + 16 * c + 8 * hl))
+                 : __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+  const bool plain = __all(limit >= key_hi);
+  const bool idle = it.row0 + 32 * wave >= it.row1;  // no row in this wave
+
+  const __amdgpu_buffer_rsrc_t kr = it.prefix ? rows_of<__bf16>(a.pk, a.pks, it, key_hi) : rows_of<__bf16>(a.k, a.ks, it, key_hi);
+  const __amdgpu_buffer_rsrc_t vr = it.prefix ? rows_of<__bf16>(a.pv, a.pvs, it, key_hi) : rows_of<__bf16>(a.v, a.vs, it, key_hi);
+  const uint32_t krow = (uint32_t)(it.prefix ? a.pks[2] : a.ks[2]) * 2, vrow = (uint32_t)(it.prefix ? a.pvs[2] : a.vs[2]) * 2;
+
+  const bool causal = !it.prefix && a.T > 1;
+  bool odd = false;  // as for few rows
+  u32x4 kreg[kUnits], vreg[kUnits];
+  auto load = [&](int key0) {
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int p = tid + kThreads * u;
+      kreg[u] = __builtin_amdgcn_raw_buffer_load_b128(kr, (uint32_t)(key0 + p / kChunks) * krow + (uint32_t)(p % kChunks) * 16, 0, 0);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int p = tid + kThreads * u;
+      vreg[u] = __builtin_amdgcn_raw_buffer_load_b128(vr, (uint32_t)(key0 + p / kChunks) * vrow + (uint32_t)(p % kChunks) * 16, 0, 0);
+    }
+  };
+  auto store = [&](int buf) {
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int p = tid + kThreads * u, r = p / kChunks, x = p % kChunks;
+      *reinterpret_cast<u32x4*>(sh.k[buf] + r * kRowBytes + ((x ^ (r & kSwz)) * 16)) = kreg[u];
+      *reinterpret_cast<u32x4*>(sh.v[buf] + r * kRowBytes + ((x ^ ((r & 3) << 1)) * 16)) = vreg[u];
+      if (causal) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) odd = odd || (vreg[u][c] & 0x7F800000u) == 0x7F800000u || (vreg[u][c] & 0x7F80u) == 0x7F80u;
+      }
+    }
+  };
+  // K fragment (keys 32 kt + n, entries 16 c + 8 hl ..), V^T fragment (entries 32
+  // dt + n, the keys that the lane's logits of step ks hold).
+  auto kfrag = [&](int buf, int kt, int c) {
+    return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(sh.k[buf] + (32 * kt + n) * kRowBytes +
+                                                                      (((2 * c + hl) ^ (n & kSwz)) * 16)));
+  };
+  const int i16 = lane & 15, vkey = 4 * hl + (i16 >> 2);
+  uint32_t va[kDt];
+#pragma unroll
+  for (int dt = 0; dt < kDt; ++dt)
+    va[dt] = (uint32_t)(vkey * kRowBytes + (((4 * dt + 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1)) ^ ((vkey & 3) << 1)) * 16) +
+                        (i16 & 1) * 8);
+  auto vfrag = [&](int buf, int ks, int dt) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    const unsigned char* p = sh.v[buf] + va[dt] + ks * 16 * kRowBytes;
+    union {
+      s16x4 h[2];
+      bf16x8 v;
+    } u;
+    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
+    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + 8 * kRowBytes));
+    return u.v;
+  };
+
+  f32x16 acc[kDt];
+#pragma unroll
+  for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[dt][i] = 0.f;
+  float m = -INFINITY, l = 0.f;
+
+  if (key_lo < key_hi) {
+    load(key_lo);
+    store(0);
+  }
+  int buf = 0;
+  for (int key0 = key_lo; key0 < key_hi; key0 += kTileKeys, buf ^= 1) {
+    __syncthreads();
+    const int next = key0 + kTileKeys;
+    if (next < key_hi) load(next);
+    if (!idle) {
+      f32x16 s[2];
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+        f32x16 t;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) t[i] = 0.f;
+#pragma unroll
+        for (int c = 0; c < kC; ++c) t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kfrag(buf, kt, c), qf[c], t, 0, 0, 0);
+        s[kt] = t;
+      }
+      const bool masked = !plain || next > key_hi;
+      if (masked) {
+        const int lim = limit - key0 - 4 * hl;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (32 * kt + 8 * (i / 4) + i % 4 >= lim) s[kt][i] = -INFINITY;
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[kt][i]);
+      auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+      const float mn = fmaxf(m, mx * a.c2);
+      const float ref = mn == -INFINITY ? 0.f : mn;
+      const float alpha = __builtin_amdgcn_exp2f(m - ref);
+      m = mn;
+      float sum[2] = {0.f, 0.f};
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[kt][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i], a.c2, -ref));
+          sum[i & 1] += s[kt][i];
+        }
+      l = l * alpha + (sum[0] + sum[1]);
+      if (__ballot(alpha != 1.f)) {
+#pragma unroll
+        for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[dt][i] *= alpha;
+      }
+      bf16x8 pf[4];
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) pf[ks][i] = (__bf16)s[ks / 2][8 * (ks % 2) + i];
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+        for (int dt = 0; dt < kDt; ++dt)
+          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vfrag(buf, ks, dt), pf[ks], acc[dt], 0, 0, 0);
+    }
+    if (next < key_hi) store(buf ^ 1);
+  }
+
+  if (causal && __syncthreads_or(odd)) {
+    odd_item<__bf16, D>(a, it);
+    return;
+  }
+  auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+  l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  if (real) {
+#pragma unroll
+    for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const float o[4] = {acc[dt][i], acc[dt][i + 1], acc[dt][i + 2], acc[dt][i + 3]};
+        put<__bf16, D, 4>(a, it, at, m, l, 32 * dt + 2 * i + 4 * hl, o);
+      }
+  }
+}
+
+// What takes the prefix's items and the own caches' (rows per work-group: 16,
+// 32 or 128).  The prefix's come first: they are the longer ones.
+template <typename T, int D, int ROWS>
+struct Part {
+  using Shared = StreamShared<D, ROWS / 16>;
+  static __device__ __forceinline__ void run(const PrefixLaunch& a, const Item& it, Shared& sh) {
+    stream_item<T, D, ROWS / 16>(a, it, sh);
+  }
+};
+template <int D>
+struct Part<__bf16, D, kTileRows> {
+  using Shared = TileShared<D>;
+  static __device__ __forceinline__ void run(const PrefixLaunch& a, const Item& it, Shared& sh) { tile_item<D>(a, it, sh); }
+};
+
+template <typename T, int D, int PREFIX, int OWN>
+__global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixLaunch a) {
+  using P = Part<T, D, PREFIX>;
+  using O = Part<T, D, OWN>;
+  union Shared {
+    typename P::Shared p;
+    typename O::Shared o;
+  };
+  __shared__ __attribute__((aligned(16))) unsigned char smem[sizeof(Shared)];
+  Shared& sh = *reinterpret_cast<Shared*>(smem);
+  const int i = blockIdx.x;
+  const bool prefix = i < a.prefix_items;
+  const Item it = item_of(a, prefix, prefix ? i : i - a.prefix_items, prefix ? PREFIX : OWN);
+  if (it.nothing(a)) return;
+  if constexpr (PREFIX == OWN) {
+    O::run(a, it, sh.o);
+  } else {
+    if (prefix) P::run(a, it, sh.p);
+    else O::run(a, it, sh.o);
+  }
+}
+
+// A row's chunks joined: one work-group per row, D / 4 threads per chunk.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixLaunch a) {
-  constexpr int kPer = D / 64;
-  const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+__global__ __launch_bounds__(kThreads) void prefix_merge_kernel(PrefixLaunch a) {
+  constexpr int kPer = D / 4, kSlots = kThreads / kPer, kUnroll = 4;
+  __shared__ float so[kSlots][D], sl[kSlots], smax[kWaves];
+  const int tid = threadIdx.x, d0 = (tid % kPer) * 4, mine = tid / kPer;
+  const int64_t row = blockIdx.x;
   const int Hq = a.H * a.G;
-  if (row >= (int64_t)a.B * Hq * a.T) return;
   const int t = (int)(row % a.T);
   const int64_t bh = row / a.T;
   const int b = (int)(bh / Hq), e = (int)(bh % Hq) % a.G;
@@ -505,7 +766,7 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixLaunch a) {
       const int n = prefix_len(a, b / a.per_group), c = chunk_of(n, a.prefix_split);
       np = (n + c - 1) / c;
     }
-    const int r0 = (t * a.G + e) / a.block_rows * a.block_rows, r1 = min(a.G * a.T, r0 + a.block_rows);
+    const int r0 = (t * a.G + e) / a.own_rows * a.own_rows, r1 = min(a.G * a.T, r0 + a.own_rows);
     const int n = own_limit(a, b, last_real(a, b, r0 / a.G, (r1 - 1) / a.G)), c = chunk_of(n, a.own_split);
     no = (n + c - 1) / c;
   }
@@ -513,37 +774,72 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixLaunch a) {
   const int total = np + no;
   auto slot = [&](int i) { return base + (i < np ? i : a.prefix_split + i - np); };
   float m = -INFINITY;
-  for (int i = lane; i < total; i += 64) m = fmaxf(m, a.part_ml[slot(i)].x);
+  for (int i = tid; i < total; i += kThreads) m = fmaxf(m, a.part_ml[slot(i)].x);
+  // The first chunks' outputs are on their way while the maximum is found.
+  f32x4 w[kUnroll];
+  float2 ml[kUnroll];
+  auto load = [&](int i0) {
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int i = i0 + u * kSlots + mine;
+      ml[u] = float2{-INFINITY, 0.f};
+      w[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (i < total) {
+        ml[u] = a.part_ml[slot(i)];
+        w[u] = *reinterpret_cast<const f32x4*>(a.part_o + slot(i) * D + d0);
+      }
+    }
+  };
+  load(0);
 #pragma unroll
   for (int x = 1; x < 64; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
+  if ((tid & 63) == 0) smax[tid >> 6] = m;
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < kWaves; ++x) m = fmaxf(m, smax[x]);
   const float ref = m == -INFINITY ? 0.f : m;
-  float l = 0.f, o[kPer];
+  float l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int i0 = 0; i0 < total; i0 += kUnroll * kSlots) {
+    if (i0) load(i0);
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) o[i] = 0.f;
-  for (int i = 0; i < total; ++i) {
-    const float2 ml = a.part_ml[slot(i)];
-    const float c = __builtin_amdgcn_exp2f(ml.x - ref);
-    l += c * ml.y;
-#pragma unroll
-    for (int x = 0; x < kPer; ++x) o[x] += c * a.part_o[slot(i) * D + kPer * lane + x];
+    for (int u = 0; u < kUnroll; ++u) {
+      const float c = __builtin_amdgcn_exp2f(ml[u].x - ref);
+      l += c * ml[u].y;
+      o += c * w[u];
+    }
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  T* dst = reinterpret_cast<T*>(a.out) + row * D + kPer * lane;
+  *reinterpret_cast<f32x4*>(&so[mine][d0]) = o;
+  if (d0 == 0) sl[mine] = l;
+  __syncthreads();
+  if (tid >= D) return;
+  float lt = 0.f, x = 0.f;
 #pragma unroll
-  for (int x = 0; x < kPer; ++x) dst[x] = (T)(o[x] * inv);
-  if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+  for (int i = 0; i < kSlots; ++i) {
+    lt += sl[i];
+    x += so[i][tid];
+  }
+  reinterpret_cast<T*>(a.out)[row * D + tid] = (T)(lt == 0.f ? 0.f : x / lt);
+  if (a.lse && tid == 0) a.lse[row] = lt == 0.f ? -INFINITY : (m + log2f(lt)) * 0.69314718055994531f;
 }
 
 template <typename T, int D>
 hipError_t launch_t(const PrefixLaunch& a, hipStream_t stream) {
-  const int64_t items = (int64_t)a.prefix_items + a.own_items;
-  if (a.block_rows == 16) prefix_stream_kernel<T, D, 1><<<(unsigned)items, kStreamThreads, 0, stream>>>(a);
-  else prefix_stream_kernel<T, D, 2><<<(unsigned)items, kStreamThreads, 0, stream>>>(a);
-  if (hipError_t e = hipGetLastError()) return e;
-  if (!a.direct) {
-    const int64_t rows = (int64_t)a.B * a.H * a.G * a.T;
-    prefix_merge_kernel<T, D><<<(unsigned)((rows + 3) / 4), 256, 0, stream>>>(a);
+  const dim3 grid((unsigned)(a.prefix_items + a.own_items));
+  auto run = [&](auto kernel) { kernel<<<grid, kThreads, 0, stream>>>(a); };
+  const int own = a.own_rows, prefix = std::max(a.prefix_rows, own);
+  if constexpr (std::is_same_v<T, __bf16>) {
+    if (own == kTileRows) run(prefix_kernel<T, D, kTileRows, kTileRows>);
+    else if (prefix == kTileRows && own == 32) run(prefix_kernel<T, D, kTileRows, 32>);
+    else if (prefix == kTileRows) run(prefix_kernel<T, D, kTileRows, 16>);
   }
+  if (prefix < kTileRows) {
+    if (own == 32) run(prefix_kernel<T, D, 32, 32>);
+    else if (prefix == 32) run(prefix_kernel<T, D, 32, 16>);
+    else run(prefix_kernel<T, D, 16, 16>);
+  }
+  if (hipError_t e = hipGetLastError()) return e;
+  if (!a.direct) prefix_merge_kernel<T, D><<<(unsigned)((int64_t)a.B * a.H * a.G * a.T), kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 

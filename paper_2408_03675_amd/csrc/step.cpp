@@ -72,7 +72,7 @@ int check_prefix(const nacl_problem* p, const nacl_prefix* x) {
 // most n_split chunks.
 struct Plan {
   int per_group = 1, Lp = 0;
-  int block_rows = 16;
+  int prefix_rows = 16, own_rows = 16;
   int prefix_blocks = 0, prefix_split = 0, own_blocks = 0, own_split = 0;
   int64_t prefix_items = 0, own_items = 0, rows = 0;
   bool direct = false;
@@ -87,17 +87,22 @@ Plan plan_of(const nacl_problem* p, const nacl_step* s, const nacl_prefix* x) {
   a.Lp = x ? x->L : 0;
   a.rows = (int64_t)p->B * p->H * G * s->T;
   const int64_t own_rows = (int64_t)G * s->T, prefix_rows = own_rows * a.per_group;
-  a.block_rows = (x ? prefix_rows : own_rows) > 16 ? 32 : 16;
+  auto block = [&](int64_t rows) {
+    return rows <= 16 ? 16 : rows <= 32 || p->dtype == NACL_F32 ? 32 : nacl::kPrefixTileRows;
+  };
+  a.own_rows = block(own_rows);
+  a.prefix_rows = x ? block(prefix_rows) : a.own_rows;
   auto up = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
-  a.own_blocks = (int)up(own_rows, a.block_rows);
-  a.prefix_blocks = x ? (int)up(prefix_rows, a.block_rows) : 0;
-  // Chunks of about the same number of keys in both, four work-groups per CU
-  // in all.
+  a.own_blocks = (int)up(own_rows, a.own_rows);
+  a.prefix_blocks = x ? (int)up(prefix_rows, a.prefix_rows) : 0;
   const int64_t own_units = (int64_t)p->B * p->H * a.own_blocks, prefix_units = (int64_t)groups * p->H * a.prefix_blocks;
-  const int64_t keys = own_units * p->L + prefix_units * a.Lp;
+  // Chunks of about the same number of keys in both, four work-groups per CU in
+  // all; a prefix read by tiles in chunks that fill the chip twice over.
+  const bool tiles = x && a.prefix_rows == nacl::kPrefixTileRows;
+  const int64_t keys = own_units * p->L + (tiles ? 0 : prefix_units * a.Lp);
   const int64_t chunk = std::max<int64_t>(nacl::kPrefixMinChunk, up(keys, 4 * kPlanCus));
   a.own_split = (int)up(p->L, chunk);
-  a.prefix_split = (int)up(a.Lp, chunk);
+  a.prefix_split = (int)up(a.Lp, tiles ? std::max<int64_t>(256, up(prefix_units * a.Lp, 2 * kPlanCus)) : chunk);
   a.own_items = own_units * a.own_split;
   a.prefix_items = prefix_units * a.prefix_split;
   a.direct = !x && a.own_split == 1;
@@ -281,7 +286,8 @@ int nacl_prefix_attention(const nacl_problem* p, const nacl_step* s, const nacl_
   a.row0 = s->row0;
   a.Lp = plan.Lp;
   a.per_group = plan.per_group;
-  a.block_rows = plan.block_rows;
+  a.prefix_rows = plan.prefix_rows;
+  a.own_rows = plan.own_rows;
   a.prefix_blocks = plan.prefix_blocks;
   a.prefix_split = plan.prefix_split;
   a.prefix_items = (int)plan.prefix_items;
