@@ -510,12 +510,32 @@ class _On:
             self.guard.__exit__(*exc)
 
 
+def _like(t, name, dev, shape, dtype):
+    """_gpu's checks of a contiguous tensor in one expression, for calls where
+    the host's time counts; what does not pass is reported by _gpu."""
+    if not (isinstance(t, torch.Tensor) and t.device == dev and t.shape == shape and t.dtype == dtype and t.is_contiguous()):
+        _gpu(t, name, dev, shape, dtype, contiguous=True)
+
+
 def _rows4(t, name, dev, shape, dtype):
     """A [., ., ., D] tensor with a contiguous last dimension; its strides."""
-    _gpu(t, name, dev, shape, dtype)
-    if t.stride(3) != 1:
+    if not (isinstance(t, torch.Tensor) and t.device == dev and t.shape == shape and t.dtype == dtype):
+        _gpu(t, name, dev, shape, dtype)
+    st = t.stride()
+    if st[3] != 1:
         raise ValueError(f"{name} must have a contiguous last dimension")
-    return t.stride()[:3]
+    return st
+
+
+def _cache(t, name, dev, step, strides):
+    """A cache tensor of the step's problem."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device == dev and t.shape == step.cache_shape and
+            t.dtype == step.dtype and t.stride() == strides):
+        _gpu(t, name, dev, step.cache_shape, step.dtype, strides[:3])
+
+
+def _raw_stream(dev):
+    return torch._C._cuda_getCurrentRawStream(dev.index)
 
 
 class Step:
@@ -527,20 +547,44 @@ class Step:
         for t, name in ((lens, "lens"), (n_new, "n_new")):
             if t is not None:
                 _gpu(t, name, t.device, (prob.B,), torch.int32, contiguous=True)
-        self.T, self.lens, self.n_new = int(T), lens, n_new
+        if lens is not None and n_new is not None and lens.device != n_new.device:
+            raise ValueError("lens and n_new are on different devices")
+        self.prob, self.T, self.lens, self.n_new = prob, int(T), lens, n_new
+        self.dev = next((t.device for t in (lens, n_new) if t is not None), None)
+        B, H, L, D, Hq = prob.B, prob.H, prob.L, prob.D, prob.H * max(1, prob.q_group)
+        self.dtype = prob.torch_dtype
+        self.q_shape, self.new_shape = (B, Hq, self.T, D), (B, H, self.T, D)
+        self.cache_shape = (B, H, L, D)
+        self.fits = (H, D, self.dtype)
+        self.k_stride, self.v_stride = tuple(prob.c.k_stride) + (1,), tuple(prob.c.v_stride) + (1,)
         s = _Step()
         s.T, s.row0 = self.T, int(row0)
         s.lens = None if lens is None else lens.data_ptr()
         s.n_new = None if n_new is None else n_new.data_ptr()
-        dense = (prob.H * prob.q_group * self.T * prob.D, self.T * prob.D, prob.D)
+        dense = (Hq * self.T * D, self.T * D, D)
         s.q_stride[:] = s.q_out_stride[:] = dense
-        s.k_stride[:] = s.v_stride[:] = (prob.H * self.T * prob.D, self.T * prob.D, prob.D)
+        s.k_stride[:] = s.v_stride[:] = (H * self.T * D, self.T * D, D)
         self.c = s
+        self._strided = {}  # nacl_step by the strides of the call's tensors
 
-    def on(self, dev):
-        for t, name in ((self.lens, "lens"), (self.n_new, "n_new")):
-            if t is not None and t.device != dev:
-                raise ValueError(f"the step's {name} is on {t.device}, the call runs on {dev}")
+    def on(self, prob, dev):
+        if prob is not self.prob:
+            raise ValueError("the step was made for another problem")
+        if self.dev is not None and self.dev != dev:
+            raise ValueError(f"the step's lengths are on {self.dev}, the call runs on {dev}")
+
+    def strided(self, q, k=None, v=None, q_out=None):
+        key = (q, k, v, q_out)
+        s = self._strided.get(key)
+        if s is None:
+            s = _Step.from_buffer_copy(self.c)
+            for field, st in (("q_stride", q), ("k_stride", k), ("v_stride", v), ("q_out_stride", q_out)):
+                if st is not None:
+                    getattr(s, field)[:] = st[:3]
+            if len(self._strided) >= 64:
+                self._strided.clear()
+            self._strided[key] = s
+        return s
 
 
 class Rotation:
@@ -557,6 +601,10 @@ class Rotation:
             if t is not None:
                 _gpu(t, name, t.device, (prob.D,), prob.torch_dtype, contiguous=True)
         self.tensors = tuple(t for t in (inv_freq, q_weight, k_weight) if t is not None)
+        self.dev = self.tensors[0].device if self.tensors else None
+        self.fits = (prob.D, prob.torch_dtype)
+        if any(t.device != self.dev for t in self.tensors):
+            raise ValueError("the rotation's tensors are on different devices")
         r = _Rotation()
         r.rot = 0 if inv_freq is None else 2 * inv_freq.numel()
         r.interleaved, r.eps = int(bool(interleaved)), float(eps)
@@ -564,11 +612,15 @@ class Rotation:
         r.k_weight = None if k_weight is None else k_weight.data_ptr()
         r.inv_freq = None if inv_freq is None else inv_freq.data_ptr()
         self.c = r
+        self._by_stride = {}  # nacl_rotation by pos_stride
 
-    def on(self, dev):
-        for t in self.tensors:
-            if t.device != dev:
-                raise ValueError(f"the rotation's tensors are on {t.device}, the call runs on {dev}")
+    def with_stride(self, n):
+        r = self._by_stride.get(n)
+        if r is None:
+            r = _Rotation.from_buffer_copy(self.c)
+            r.pos_stride = n
+            self._by_stride[n] = r
+        return r
 
 
 class Prefix:
@@ -582,11 +634,12 @@ class Prefix:
         x = _Prefix()
         x.G, x.L = G, L
         self.dev = _gpu(k, "the prefix's k", k.device).device
-        x.k_stride[:] = _rows4(k, "the prefix's k", self.dev, (G, prob.H, L, prob.D), prob.torch_dtype)
-        x.v_stride[:] = _rows4(v, "the prefix's v", self.dev, (G, prob.H, L, prob.D), prob.torch_dtype)
+        x.k_stride[:] = _rows4(k, "the prefix's k", self.dev, (G, prob.H, L, prob.D), prob.torch_dtype)[:3]
+        x.v_stride[:] = _rows4(v, "the prefix's v", self.dev, (G, prob.H, L, prob.D), prob.torch_dtype)[:3]
         if lens is not None:
             _gpu(lens, "the prefix's lens", self.dev, (G,), torch.int32, contiguous=True)
         self.k, self.v, self.lens = k, v, lens
+        self.fits = (prob.H, prob.D, prob.torch_dtype)
         x.k, x.v = k.data_ptr(), v.data_ptr()
         x.lens = None if lens is None else lens.data_ptr()
         self.c = x
@@ -598,31 +651,29 @@ def rotate_append(prob, step, rotation, positions, q_new, k_new, v_new, k, v, q_
     [B, H*q_group, T, D], k_new, v_new [B, H, T, D] of any strides; positions
     int32 [B, T], or [T] shared by the batch.  Returns q_out (a new tensor, or
     the given one, which may be q_new)."""
-    lib = load_library()
-    dev = _gpu(k, "k", k.device).device
-    prob.qkv(k, "k", dev, "k")
-    prob.qkv(v, "v", dev, "v")
-    step.on(dev)
-    rotation.on(dev)
-    rows, dt = (prob.B, prob.H * prob.q_group, step.T, prob.D), prob.torch_dtype
-    s = _Step.from_buffer_copy(step.c)
-    s.q_stride[:] = _rows4(q_new, "q_new", dev, rows, dt)
-    new = (prob.B, prob.H, step.T, prob.D)
-    s.k_stride[:] = _rows4(k_new, "k_new", dev, new, dt)
-    s.v_stride[:] = _rows4(v_new, "v_new", dev, new, dt)
+    lib = _lib or load_library()
+    dev = getattr(k, "device", None)
+    _cache(k, "k", dev, step, step.k_stride)
+    _cache(v, "v", dev, step, step.v_stride)
+    step.on(prob, dev)
+    if rotation.fits != step.fits[1:]:
+        raise ValueError("the rotation was made for another head size or dtype")
+    if rotation.dev is not None and rotation.dev != dev:
+        raise ValueError(f"the rotation's tensors are on {rotation.dev}, the call runs on {dev}")
+    dt = step.dtype
     if q_out is None:
-        q_out = torch.empty(rows, dtype=dt, device=dev)
-    s.q_out_stride[:] = _rows4(q_out, "q_out", dev, rows, dt)
-    r = rotation.c
+        q_out = torch.empty(step.q_shape, dtype=dt, device=dev)
+    s = step.strided(_rows4(q_new, "q_new", dev, step.q_shape, dt), _rows4(k_new, "k_new", dev, step.new_shape, dt),
+                     _rows4(v_new, "v_new", dev, step.new_shape, dt), _rows4(q_out, "q_out", dev, step.q_shape, dt))
+    pos = None
     if positions is not None:
-        _gpu(positions, "positions", dev, dtype=torch.int32, contiguous=True)
-        if tuple(positions.shape) not in ((prob.B, step.T), (step.T,)):
-            raise ValueError(f"positions has shape {tuple(positions.shape)}, expected [B, T] or [T]")
-        r = _Rotation.from_buffer_copy(r)
-        r.pos_stride = step.T if positions.dim() == 2 else 0
+        per_row = positions.dim() == 2
+        _like(positions, "positions", dev, (prob.B, step.T) if per_row else (step.T,), torch.int32)
+        pos = positions.data_ptr()
+    r = rotation.with_stride(step.T if pos is not None and per_row else 0)
     with _On(dev):
-        _check(lib.nacl_rotate_append(prob.ref(), ctypes.byref(s), ctypes.byref(r), _ptr(positions), _ptr(q_new),
-                                      _ptr(k_new), _ptr(v_new), _ptr(q_out), _ptr(k), _ptr(v), _stream(dev)))
+        _check(lib.nacl_rotate_append(prob.ref(), s, r, pos, q_new.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
+                                      q_out.data_ptr(), k.data_ptr(), v.data_ptr(), _raw_stream(dev)))
     return q_out
 
 
@@ -641,32 +692,33 @@ def prefix_attention(prob, step, q, k, v, prefix=None, out=None, lse=None, ws=No
     (which holds the step's own tokens already) and to the prefix that groups of
     sequences share (include/nacl.h: nacl_prefix_attention).  Returns (out
     [B, H*q_group, T, D], lse [B, H*q_group, T] fp32); lse=False: no lse."""
-    lib = load_library()
-    dev = _gpu(k, "k", k.device).device
-    prob.qkv(k, "k", dev, "k")
-    prob.qkv(v, "v", dev, "v")
-    step.on(dev)
-    if prefix is not None and prefix.dev != dev:
-        raise ValueError(f"the prefix is on {prefix.dev}, the call runs on {dev}")
-    rows, dt = (prob.B, prob.H * prob.q_group, step.T, prob.D), prob.torch_dtype
-    s = _Step.from_buffer_copy(step.c)
-    s.q_stride[:] = _rows4(q, "q", dev, rows, dt)
+    lib = _lib or load_library()
+    dev = getattr(k, "device", None)
+    _cache(k, "k", dev, step, step.k_stride)
+    _cache(v, "v", dev, step, step.v_stride)
+    step.on(prob, dev)
+    if prefix is not None and (prefix.dev != dev or prefix.fits != step.fits):
+        raise ValueError(f"the prefix is on {prefix.dev} with (heads, D, dtype) {prefix.fits}, the call's are on {dev} "
+                         f"with {step.fits}")
+    s = step.strided(_rows4(q, "q", dev, step.q_shape, step.dtype))
     if out is None:
-        out = torch.empty(rows, dtype=dt, device=dev)
-    _gpu(out, "out", dev, rows, dt, contiguous=True)
+        out = torch.empty(step.q_shape, dtype=step.dtype, device=dev)
+    else:
+        _like(out, "out", dev, step.q_shape, step.dtype)
     if lse is None:
-        lse = torch.empty(rows[:3], dtype=torch.float32, device=dev)
+        lse = torch.empty(step.q_shape[:3], dtype=torch.float32, device=dev)
     elif lse is False:
         lse = None
-    if lse is not None:
-        _gpu(lse, "lse", dev, rows[:3], torch.float32, contiguous=True)
+    else:
+        _like(lse, "lse", dev, step.q_shape[:3], torch.float32)
     if ws is None:
         ws = prefix_workspace(prob, step, prefix, dev)
-    _gpu(ws, "ws", dev, dtype=torch.uint8, contiguous=True)
+    n = ws.numel()
+    _like(ws, "ws", dev, (n,), torch.uint8)
     with _On(dev):
-        _check(lib.nacl_prefix_attention(prob.ref(), ctypes.byref(s), None if prefix is None else ctypes.byref(prefix.c),
-                                         _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), _ptr(ws), ws.numel(),
-                                         _stream(dev)))
+        _check(lib.nacl_prefix_attention(prob.ref(), s, None if prefix is None else prefix.c, q.data_ptr(), k.data_ptr(),
+                                         v.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
+                                         ws.data_ptr(), n, _raw_stream(dev)))
     return out, lse
 
 
@@ -691,34 +743,48 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, toke
     from uniform numbers u [N] in [0, 1) (include/nacl.h: nacl_sample).  The
     settings are [N] GPU tensors, top_k int32 and the others fp32.  Returns
     (tokens int32 [N], logprobs fp32 [N]); logprobs=False: no logprobs."""
-    lib = load_library()
-    dev = _gpu(logits, "logits", logits.device).device
-    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16):
+    lib = _lib or load_library()
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("logits must be [N, V] of fp32 or bf16")
+    dev = logits.device
+    if not logits.is_cuda:
+        _gpu(logits, "logits", dev)
     N, V = logits.shape
-    if V > 1 and logits.stride(1) != 1:
+    stride, one = logits.stride()
+    if V > 1 and one != 1:
         raise ValueError("logits must have a contiguous last dimension")
-    _gpu(u, "u", dev, (N,), torch.float32, contiguous=True)
-    d = _draw(N, V, logits.dtype, max(V, logits.stride(0)) if N > 1 else V)
-    if N > 1 and logits.stride(0) < V:
+    if N > 1 and stride < V:
         raise ValueError("rows of logits must not overlap")
-    for t, name, dt in ((temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32),
-                        (top_p, "top_p", torch.float32), (min_p, "min_p", torch.float32)):
-        if t is not None:
-            setattr(d, name, _gpu(t, name, dev, (N,), dt, contiguous=True).data_ptr())
+    rows = (N,)
+    _like(u, "u", dev, rows, torch.float32)
+    d = _Draw(N, V, NACL_F32 if logits.dtype == torch.float32 else NACL_BF16, stride if N > 1 else V)
+    if temperature is not None:
+        _like(temperature, "temperature", dev, rows, torch.float32)
+        d.temperature = temperature.data_ptr()
+    if top_k is not None:
+        _like(top_k, "top_k", dev, rows, torch.int32)
+        d.top_k = top_k.data_ptr()
+    if top_p is not None:
+        _like(top_p, "top_p", dev, rows, torch.float32)
+        d.top_p = top_p.data_ptr()
+    if min_p is not None:
+        _like(min_p, "min_p", dev, rows, torch.float32)
+        d.min_p = min_p.data_ptr()
     if tokens is None:
-        tokens = torch.empty((N,), dtype=torch.int32, device=dev)
-    _gpu(tokens, "tokens", dev, (N,), torch.int32, contiguous=True)
+        tokens = torch.empty(rows, dtype=torch.int32, device=dev)
+    else:
+        _like(tokens, "tokens", dev, rows, torch.int32)
     if logprobs is None:
-        logprobs = torch.empty((N,), dtype=torch.float32, device=dev)
+        logprobs = torch.empty(rows, dtype=torch.float32, device=dev)
     elif logprobs is False:
         logprobs = None
-    if logprobs is not None:
-        _gpu(logprobs, "logprobs", dev, (N,), torch.float32, contiguous=True)
+    else:
+        _like(logprobs, "logprobs", dev, rows, torch.float32)
     if ws is None:
         ws = sample_workspace(N, V, dev)
-    _gpu(ws, "ws", dev, dtype=torch.uint8, contiguous=True)
+    n = ws.numel()
+    _like(ws, "ws", dev, (n,), torch.uint8)
     with _On(dev):
-        _check(lib.nacl_sample(ctypes.byref(d), _ptr(logits), _ptr(u), _ptr(tokens), _ptr(logprobs), _ptr(ws), ws.numel(),
-                               _stream(dev)))
+        _check(lib.nacl_sample(d, logits.data_ptr(), u.data_ptr(), tokens.data_ptr(),
+                               None if logprobs is None else logprobs.data_ptr(), ws.data_ptr(), n, _raw_stream(dev)))
     return tokens, logprobs

@@ -254,3 +254,28 @@ def test_log_sum_exp_feeds_the_score():
     z = torch.logsumexp(torch.cat((a, b), dim=3), dim=3, keepdim=True)
     ref = (a - z).exp().sum(dim=2)
     assert ((F.double() - ref).abs() <= 1e-3 * ref + 1e-30).all()
+
+
+@pytest.mark.parametrize("G,T,B,Lp", [(2, 12, 2, 0), (8, 9, 2, 300), (1, 150, 1, 40)])
+def test_hidden_values_in_larger_blocks(G, T, B, Lp):
+    """Blocks of 32 and 128 rows: a token with an infinite value and one with a
+    NaN value reach the queries from it on, earlier ones keep their results."""
+    H, L, D = 2, T + 90, 128
+    q, k, v, kp, vp, _, _ = _make(B, H, G, T, L, D, "bf16", 1, Lp, seed=3)
+    lens = torch.full((B,), 70, dtype=torch.int32)
+    plens = torch.tensor([Lp], dtype=torch.int32) if Lp else None
+    prob = nacl.Problem(B, H, L, D, "bf16", [L - 1], q_group=G)
+    step = nacl.Step(prob, T, lens=lens.to(DEV))
+    prefix = nacl.Prefix(prob, kp, vp) if Lp else None
+    v[0, 0, 70 + T // 2] = float("inf")
+    v[0, 1, 70 + T // 3, 5] = float("nan")
+    k[B - 1, 1, 70 + T - 1] = float("nan")
+    out, lse = nacl.prefix_attention(prob, step, q, k, v, prefix=prefix)
+    torch.cuda.synchronize()
+    late = lambda b, hq, t: (b == 0 and t >= (T // 2, T // 3)[hq // G]) or (b == B - 1 and hq // G == 1 and t == T - 1)
+    rows = [x for x in _rows(B, H * G, T, 400) if not late(*x)]
+    check_rows(q, k, v, kp, vp, lens, plens, out, lse, prob.c.sm_scale, rows)
+    assert torch.isinf(out[0, 0, T // 2:]).all()
+    odd = torch.isnan(out[0, G, T // 3:T - 1])
+    assert odd[:, 5].all() and not odd[:, :5].any() and not odd[:, 6:].any()
+    assert torch.isnan(lse[B - 1, G:, T - 1]).all()
