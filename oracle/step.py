@@ -51,28 +51,20 @@ def draw_token(x, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, weight=None
         return -1, -math.inf
     if not temperature > 0:
         temperature, top_k = 1.0, 1
-    order = sorted(range(len(x)), key=lambda i: (-x[i], i))
+    order = np.argsort(-x, kind="stable")
     if top_k > 0:
         order = order[:top_k]
-    if weight is None:
-        def weight(d, t):
-            return math.exp(d / t)
-    w = {i: 1.0 if x[i] == m else 0.0 if x[i] == -math.inf or m == math.inf else weight(x[i] - m, temperature) for i in order}
+    with np.errstate(all="ignore"):
+        w = np.exp((x - m) / temperature) if weight is None else weight(x - m, temperature)
+    w = np.where(x == m, 1.0, np.where((x == -math.inf) | (m == math.inf), 0.0, w))
     if top_p < 1:
-        total, reach, kept = sum(w.values()), 0.0, []
-        for i in order:
-            kept.append(i)
-            reach += w[i]
-            if reach >= top_p * total:
-                break
-        order = kept
+        reach = np.cumsum(w[order])
+        order = order[:1 + int((reach < top_p * reach[-1]).sum())]
     if min_p > 0:
-        order = [i for i in order if w[i] >= min(min_p, 1.0)]
-    total, cum, token = sum(w[i] for i in order), 0.0, None
-    for i in sorted(order):
-        if w[i] > 0:
-            token = i
-        cum += w[i]
-        if cum > u * total:
-            break
-    return token, math.log(w[token] / total)
+        order = order[w[order] >= min(min_p, 1.0)]
+    order = np.sort(order)
+    cum = np.cumsum(w[order])
+    at = int((cum <= u * cum[-1]).sum())
+    if at == len(order) or w[order[at]] == 0:
+        at = int(np.flatnonzero(w[order] > 0)[-1])
+    return int(order[at]), math.log(w[order[at]] / cum[-1])

@@ -2,15 +2,16 @@
 // (nacl_sample).
 //
 // Two launches and one pass over the logits.  sample_slices_kernel reads slices
-// of a row (kSlice tokens, whatever the batch, so that a row's sums and its
-// result do not depend on it) and sorts what can matter into bins of an eighth of
-// a power of two of the weight: bin(x) = floor(8 x log2(e) / temperature), the
-// same grid for every slice and without the row's maximum.  A bin holds the
-// count of its tokens and the sum of their weights over the bin's lower edge,
-// both as integers, so that the order of the atomics does not show.
-// sample_finish_kernel joins a row's slices, finds the bin in which the kept
-// tokens end, reads the row again only for the tokens down to that bin, sorts
-// those and draws.
+// of a row (their size depends on V alone, so that a row's sums and its result do
+// not depend on the batch) and sorts what can matter into bins of an eighth of a
+// power of two of the weight: bin(x) = floor(8 x log2(e) / temperature), the same
+// grid for every slice and without the row's maximum.  A bin holds the count of
+// its tokens and the sum of their weights over the bin's lower edge, both as
+// integers, so that the order of the atomics does not show; where few tokens are
+// binned the slice lists them too.  sample_finish_kernel, a work-group per row,
+// joins the slices, finds the bin in which the kept tokens end, collects the
+// tokens of that bin (from the lists, or from the slices that have some) or, if
+// they are few, all down to it, sorts them and draws.
 
 #include "device_common.h"
 #include "internal.h"
@@ -20,25 +21,34 @@ namespace nacl {
 namespace {
 
 constexpr int kSliceThreads = 512;
-constexpr int kSlicePer = 16;                            // tokens per thread
-constexpr int kSlice = kSliceThreads * kSlicePer;        // tokens per slice
+constexpr int kMinSlice = kSliceThreads * 16;            // tokens per slice: 16 or 32 per thread
 constexpr int kBins = 256;                               // 32 powers of two below a slice's largest
-constexpr int kMaxSlices = (NACL_MAX_V + kSlice - 1) / kSlice;
+constexpr int kMaxSlices = NACL_MAX_V / (2 * kMinSlice);
 constexpr int kFinishThreads = 1024;
-constexpr int kList = 4096;                              // tokens that the finish sorts
+constexpr int kList = kFinishThreads;                    // tokens that the finish sorts, one per thread
+constexpr int kKeep = 128;                               // tokens that a slice lists
 constexpr float kUnit = 0x1p22f;                         // a weight over its bin's edge, in units
 constexpr int kCountShift = 43;                          // of a bin word: count above, weight units below
+constexpr uint64_t kUnitMask = ((uint64_t)1 << kCountShift) - 1;
 constexpr float kMaxBin = 0x1p20f;                       // bins beyond are too coarse to use
 static_assert(NACL_MAX_V < (1 << (64 - kCountShift)) && NACL_MAX_V * 1.1 * 0x1p22 < 0x1p43, "bin words");
 
-// What a slice leaves for the finish, followed by its bins.
+// Long vocabularies take longer slices: a work-group then has more in flight.
+// (Short ones need the work-groups.)
+constexpr int slice_of(int V) { return V > 65536 ? 2 * kMinSlice : kMinSlice; }
+static_assert(65536 / kMinSlice <= kMaxSlices, "slices");
+
+// What a slice leaves for the finish: this, then its bins, then its list.
 struct SliceInfo {
   float max;     // largest logit
   int top;       // its bin (the slice's bins go down from it)
   int n_bins;    // bins filled; -1: the logits are beyond the grid
   int left;      // top-k: a token above -infinity lies below the bins
   double rest;   // weights outside the bins over the largest one's
+  int n_list;    // tokens in the bins, as words; -1: too many for the list
+  int pad;
 };
+constexpr int kSliceBytes = sizeof(SliceInfo) + (kBins + kKeep) * 8;
 
 struct Settings {
   float scale;   // log2(e) / temperature
@@ -80,45 +90,56 @@ __device__ __forceinline__ float over_edge(float x, float scale, float bin) {
   return __builtin_amdgcn_exp2f(__builtin_fmaf(x, scale, -0.125f * bin));
 }
 
-// kSlicePer logits of a thread: runs of 8, kSliceThreads * 8 apart.
-template <typename T>
-__device__ __forceinline__ void load_slice(const T* row, int V, int i0, int tid, float (&x)[kSlicePer]) {
+// Order of tokens as falling words: larger logits first, then lower indexes.
+__device__ __forceinline__ uint64_t word_of(float x, uint32_t i) { return (uint64_t)float_order_key(x) << 32 | (uint32_t)~i; }
+__device__ __forceinline__ float float_of_key(uint32_t key) {
+  return __uint_as_float((key & 0x80000000u) ? key & 0x7FFFFFFFu : ~key);
+}
+
+// 8 E logits of a thread: runs of 8, `apart` tokens from one to the next, in
+// range below `end`.
+template <typename T, int E>
+__device__ __forceinline__ void load_run(const T* row, int i0, int apart, int end, float (&x)[8 * E]) {
 #pragma unroll
-  for (int e = 0; e < kSlicePer / 8; ++e) {
-    const int i = i0 + (e * kSliceThreads + tid) * 8;
+  for (int e = 0; e < E; ++e) {
+    const int i = i0 + e * apart;
     T raw[8];
-    if (i + 8 <= V) {
+    if (i + 8 <= end) {
       __builtin_memcpy(raw, row + i, sizeof(raw));
 #pragma unroll
       for (int c = 0; c < 8; ++c) x[8 * e + c] = clean((float)raw[c]);
     } else {
 #pragma unroll
-      for (int c = 0; c < 8; ++c) x[8 * e + c] = i + c < V ? logit(row, i + c) : -INFINITY;
+      for (int c = 0; c < 8; ++c) x[8 * e + c] = i + c < end ? logit(row, i + c) : -INFINITY;
     }
   }
 }
 
-template <typename T>
+template <typename T, int E>
 __global__ __launch_bounds__(kSliceThreads) void sample_slices_kernel(SampleLaunch a, int n_slices) {
+  constexpr int kPer = 8 * E, kSlice = kSliceThreads * kPer;
   __shared__ unsigned long long bins[kBins];
+  __shared__ uint64_t list[kKeep];
   __shared__ uint32_t tops[kBins];
   __shared__ float wmax[kSliceThreads / 64];
   __shared__ double wrest[kSliceThreads / 64];
-  __shared__ int need;
+  __shared__ int need, listed;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int slice = blockIdx.x, n = blockIdx.y;
-  const Settings s = settings_of(a, n);
   const T* row = reinterpret_cast<const T*>(a.logits) + (int64_t)n * a.stride;
 
-  float x[kSlicePer];
-  load_slice(row, a.V, slice * kSlice, tid, x);
+  float x[kPer];
+  const int i0 = slice * kSlice + 8 * tid;
+  load_run<T, E>(row, i0, kSliceThreads * 8, a.V, x);
+  const Settings s = settings_of(a, n);
   if (tid < kBins) {
     bins[tid] = 0;
     tops[tid] = 0;
   }
+  if (tid == 0) listed = 0;
   float tmax = x[0];
 #pragma unroll
-  for (int i = 1; i < kSlicePer; ++i) tmax = fmaxf(tmax, x[i]);
+  for (int i = 1; i < kPer; ++i) tmax = fmaxf(tmax, x[i]);
   float mx = tmax;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) mx = fmaxf(mx, __shfl_xor(mx, d));
@@ -127,12 +148,11 @@ __global__ __launch_bounds__(kSliceThreads) void sample_slices_kernel(SampleLaun
 #pragma unroll
   for (int w = 0; w < kSliceThreads / 64; ++w) mx = fmaxf(mx, wmax[w]);
 
-  char* out = static_cast<char*>(a.ws) + ((int64_t)n * n_slices + slice) * (sizeof(SliceInfo) + kBins * 8);
-  SliceInfo* info = reinterpret_cast<SliceInfo*>(out);
+  SliceInfo* info = reinterpret_cast<SliceInfo*>(static_cast<char*>(a.ws) + ((int64_t)n * n_slices + slice) * kSliceBytes);
   const float top = bin_of(mx, s.scale);
   // All hidden, or beyond the grid (infinite and NaN products among that).
   if (mx == -INFINITY || !(__builtin_fabsf(top) < kMaxBin) || s.scale < 0x1p-60f) {
-    if (tid == 0) *info = SliceInfo{mx, 0, mx == -INFINITY ? 0 : -1, 0, 0.0};
+    if (tid == 0) *info = SliceInfo{mx, 0, mx == -INFINITY ? 0 : -1, 0, 0.0, 0, 0};
     return;
   }
 
@@ -180,22 +200,27 @@ __global__ __launch_bounds__(kSliceThreads) void sample_slices_kernel(SampleLaun
 
   float rest = 0.f;
   bool left = false;
-  const bool with_rest = s.k == 0 && (s.p < 1.f || s.m == 0.f);
   if (n_bins > 0) {
+    const bool with_rest = s.k == 0 && s.p < 1.f;
     const float n_binsf = (float)n_bins;
 #pragma unroll
-    for (int i = 0; i < kSlicePer; ++i) {
+    for (int i = 0; i < kPer; ++i) {
       const float b = bin_of(x[i], s.scale), j = top - b;
-      if (j < n_binsf)
+      if (j < n_binsf) {
         atomicAdd(&bins[(int)j], (1ull << kCountShift) + (uint32_t)rintf(over_edge(x[i], s.scale, b) * kUnit));
-      else if (with_rest)
+        if (listed <= kKeep) {  // a count past kKeep says that there are more
+          const int at = atomicAdd(&listed, 1);
+          if (at < kKeep) list[at] = word_of(x[i], i0 + (i / 8) * kSliceThreads * 8 + i % 8);
+        }
+      } else if (with_rest) {
         rest += __builtin_amdgcn_exp2f((x[i] - mx) * s.scale);
-      else
+      } else {
         left = left || x[i] > -INFINITY;
+      }
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < kSlicePer; ++i) rest += x[i] == mx ? 1.f : __builtin_amdgcn_exp2f((x[i] - mx) * s.scale);
+    for (int i = 0; i < kPer; ++i) rest += __builtin_amdgcn_exp2f((x[i] - mx) * s.scale);
   }
   double total = rest;
 #pragma unroll
@@ -205,9 +230,11 @@ __global__ __launch_bounds__(kSliceThreads) void sample_slices_kernel(SampleLaun
   if (tid == 0) {
     total = 0.0;
     for (int w = 0; w < kSliceThreads / 64; ++w) total += wrest[w];
-    *info = SliceInfo{mx, (int)top, n_bins, any_left, total};
+    *info = SliceInfo{mx, (int)top, n_bins, any_left, total, n_bins > 0 && listed <= kKeep ? listed : -1, 0};
   }
-  if (tid < n_bins) reinterpret_cast<unsigned long long*>(info + 1)[tid] = bins[tid];
+  unsigned long long* words = reinterpret_cast<unsigned long long*>(info + 1);
+  if (tid < n_bins) words[tid] = bins[tid];
+  if (tid < min(listed, kKeep)) words[kBins + tid] = list[tid];
 }
 
 // Exclusive sums in thread order and the sum of all, by a fixed tree.
@@ -234,101 +261,131 @@ __device__ U block_scan(U x, U* total, U* tmp) {
   return base + before;
 }
 
-// Sorts n words of LDS (a power of two) in falling order.
-__device__ void sort_falling(uint64_t* v, int n) {
-  for (int size = 2; size <= n; size *= 2)
-    for (int step = size / 2; step > 0; step /= 2) {
-      __syncthreads();
-      for (int i = threadIdx.x; i < n / 2; i += kFinishThreads) {
-        const int lo = (i / step) * 2 * step + (i % step), hi = lo + step;
-        const uint64_t x = v[lo], y = v[hi];
-        const bool falling = (lo & size) == 0;
-        if ((x < y) == falling) {
-          v[lo] = y;
-          v[hi] = x;
-        }
+// Sorts words in falling order, one per thread, those of the first `size`
+// threads (a power of two from 64 on; every thread takes part).
+__device__ uint64_t sort_falling(uint64_t v, int size, uint64_t* tmp) {
+  const int tid = threadIdx.x;
+  for (int k = 2; k <= size; k *= 2)
+    for (int j = k / 2; j > 0; j /= 2) {
+      uint64_t other;
+      if (j >= 64) {
+        __syncthreads();
+        tmp[tid] = v;
+        __syncthreads();
+        other = tmp[tid ^ j];
+      } else {
+        other = __shfl_xor(v, j);
       }
+      const bool larger = ((tid & j) == 0) == ((tid & k) == 0);
+      if ((other > v) == larger) v = other;
     }
   __syncthreads();
+  return v;
 }
 
-__device__ __forceinline__ double pow2(double x) { return exp2(x); }
+// 2^(-j / 8).
+__device__ __forceinline__ double eighths(int j) {
+  constexpr double kRoot[8] = {1.0,
+                               0.91700404320467123174,
+                               0.84089641525371454303,
+                               0.77110541270397041180,
+                               0.70710678118654752440,
+                               0.64841977732550483297,
+                               0.59460355750136053336,
+                               0.54525386633262882702};
+  double r = kRoot[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) r = (j & 7) == i ? kRoot[i] : r;
+  return ldexp(r, -(j >> 3));
+}
 
 struct FinishShared {
   uint64_t list[kList];
-  double value[kList];
   double tmp[kFinishThreads / 64];
   uint64_t tmpu[kFinishThreads / 64];
-  unsigned long long bins[kBins];
-  uint32_t hist[kBins];
+  unsigned long long bins[kBins];          // finish_any: a pass's; otherwise the row's
+  uint64_t before_c[kBins + 1];            // tokens above each bin, and their weight
+  double before_w[kBins + 1];
   SliceInfo info[kMaxSlices];
   double slice_w[kMaxSlices];
-  uint32_t wanted[kMaxSlices / 32];
+  unsigned long long extra[kMaxSlices];    // units of a slice's tokens of the last bin above the list's
   int pick[4];
-  uint64_t picku[2];
+  uint64_t picku;
+  double pickd;
 };
-
-// Order of tokens as falling words: larger logits first, then lower indexes.
-__device__ __forceinline__ uint64_t word_of(float x, uint32_t i) { return (uint64_t)float_order_key(x) << 32 | (uint32_t)~i; }
-__device__ __forceinline__ float float_of_key(uint32_t key) {
-  return __uint_as_float((key & 0x80000000u) ? key & 0x7FFFFFFFu : ~key);
-}
 
 // Which tokens are kept: those whose word is at least `last` and logit at least
 // `least`.
 struct Kept {
   uint64_t last;
-  double least;
+  float least;
   __device__ __forceinline__ bool operator()(float x, uint32_t i) const {
-    return x > -INFINITY && word_of(x, i) >= last && (double)x >= least;
+    return x > -INFINITY && word_of(x, i) >= last && x >= least;
   }
 };
+// The smallest logit that min-p keeps.
+__device__ __forceinline__ float least_of(const Settings& s, float mx) {
+  if (!(s.m > 0.f) || !(s.scale > 0.f)) return -INFINITY;
+  if (mx == INFINITY) return mx;
+  const double limit = (double)mx + log2((double)s.m) / (double)s.scale;
+  const float x = (float)limit;
+  return (double)x < limit ? float_of_key(float_order_key(x) + 1) : x;
+}
 
 __device__ __forceinline__ void answer(const SampleLaunch& a, int n, int token, double p) {
   a.tokens[n] = token;
   if (a.logprobs) a.logprobs[n] = token < 0 ? -INFINITY : (float)log(p);
 }
 
-// The draw among the kept tokens of [i0, i1), whose weights start at `before`
-// and of which the one is wanted at which the sum passes `at`.  A thread takes a
-// run of tokens; of a sum that falls short by rounding, the last token.
-template <typename T, class W>
-__device__ void draw_in(const SampleLaunch& a, int n, const T* row, int i0, int i1, double at, double total, const Kept& kept,
-                        const W& weight, FinishShared& sh) {
-  const int per = (i1 - i0 + kFinishThreads - 1) / kFinishThreads;
-  const int lo = min(i1, i0 + (int)threadIdx.x * per), hi = min(i1, lo + per);
-  double sum = 0.0;
-  int last = -1;
-  for (int i = lo; i < hi; ++i) {
-    const float x = logit(row, i);
-    const double w = kept(x, i) ? weight(x) : 0.0;
-    sum += w;
-    if (w > 0.0) last = i;
-  }
-  double all;
-  const double before = block_scan(sum, &all, sh.tmp);
-  if (threadIdx.x == 0) sh.pick[0] = -1;
-  __syncthreads();
-  if (last >= 0) atomicMax(&sh.pick[0], last);
-  if (threadIdx.x == 0) sh.pick[1] = 0x7FFFFFFF;
-  __syncthreads();
-  if (before + sum > at && sum > 0.0) {  // the first such thread's first such token
-    double cum = before;
-    for (int i = lo; i < hi; ++i) {
-      const float x = logit(row, i);
-      const double w = kept(x, i) ? weight(x) : 0.0;
-      cum += w;
-      if (w > 0.0 && cum > at) {
-        atomicMin(&sh.pick[1], i);
-        break;
-      }
-    }
-  }
+// Threads' candidates in order: the first at which the running sum, `before` plus
+// the thread's `sum`, passes `at`; of a sum that falls short by rounding, the last
+// thread with a weight.
+__device__ int pick_thread(double before, double sum, double at, FinishShared& sh) {
   __syncthreads();
   if (threadIdx.x == 0) {
-    const int token = sh.pick[1] == 0x7FFFFFFF ? sh.pick[0] : sh.pick[1];
-    answer(a, n, token, token < 0 ? 0.0 : weight(logit(row, token)) / total);
+    sh.pick[2] = -1;
+    sh.pick[3] = 0x7FFFFFFF;
   }
+  __syncthreads();
+  if (sum > 0.0) {
+    atomicMax(&sh.pick[2], (int)threadIdx.x);
+    if (before + sum > at) atomicMin(&sh.pick[3], (int)threadIdx.x);
+  }
+  __syncthreads();
+  return sh.pick[3] == 0x7FFFFFFF ? sh.pick[2] : sh.pick[3];
+}
+
+// The draw among the kept tokens of a slice, of which the one is wanted at which
+// the sum of the weights passes `at`.  A thread takes a run of 8 E tokens.
+template <typename T, int E, class W>
+__device__ void draw_slice(const SampleLaunch& a, int n, const T* row, int slice, double at, double total, const Kept& kept,
+                           const W& weight, FinishShared& sh) {
+  constexpr int kPer = 8 * E;
+  const int lo = (slice * kFinishThreads + (int)threadIdx.x) * kPer;
+  float x[kPer];
+  load_run<T, E>(row, lo, 8, a.V, x);
+  double sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+    if (kept(x[i], lo + i)) sum += weight(x[i]);
+  double all;
+  const double before = block_scan(sum, &all, sh.tmp);
+  // That thread's tokens again, a lane each.
+  const int thread = pick_thread(before, sum, at, sh);
+  if ((int)threadIdx.x == thread) sh.pickd = before;
+  __syncthreads();
+  if (threadIdx.x >= 64) return;
+  const int lane = threadIdx.x, i = (slice * kFinishThreads + thread) * kPer + lane;
+  const float y = lane < kPer && i < a.V ? logit(row, i) : -INFINITY;
+  const double w = kept(y, i) ? weight(y) : 0.0;
+  double cum = w;
+#pragma unroll
+  for (int d = 1; d < kPer; d *= 2) {
+    const double z = __shfl_up(cum, d);
+    if (lane >= d) cum += z;
+  }
+  const uint64_t with = __ballot(w > 0.0), past = __ballot(w > 0.0 && sh.pickd + cum > at);
+  if (lane == (past ? __builtin_ctzll(past) : 63 - __builtin_clzll(with | 1))) answer(a, n, i, w / total);
 }
 
 // Any row, slowly: the last kept token by a search over the words' range that
@@ -354,8 +411,7 @@ __device__ void finish_any(const SampleLaunch& a, int n, const Settings& s, cons
   block_scan(sum, &total, sh.tmpu);
   block_scan(count, &seen, sh.tmpu);
   uint64_t last = 0;
-  double least = -INFINITY;
-  if (s.m > 0.f && scale > 0.f) least = mx < INFINITY ? (double)mx + log2((double)s.m) / (double)scale : (double)mx;
+  const float least = least_of(s, mx);
   for (int by_weight = 0; by_weight < 2; ++by_weight) {
     uint64_t want;
     if (by_weight) {
@@ -385,18 +441,18 @@ __device__ void finish_any(const SampleLaunch& a, int n, const Settings& s, cons
       const uint64_t before = above + block_scan(mine, &all, sh.tmpu);
       if (tid < kBins && before < want && before + mine >= want) {
         sh.pick[0] = kBins - 1 - tid;
-        sh.picku[0] = before;
+        sh.picku = before;
       }
       if (tid == 0 && above + all < want) {  // not reached: everything
         sh.pick[0] = 0;
-        sh.picku[0] = above + all;
+        sh.picku = above + all;
       }
       __syncthreads();
       const uint64_t base = lo + ((uint64_t)sh.pick[0] << shift);
       const uint64_t width = ((uint64_t)1 << shift) - 1;
       if (hi - base > width) hi = base + width;
       lo = base;
-      above = sh.picku[0];
+      above = sh.picku;
       __syncthreads();
     }
     last = max(last, lo);
@@ -410,324 +466,364 @@ __device__ void finish_any(const SampleLaunch& a, int n, const Settings& s, cons
     }
   }
   const Kept kept{last, least};
+  const int per = (V + kFinishThreads - 1) / kFinishThreads;
+  const int i0 = min(V, tid * per), i1 = min(V, i0 + per);
   double part = 0.0, all;
-  for (int i = tid; i < V; i += kFinishThreads) {
+  for (int i = i0; i < i1; ++i) {
     const float x = logit(row, i);
     if (kept(x, i)) part += weight(x);
   }
-  block_scan(part, &all, sh.tmp);
+  const double before = block_scan(part, &all, sh.tmp);
   const float u = a.u[n];
   const double at = u > 0.f ? (double)u * all : 0.0;
-  draw_in(a, n, row, 0, V, at, all, kept, weight, sh);
+  if (tid == pick_thread(before, part, at, sh)) {
+    double cum = before, w_of = 0.0;
+    int token = -1;
+    for (int i = i0; i < i1; ++i) {
+      const float x = logit(row, i);
+      const double w = kept(x, i) ? weight(x) : 0.0;
+      if (w > 0.0 && (token < 0 || cum <= at)) {
+        token = i;
+        w_of = w;
+      }
+      cum += w;
+    }
+    answer(a, n, token, w_of / all);
+  }
 }
 
-template <typename T>
-__global__ __launch_bounds__(kFinishThreads) void sample_finish_kernel(SampleLaunch a, int n_slices) {
-  __shared__ FinishShared sh;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = blockIdx.x, V = a.V;
-  const Settings s = settings_of(a, n);
-  const T* row = reinterpret_cast<const T*>(a.logits) + (int64_t)n * a.stride;
-  constexpr int64_t kStep = sizeof(SliceInfo) + kBins * 8;
-  const char* in = static_cast<const char*>(a.ws) + (int64_t)n * n_slices * kStep;
-  auto bins_of = [&](int i) { return reinterpret_cast<const unsigned long long*>(in + i * kStep + sizeof(SliceInfo)); };
-
-  for (int i = tid; i < n_slices; i += kFinishThreads) sh.info[i] = *reinterpret_cast<const SliceInfo*>(in + i * kStep);
-  for (int i = tid; i < kMaxSlices / 32; i += kFinishThreads) sh.wanted[i] = 0;
-  if (tid < 4) sh.pick[tid] = kBins;
-  __syncthreads();
-  float mx = -INFINITY;
-  int top = -0x7FFFFFFF;
-  bool beyond = false, left = false;
-  for (int i = 0; i < n_slices; ++i) {
-    mx = fmaxf(mx, sh.info[i].max);
-    left = left || sh.info[i].left;
-    if (sh.info[i].n_bins < 0) beyond = true;
-    else if (sh.info[i].max > -INFINITY) top = max(top, sh.info[i].top);
-  }
-  if (mx == -INFINITY) {
-    if (tid == 0) answer(a, n, -1, 0.0);
-    return;
-  }
-  if (beyond) {
-    finish_any(a, n, s, row, mx, sh);
-    return;
-  }
-  const float scale = s.scale;
+// A row from its slices' bins; false where they do not suffice.
+template <typename T, int E>
+__device__ __forceinline__ bool finish_bins(const SampleLaunch& a, int n, int n_slices, const Settings& s, const T* row, const char* in,
+                                            float mx, int top, bool left, FinishShared& sh) {
+  constexpr int kSlice = kFinishThreads * 8 * E;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const float u = a.u[n];
-  // A weight relative to the edge of the row's top bin.
+  auto words_of = [&](int i) { return reinterpret_cast<const unsigned long long*>(in + i * kSliceBytes + sizeof(SliceInfo)); };
+  const float scale = s.scale;
+  auto logit_of = [](uint64_t w) { return float_of_key((uint32_t)(w >> 32)); };
+  // A weight relative to the edge of the row's top bin, in units.
   auto weight = [=](float x) -> double {
     const float b = bin_of(x, scale);
-    return rintf(over_edge(x, scale, b) * kUnit) * pow2(((double)b - top) * 0.125);
+    return (double)rintf(over_edge(x, scale, b) * kUnit) * eighths(top - (int)b);
+  };
+  // Each slice's weight outside its bins, relative to the row's largest.
+  auto rest_of = [&](int i) -> double {
+    return i < n_slices && sh.info[i].max > -INFINITY ? sh.info[i].rest * exp2(((double)sh.info[i].max - (double)mx) * (double)scale)
+                                                      : 0.0;
   };
 
   if (s.k == 0 && s.p >= 1.f && s.m == 0.f) {
     // Everything is kept: the slice by the slices' sums, then the token.
-    double w = tid < n_slices && sh.info[tid].max > -INFINITY
-                   ? sh.info[tid].rest * pow2(((double)sh.info[tid].max - (double)mx) * (double)scale)
-                   : 0.0;
+    const double w = rest_of(tid);
     double all;
     const double before = block_scan(w, &all, sh.tmp);
-    const double at = u > 0.f ? fmin((double)u * all, all) : 0.0;
-    if (tid == 0) sh.pick[0] = -1, sh.pick[1] = 0x7FFFFFFF;
+    const double at = u > 0.f ? (double)u * all : 0.0;
+    const int slice = pick_thread(before, w, at, sh);
+    if (tid == slice) sh.pickd = before;
     __syncthreads();
-    if (w > 0.0) atomicMax(&sh.pick[0], tid);
-    if (w > 0.0 && before + w > at) atomicMin(&sh.pick[1], tid);
-    __syncthreads();
-    const int slice = sh.pick[1] == 0x7FFFFFFF ? sh.pick[0] : sh.pick[1];
-    if (tid == slice) sh.value[0] = before;
-    __syncthreads();
-    const double start = sh.value[0];
-    auto plain = [=](float x) -> double {
-      return x == mx ? 1.0 : pow2(((double)x - (double)mx) * (double)scale);
-    };
-    draw_in(a, n, row, slice * kSlice, min(V, (slice + 1) * kSlice), at - start, all, Kept{0, -INFINITY}, plain, sh);
-    return;
+    auto plain = [=](float x) -> double { return (double)__builtin_amdgcn_exp2f((x - mx) * scale); };
+    draw_slice<T, E>(a, n, row, slice, at - sh.pickd, all, Kept{0, -INFINITY}, plain, sh);
+    return true;
   }
 
-  // The row's bins, and the first one (from the top) at which the kept tokens
-  // have ended for sure: `end`.
+  // The row's bins.
   uint64_t units = 0, count = 0;
   if (tid < kBins) {
     for (int i = 0; i < n_slices; ++i) {
-      if (sh.info[i].max == -INFINITY) continue;
-      const int j = tid - (top - sh.info[i].top);
-      if (j >= 0 && j < sh.info[i].n_bins) {
-        const uint64_t x = bins_of(i)[j];
+      const SliceInfo& f = sh.info[i];
+      const int j = tid - (top - f.top);
+      if (f.max > -INFINITY && j >= 0 && j < f.n_bins) {
+        const uint64_t x = words_of(i)[j];
         count += x >> kCountShift;
-        units += x & ((1ull << kCountShift) - 1);
+        units += x & kUnitMask;
       }
     }
   }
-  const double here = (double)units * pow2(-0.125 * tid);
+  const double here = (double)units * eighths(tid < kBins ? tid : 0);
   uint64_t all_c;
   double all_w;
   const uint64_t before_c = block_scan(count, &all_c, sh.tmpu);
   const double before_w = block_scan(here, &all_w, sh.tmp);
-  double least = -INFINITY;
-  if (s.m > 0.f) least = (double)mx + log2((double)s.m) / (double)scale;
-  double target = 0.0;
-  if (s.k > 0) {
-    if (tid < kBins && before_c < (uint64_t)s.k && before_c + count >= (uint64_t)s.k) sh.pick[0] = tid;
-  } else if (s.p < 1.f) {
-    // The sum of everything: the bins and the slices' rests.
-    double rest = tid < n_slices && sh.info[tid].max > -INFINITY
-                      ? sh.info[tid].rest * kUnit * pow2((double)sh.info[tid].max * (double)scale - 0.125 * top)
-                      : 0.0;
+  if (tid < kBins) {
+    sh.before_c[tid] = before_c;
+    sh.before_w[tid] = before_w;
+    if (tid == kBins - 1) {
+      sh.before_c[kBins] = all_c;
+      sh.before_w[kBins] = all_w;
+    }
+  }
+  const float least = least_of(s, mx);
+  double target = INFINITY;
+  if (s.k == 0 && s.p < 1.f) {
+    // Of the sum of everything: the bins and the slices' rests.
     double all_rest;
-    block_scan(rest, &all_rest, sh.tmp);
-    target = (double)s.p * (all_w + all_rest);
-    if (tid < kBins && before_w < target && before_w + here >= target) sh.pick[0] = tid;
+    block_scan(rest_of(tid), &all_rest, sh.tmp);
+    target = (double)s.p * (all_w + all_rest * (kUnit * exp2((double)mx * (double)scale - 0.125 * top)));
+  }
+  __syncthreads();
+  // The first bin, from the top, down to which the top k lie (or the top-p
+  // target) and the min-p limit's: the kept tokens end at `end`.
+  if (tid < kBins) {
+    const bool by_k = s.k > 0 && before_c < (uint64_t)s.k && sh.before_c[tid + 1] >= (uint64_t)s.k;
+    const bool by_p = s.k == 0 && s.p < 1.f && before_w < target && sh.before_w[tid + 1] >= target;
+    if (by_k || by_p) sh.pick[0] = tid;
   }
   if (tid == 0 && s.m > 0.f) {
-    const double j = (double)top - (double)bin_of((float)least, scale);
+    const float j = (float)top - bin_of(least, scale);
     if (j < kBins) sh.pick[1] = (int)j;
   }
   __syncthreads();
   int end = sh.pick[0];
   if (s.k == 0) end = min(end, sh.pick[1]);
   else if (all_c < (uint64_t)s.k && !left) end = kBins - 1;  // fewer than k tokens: all of them
-  if (end == kBins) {  // below the bins
-    finish_any(a, n, s, row, mx, sh);
-    return;
-  }
-  // Tokens down to `end`, or the last bin's alone if those are too many.
-  if (tid == end) {
-    sh.picku[0] = before_c + count;
-    sh.picku[1] = before_c;
-    sh.value[0] = before_w;
-  }
-  __syncthreads();
-  const uint64_t down_to = sh.picku[0], in_last = down_to - sh.picku[1];
-  const bool whole = down_to <= kList;
-  if (!whole && (in_last > kList || s.k > 0)) {
-    finish_any(a, n, s, row, mx, sh);
-    return;
-  }
-  const double above = whole ? 0.0 : sh.value[0];
-  const int from = whole ? 0 : end;
-  __syncthreads();
-  if (tid == 0) sh.pick[2] = 0;
-  // Slices with such tokens.
-  for (int i = wave; i < n_slices; i += kFinishThreads / 64) {
-    if (sh.info[i].max == -INFINITY) continue;
-    const int off = top - sh.info[i].top;
-    bool any = false;
-    for (int j = from + lane; j <= end; j += 64) any = any || (j - off >= 0 && j - off < sh.info[i].n_bins && bins_of(i)[j - off]);
-    if (__any(any) && lane == 0) atomicOr(&sh.wanted[i / 32], 1u << (i % 32));
-  }
-  __syncthreads();
-  const float first = (float)top - from, lastb = (float)top - end;
-  for (int i = wave; i < n_slices * (kSlice / 512); i += kFinishThreads / 64) {
-    const int slice = i / (kSlice / 512);
-    if (!(sh.wanted[slice / 32] >> (slice % 32) & 1)) continue;
-    const int at = i * 512 + lane * 8;
-    T raw[8];
-    float x[8];
-    if (at + 8 <= V) {
-      __builtin_memcpy(raw, row + at, sizeof(raw));
-#pragma unroll
-      for (int c = 0; c < 8; ++c) x[c] = clean((float)raw[c]);
-    } else {
-#pragma unroll
-      for (int c = 0; c < 8; ++c) x[c] = at + c < V ? logit(row, at + c) : -INFINITY;
-    }
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      const float b = bin_of(x[c], scale);
-      if (b <= first && b >= lastb) {
-        const int slot = atomicAdd(&sh.pick[2], 1);
-        if (slot < kList) sh.list[slot] = word_of(x[c], at + c);
+  if (end >= kBins) return false;  // below the bins
+
+  // Calls f(slice, logit, index) for the tokens in bins from .. to, from the
+  // slices' lists or, of slices that have such tokens and no list, from the logits.
+  auto visit = [&](int from, int to, auto f) {
+    const float first = (float)(top - from), last = (float)(top - to);
+    auto inside = [&](float x) {
+      const float b = bin_of(x, scale);
+      return b <= first && b >= last;
+    };
+    for (int i = wave; i < n_slices; i += kFinishThreads / 64) {
+      for (int c = lane; c < sh.info[i].n_list; c += 64) {
+        const uint64_t w = words_of(i)[kBins + c];
+        if (inside(logit_of(w))) f(i, logit_of(w), ~(uint32_t)w);
       }
     }
-  }
-  __syncthreads();
-  const int m = min(sh.pick[2], kList);
-  int padded = 64;
-  while (padded < m) padded *= 2;
-  for (int i = m + tid; i < padded; i += kFinishThreads) sh.list[i] = 0;
-  sort_falling(sh.list, padded);
+    constexpr int kBatch = 8 / (int)sizeof(T);  // runs of 8 in flight per thread
+    const int n_runs = n_slices * E;
+    for (int c0 = 0; c0 < n_runs; c0 += kBatch) {
+      T raw[kBatch][8];
+      uint32_t runs = 0, mask = 0;
+      auto start = [&](int b) { return ((c0 + b) * kFinishThreads + tid) * 8; };
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        const int slice = (c0 + b) / E;
+        if (slice < n_slices) {
+          const SliceInfo& g = sh.info[slice];
+          const int off = top - g.top;
+          if (g.max > -INFINITY && g.n_list < 0 && to >= off && from - off < g.n_bins) runs |= 1u << b;
+        }
+        if (runs >> b & 1 && start(b) + 8 <= a.V) __builtin_memcpy(raw[b], row + start(b), sizeof(raw[b]));
+      }
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b)
+        if (runs >> b & 1) {
+          if (start(b) + 8 <= a.V) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c) mask |= inside(clean((float)raw[b][c])) ? 1u << (8 * b + c) : 0u;
+          } else {
+            for (int c = 0; start(b) + c < a.V; ++c) mask |= inside(logit(row, start(b) + c)) ? 1u << (8 * b + c) : 0u;
+          }
+        }
+      for (; mask; mask &= mask - 1) {  // few
+        const int c = __builtin_ctz(mask), b = c / 8, i = start(b) + c % 8;
+        f((c0 + b) / E, logit(row, i), (uint32_t)i);
+      }
+    }
+    __syncthreads();
+  };
+  // The tokens of bins from .. to with words in [lo, hi], at most kList: one
+  // word per thread in falling order (0 past their number).
+  auto collect = [&](int from, int to, uint64_t lo, uint64_t hi) -> uint64_t {
+    if (tid == 0) sh.pick[2] = 0;
+    if (tid < kMaxSlices) sh.extra[tid] = 0;
+    __syncthreads();
+    visit(from, to, [&](int slice, float x, uint32_t i) {
+      const uint64_t w = word_of(x, i);
+      if (w > hi) {
+        atomicAdd(&sh.extra[slice], (unsigned long long)rintf(over_edge(x, scale, bin_of(x, scale)) * kUnit));
+      } else if (w >= lo) {
+        const int at = atomicAdd(&sh.pick[2], 1);
+        if (at < kList) sh.list[at] = w;
+      }
+    });
+    const int m = min(sh.pick[2], kList);
+    int size = 64;
+    while (size < m) size *= 2;
+    const uint64_t w = tid < m ? sh.list[tid] : 0;
+    __syncthreads();
+    return sort_falling(w, size, sh.list);
+  };
 
-  // The kept ones among them, in falling order; a thread takes a run.
-  const int per = (padded + kFinishThreads - 1) / kFinishThreads;
-  const int lo = min(m, tid * per), hi = min(m, lo + per);
-  double sum = 0.0;
-  for (int i = lo; i < hi; ++i) {
-    const double w = weight(float_of_key((uint32_t)(sh.list[i] >> 32)));
-    sh.value[i] = w;
-    if (s.k == 0 || i < s.k) sum += w;
+  // All kept tokens, if few, or those at the end of the last bin, above which
+  // `above` tokens of weight `above_w` are kept; and each one's weight.  With a
+  // top-p limit on the top k in two steps: the top k's sum, then the bin in which
+  // a part of it is reached.
+  const bool whole = sh.before_c[end + 1] <= kList;
+  uint64_t v = 0, above = 0;
+  double w = 0.0, above_w = 0.0, sum;
+  for (bool sum_k = s.k > 0 && s.p < 1.f;; sum_k = false) {
+    if (!sum_k && !whole && s.k > 0) {
+      __syncthreads();
+      if (tid == 0) sh.pick[0] = end;
+      __syncthreads();
+      if (tid < end && sh.before_w[tid] < target && sh.before_w[tid + 1] >= target) sh.pick[0] = tid;
+      __syncthreads();
+      end = min(end, min(sh.pick[0], sh.pick[1]));
+    }
+    uint64_t w_lo = 0, w_hi = ~(uint64_t)0;
+    if (!whole) {
+      const int e = end, k = s.k;
+      above = sh.before_c[e];
+      above_w = sh.before_w[e];
+      uint64_t n_here = sh.before_c[e + 1] - above;
+      // Too many: the part of the bin in which the kept tokens end, by the bins'
+      // way of search over the words, 256 parts a pass.
+      const float b = (float)(top - e);
+      // (the bin's edges, wider by what their rounding may be)
+      uint64_t lo = (uint64_t)(float_order_key(b == 0.f ? -0x1p-60f : b / (8.f * scale)) - 16) << 32;
+      uint64_t hi = (uint64_t)(float_order_key((b + 1.f) / (8.f * scale)) + 16) << 32;
+      for (int pass = 0; pass < 8 && n_here > kList; ++pass) {
+        const int shift = max(0, 64 - 8 - __builtin_clzll((hi - lo) | 255));
+        auto part_of = [&](uint64_t x) { return x < lo ? 0 : x > hi ? kBins - 1 : min(kBins - 1, (int)((x - lo) >> shift)); };
+        __syncthreads();
+        if (tid < kBins) sh.bins[tid] = 0;
+        if (tid == 0) sh.pick[0] = kBins - 1;
+        __syncthreads();
+        visit(e, e, [&](int, float x, uint32_t i) {
+          const uint64_t word = word_of(x, i);
+          if (word >= w_lo && word <= w_hi)
+            atomicAdd(&sh.bins[part_of(word)], (1ull << kCountShift) + (uint32_t)rintf(over_edge(x, scale, b) * kUnit));
+        });
+        const uint64_t mine = tid < kBins ? sh.bins[kBins - 1 - tid] : 0;  // from the top
+        uint64_t all;
+        const uint64_t before = block_scan(mine, &all, sh.tmpu);
+        auto c_of = [&](uint64_t x) { return above + (x >> kCountShift); };
+        auto w_of = [&](uint64_t x) { return above_w + (double)(x & kUnitMask) * eighths(e); };
+        if (tid < kBins) {
+          const bool by_k = k > 0 && c_of(before) < (uint64_t)k && c_of(before + mine) >= (uint64_t)k;
+          const bool by_p = !sum_k && w_of(before) < target && w_of(before + mine) >= target;
+          const bool by_m = !sum_k && s.m > 0.f && sh.pick[1] == e && tid == kBins - 1 - part_of((uint64_t)float_order_key(least) << 32);
+          if (by_k || by_p || by_m) atomicMin(&sh.pick[0], tid);
+        }
+        __syncthreads();
+        const int at = sh.pick[0];
+        if (tid == at) {
+          sh.picku = before;
+          sh.pickd = (double)(mine >> kCountShift);
+        }
+        __syncthreads();
+        above = c_of(sh.picku);
+        above_w = w_of(sh.picku);
+        n_here = (uint64_t)sh.pickd;
+        const int part = kBins - 1 - at;
+        const uint64_t p_lo = lo + ((uint64_t)part << shift), p_hi = p_lo + (((uint64_t)1 << shift) - 1);
+        if (part > 0) w_lo = max(w_lo, p_lo);
+        if (part < kBins - 1) w_hi = p_hi < w_hi ? p_hi : w_hi;
+        lo = max(w_lo, lo);
+        hi = w_hi < hi ? w_hi : hi;
+      }
+      if (n_here > kList) return false;
+    }
+    v = collect(whole ? 0 : end, end, w_lo, w_hi);
+    w = v ? weight(logit_of(v)) : 0.0;
+    if (!sum_k) break;
+    block_scan(above + tid < (uint64_t)s.k ? w : 0.0, &sum, sh.tmp);
+    target = (double)s.p * (above_w + sum);
+    if (whole) break;
   }
-  double sum_k;
-  const double before = above + block_scan(sum, &sum_k, sh.tmp);
-  if (s.k > 0) target = (double)s.p * sum_k;
-  double cum = before, kept_sum = 0.0;
-  int n_kept = 0;
-  for (int i = lo; i < hi; ++i) {
-    const bool by_k = s.k == 0 || i < s.k;
-    const bool by_p = s.p >= 1.f || cum < target || (i == 0 && above == 0.0);
-    const bool by_m = (double)float_of_key((uint32_t)(sh.list[i] >> 32)) >= least;
-    cum += sh.value[i];
-    if (!(by_k && by_p && by_m)) break;  // each holds for a leading part
-    ++n_kept;
-    kept_sum += sh.value[i];
-  }
-  uint64_t n_all;
-  block_scan((uint64_t)n_kept, &n_all, sh.tmpu);
+  bool keep = v != 0 && (s.k == 0 || above + tid < (uint64_t)s.k);
+  const double before = above_w + block_scan(keep ? w : 0.0, &sum, sh.tmp);
+  keep = keep && (before < target || (tid == 0 && above == 0)) && logit_of(v) >= least;
+  const int n_kept = __syncthreads_count(keep);  // they come first
   double total;
-  block_scan(kept_sum, &total, sh.tmp);
-  total += above;
-  const double at = u > 0.f ? fmin((double)u, 1.0) * total : 0.0;
+  block_scan(keep ? w : 0.0, &total, sh.tmp);
+  total += above_w;
+  const double at = u > 0.f ? (double)u * total : 0.0;
 
   if (whole) {
-    // In order of index: the words become (index, place).
-    const int keep = (int)n_all;
+    // In order of index (the words turned round).
     int size = 64;
-    while (size < keep) size *= 2;
-    uint64_t mine[kList / kFinishThreads];
-#pragma unroll
-    for (int c = 0; c < kList / kFinishThreads; ++c) {
-      const int i = tid + c * kFinishThreads;
-      mine[c] = i < keep ? (sh.list[i] << 32) | (uint32_t)(sh.list[i] >> 32) : 0;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int c = 0; c < kList / kFinishThreads; ++c) {
-      const int i = tid + c * kFinishThreads;
-      if (i < size) sh.list[i] = mine[c];
-    }
-    sort_falling(sh.list, size);  // ~index falls: indexes rise
-    const int pr = (size + kFinishThreads - 1) / kFinishThreads;
-    const int l0 = min(keep, tid * pr), l1 = min(keep, l0 + pr);
-    double part = 0.0, all;
-    int last = -1;
-    for (int i = l0; i < l1; ++i) {
-      const double w = weight(float_of_key((uint32_t)sh.list[i]));
-      sh.value[i] = w;
-      part += w;
-      if (w > 0.0) last = i;
-    }
-    const double b0 = block_scan(part, &all, sh.tmp);
-    if (tid == 0) sh.pick[0] = -1, sh.pick[1] = 0x7FFFFFFF;
-    __syncthreads();
-    if (last >= 0) atomicMax(&sh.pick[0], last);
-    if (part > 0.0 && b0 + part > at) {
-      double c = b0;
-      for (int i = l0; i < l1; ++i) {
-        c += sh.value[i];
-        if (sh.value[i] > 0.0 && c > at) {
-          atomicMin(&sh.pick[1], i);
-          break;
-        }
-      }
-    }
-    __syncthreads();
-    if (tid == 0) {
-      const int i = sh.pick[1] == 0x7FFFFFFF ? sh.pick[0] : sh.pick[1];
-      answer(a, n, (int)~(uint32_t)(sh.list[i] >> 32), sh.value[i] / total);
-    }
-    return;
+    while (size < n_kept) size *= 2;
+    v = sort_falling(keep ? v << 32 | v >> 32 : 0, size, sh.list);
+    w = v ? weight(float_of_key((uint32_t)v)) : 0.0;
+    const double b0 = block_scan(w, &sum, sh.tmp);
+    if (tid == pick_thread(b0, w, at, sh)) answer(a, n, (int)~(uint32_t)(v >> 32), w / total);
+    return true;
   }
 
-  // Many kept tokens: the slice by the kept weight of each, then the token.
+  // The slice by the kept weight of each, then the token.  If no token of the
+  // last bin is kept, the words of those above it are larger than any of the bin's.
+  sh.list[tid] = keep ? v : 0;
+  if (tid == (n_kept ? n_kept - 1 : 0)) sh.picku = n_kept ? v : v + 1;
   __syncthreads();
-  if (tid == 0) sh.picku[0] = n_all ? sh.list[n_all - 1] : ~0ull;
-  __syncthreads();
-  // No token of the last bin kept: those above it, whose words are larger than
-  // any of the bin's.
-  const uint64_t last = n_all ? sh.picku[0] : sh.list[0] + 1;
-  const Kept kept{last, least};
-  __syncthreads();
-  for (int i = tid; i < n_slices; i += kFinishThreads) sh.slice_w[i] = 0.0;
+  const Kept kept{sh.picku, least};
   for (int i = wave; i < n_slices; i += kFinishThreads / 64) {
-    if (sh.info[i].max == -INFINITY) continue;
-    const int off = top - sh.info[i].top;
-    double w = 0.0;
-    for (int j = lane; j < end; j += 64)
-      if (j - off >= 0 && j - off < sh.info[i].n_bins)
-        w += (double)(bins_of(i)[j - off] & ((1ull << kCountShift) - 1)) * pow2(-0.125 * j);
+    const SliceInfo& f = sh.info[i];
+    const int off = top - f.top;
+    double part = 0.0;
+    if (f.max > -INFINITY) {
+      for (int j = lane; j < end; j += 64)
+        if (j - off >= 0 && j - off < f.n_bins) part += (double)(words_of(i)[j - off] & kUnitMask) * eighths(j);
+      if (lane == 0) part += (double)sh.extra[i] * eighths(end);
+      for (int j = lane; j < n_kept; j += 64)
+        if ((int)(~(uint32_t)sh.list[j] / kSlice) == i) part += weight(logit_of(sh.list[j]));
+    }
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) w += __shfl_xor(w, d);
-    double extra = 0.0;
-    for (uint32_t j = lane; j < (uint32_t)n_all; j += 64)
-      if ((int)(~(uint32_t)sh.list[j] / kSlice) == i) extra += sh.value[j];
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) extra += __shfl_xor(extra, d);
-    if (lane == 0) sh.slice_w[i] = w + extra;
+    for (int d = 1; d < 64; d *= 2) part += __shfl_xor(part, d);
+    if (lane == 0) sh.slice_w[i] = part;
   }
   __syncthreads();
-  const double w = tid < n_slices ? sh.slice_w[tid] : 0.0;
-  double all;
-  const double b0 = block_scan(w, &all, sh.tmp);
-  if (tid == 0) sh.pick[0] = -1, sh.pick[1] = 0x7FFFFFFF;
+  const double part = tid < n_slices ? sh.slice_w[tid] : 0.0;
+  const double b0 = block_scan(part, &sum, sh.tmp);
+  const int slice = pick_thread(b0, part, at, sh);
+  if (tid == slice) sh.pickd = b0;
   __syncthreads();
-  if (w > 0.0) atomicMax(&sh.pick[0], tid);
-  if (w > 0.0 && b0 + w > at) atomicMin(&sh.pick[1], tid);
+  draw_slice<T, E>(a, n, row, slice, at - sh.pickd, total, kept, weight, sh);
+  return true;
+}
+
+template <typename T, int E>
+__global__ __launch_bounds__(kFinishThreads) void sample_finish_kernel(SampleLaunch a, int n_slices) {
+  __shared__ FinishShared sh;
+  const int tid = threadIdx.x, n = blockIdx.x;
+  const Settings s = settings_of(a, n);
+  const T* row = reinterpret_cast<const T*>(a.logits) + (int64_t)n * a.stride;
+  const char* in = static_cast<const char*>(a.ws) + (int64_t)n * n_slices * kSliceBytes;
+  if (tid < n_slices) sh.info[tid] = *reinterpret_cast<const SliceInfo*>(in + tid * kSliceBytes);
+  if (tid < 4) sh.pick[tid] = kBins;
   __syncthreads();
-  const int slice = sh.pick[1] == 0x7FFFFFFF ? sh.pick[0] : sh.pick[1];
-  if (tid == slice) sh.value[0] = b0;
-  __syncthreads();
-  const double start = sh.value[0];
-  draw_in(a, n, row, slice * kSlice, min(V, (slice + 1) * kSlice), at - start, total, kept, weight, sh);
+  float mx = -INFINITY;
+  int top = -0x7FFFFFFF;
+  bool beyond = false, left = false;
+  for (int i = 0; i < n_slices; ++i) {
+    const SliceInfo& f = sh.info[i];
+    mx = fmaxf(mx, f.max);
+    left = left || f.left;
+    beyond = beyond || f.n_bins < 0;
+    if (f.n_bins >= 0 && f.max > -INFINITY) top = max(top, f.top);
+  }
+  if (mx == -INFINITY) {
+    if (tid == 0) answer(a, n, -1, 0.0);
+    return;
+  }
+  if (!beyond && finish_bins<T, E>(a, n, n_slices, s, row, in, mx, top, left, sh)) return;
+  finish_any(a, n, s, row, mx, sh);
 }
 
 }  // namespace
 
-size_t sample_workspace(int N, int V, int) {
-  return (size_t)N * ((V + kSlice - 1) / kSlice) * (sizeof(SliceInfo) + kBins * 8);
-}
+size_t sample_workspace(int N, int V, int) { return (size_t)N * ((V + slice_of(V) - 1) / slice_of(V)) * kSliceBytes; }
 
 hipError_t launch_sample(const SampleLaunch& a, int dtype, hipStream_t stream) {
-  const int n_slices = (a.V + kSlice - 1) / kSlice;
-  const dim3 grid((unsigned)n_slices, (unsigned)a.N);
-  if (dtype == NACL_F32) {
-    sample_slices_kernel<float><<<grid, kSliceThreads, 0, stream>>>(a, n_slices);
+  const int slice = slice_of(a.V), n_slices = (a.V + slice - 1) / slice;
+  auto run = [&](auto slices, auto finish) {
+    slices<<<dim3((unsigned)n_slices, (unsigned)a.N), kSliceThreads, 0, stream>>>(a, n_slices);
     if (hipError_t e = hipGetLastError()) return e;
-    sample_finish_kernel<float><<<a.N, kFinishThreads, 0, stream>>>(a, n_slices);
-  } else {
-    sample_slices_kernel<__bf16><<<grid, kSliceThreads, 0, stream>>>(a, n_slices);
-    if (hipError_t e = hipGetLastError()) return e;
-    sample_finish_kernel<__bf16><<<a.N, kFinishThreads, 0, stream>>>(a, n_slices);
-  }
-  return hipGetLastError();
+    finish<<<a.N, kFinishThreads, 0, stream>>>(a, n_slices);
+    return hipGetLastError();
+  };
+  static_assert(kFinishThreads == 2 * kSliceThreads, "a slice in the finish");
+  const bool large = slice > kMinSlice;
+  if (dtype == NACL_F32)
+    return large ? run(sample_slices_kernel<float, 4>, sample_finish_kernel<float, 2>)
+                 : run(sample_slices_kernel<float, 2>, sample_finish_kernel<float, 1>);
+  return large ? run(sample_slices_kernel<__bf16, 4>, sample_finish_kernel<__bf16, 2>)
+               : run(sample_slices_kernel<__bf16, 2>, sample_finish_kernel<__bf16, 1>);
 }
 
 }  // namespace nacl

@@ -56,13 +56,22 @@ def test_exact_draws(V, dtype):
 
 
 def _allowed(x, u, t, k, p, m):
-    """Tokens within rounding of the borders, and ln of each one's probability.
-    A weight's exponent is a product rounded to fp32, so it is off by |ln w|
+    """(token, ln of its probability) for u and top_p within rounding of theirs: a
+    token at a border is kept or not, which moves the sum by its whole share.  A weight's exponent is a product rounded to fp32, so it is off by |ln w|
     2^-22 at most and the sums by their weighted mean of it, below ln V 2^-22 <
     2^-18; fixed-point units add V 2^-44."""
     d = 2.0 ** -18
-    return dict(draw_token(x, min(max(u + du, 0.0), 1.0), t, k, p if p >= 1 else max(p + dp, 0.0), m)
-                for du in (-d, 0, d) for dp in (-d, 0, d))
+    return [draw_token(x, min(max(u + du, 0.0), 1.0), t, k, p if p >= 1 else max(p + dp, 0.0), m)
+            for du in (-d, 0, d) for dp in (-d, 0, d)]
+
+
+def _right(x, token, lp, ok, t):
+    """A token's share may be less than the borders' rounding, so any kept one
+    between the outermost is right, with its own probability in one of the sums."""
+    if not min(i for i, _ in ok) <= token <= max(i for i, _ in ok):
+        return False
+    of = lambda i, l: l if token == i else l + (x[token] - x[i]) / t
+    return any(abs(lp - of(i, l)) <= 1e-4 + 2.0 ** -22 * abs(lp) for i, l in ok)
 
 
 @pytest.mark.parametrize("N,V,dtype", [(1, 32000, torch.float32), (7, 50257, torch.bfloat16), (40, 4099, torch.float32),
@@ -84,8 +93,7 @@ def test_draws(N, V, dtype):
     got, lps = _sample(x, u, t, k, p, m)
     for n in range(min(N, 40)):
         ok = _allowed(ref[n], u[n], t[n], k[n], p[n], m[n])
-        assert got[n] in ok, (n, got[n], ok, t[n], k[n], p[n], m[n])
-        assert abs(lps[n] - ok[got[n]]) <= 1e-4 + 2.0 ** -22 * abs(lps[n])
+        assert got[n] in dict(ok) and _right(ref[n], got[n], lps[n], ok, t[n]), (n, got[n], lps[n], ok, t[n], k[n], p[n], m[n])
 
 
 def test_odd_rows():
@@ -150,3 +158,35 @@ def test_graph_replays():
         want, wlp = nacl.sample(x, u, top_p=p)
         torch.cuda.synchronize()
         assert torch.equal(tok, want) and torch.equal(lp, wlp)
+
+
+@pytest.mark.parametrize("V,dtype", [(65536, torch.float32), (65537, torch.bfloat16), (150001, torch.bfloat16)])
+@pytest.mark.parametrize("kind", ["flat", "one_bin", "few", "ramp"])
+def test_shapes_of_rows(V, dtype, kind):
+    """Flat rows (thousands kept), all tokens in one bin, a handful of tokens in
+    a masked vocabulary, falling logits; with every kind of limit."""
+    g = torch.Generator().manual_seed(V)
+    N = 10
+    if kind == "flat":
+        x = torch.randn((N, V), generator=g) * 0.5
+    elif kind == "one_bin":
+        x = 3 + torch.rand((N, V), generator=g) * 1e-3
+    elif kind == "few":
+        x = torch.full((N, V), -math.inf)
+        x[:, torch.randint(0, V, (30,), generator=g)] = torch.randn((N, 30), generator=g) * 2
+    else:
+        x = (-torch.arange(V) * (20.0 / V)).expand(N, V).clone()
+    x = x.to(dtype)
+    t = [1.0, 0.7, 1.0, 1.3, 1.0, 1.0, 0.9, 1.0, 1.0, 0.0]
+    k = [0, 0, 40, 40, 3000, 20000, 0, 0, 9000, 7]
+    p = [1.0, 0.9, 1.0, 0.8, 1.0, 0.9, 0.999, 0.5, 0.25, 0.5]
+    m = [0.0, 0.0, 0.0, 0.0, 0.1, 0.0, 0.01, 0.3, 0.0, 0.0]
+    p = [float(np.float32(i)) for i in p]
+    t = [float(np.float32(i)) for i in t]
+    m = [float(np.float32(i)) for i in m]
+    u = [float(i) for i in torch.rand((N,), generator=g)]
+    got, lps = _sample(x.to(DEV), u, t, k, p, m)
+    ref = x.double().numpy()
+    for n in range(N):
+        ok = _allowed(ref[n], u[n], t[n], k[n], p[n], m[n])
+        assert _right(ref[n], got[n], lps[n], ok, t[n]), (n, got[n], lps[n], ok)
