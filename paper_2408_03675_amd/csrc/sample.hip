@@ -237,48 +237,103 @@ __global__ __launch_bounds__(kSliceThreads) void sample_slices_kernel(SampleLaun
   if (tid < min(listed, kKeep)) words[kBins + tid] = list[tid];
 }
 
+// One work-group and a long chain of steps: what counts in the finish is latency,
+// so lanes exchange by DPP and permlane moves (a few cycles) and not through LDS
+// (over a hundred).
+
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ uint32_t dpp(uint32_t old, uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)x, CTRL, ROWS, 0xF, false);
+}
+template <int CTRL, int ROWS = 0xF, typename U>
+__device__ __forceinline__ U dpp64(U x) {  // lanes without a source: 0
+  const uint64_t v = __builtin_bit_cast(uint64_t, x);
+  return __builtin_bit_cast(U, (uint64_t)dpp<CTRL, ROWS>(0, (uint32_t)(v >> 32)) << 32 | dpp<CTRL, ROWS>(0, (uint32_t)v));
+}
+// Inclusive sums over the wave: rows of 16 by shifts, then the last lane of row
+// 0 to row 1 and of row 2 to row 3, then of row 1 to rows 2 and 3.
+template <typename U>
+__device__ __forceinline__ U wave_scan(U x) {
+  x += dpp64<0x111>(x);
+  x += dpp64<0x112>(x);
+  x += dpp64<0x114>(x);
+  x += dpp64<0x118>(x);
+  x += dpp64<0x142, 0xA>(x);
+  x += dpp64<0x143, 0xC>(x);
+  return x;
+}
+// The value of lane ^ J.
+template <int J>
+__device__ __forceinline__ uint32_t swap_lanes(uint32_t x) {
+  if constexpr (J == 1) return dpp<0xB1>(x, x);
+  if constexpr (J == 2) return dpp<0x4E>(x, x);
+  if constexpr (J == 4) {
+    const uint32_t y = dpp<0x141>(x, x);  // lane ^ 7
+    return dpp<0x1B>(y, y);               // lane ^ 3
+  }
+  if constexpr (J == 8) return dpp<0x128>(x, x);
+  if constexpr (J == 16) {
+    auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return threadIdx.x & 16 ? a[0] : a[1];
+  }
+  if constexpr (J == 32) {
+    auto a = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return threadIdx.x & 32 ? a[0] : a[1];
+  }
+}
+
 // Exclusive sums in thread order and the sum of all, by a fixed tree.
 template <typename U>
-__device__ U block_scan(U x, U* total, U* tmp) {
+__device__ __forceinline__ U block_scan(U x, U* total, U* tmp) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  U s = x;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const U y = __shfl_up(s, d);
-    if (lane >= d) s += y;
-  }
-  U before = __shfl_up(s, 1);
-  if (lane == 0) before = 0;
+  const U s = wave_scan(x);
   __syncthreads();
   if (lane == 63) tmp[wave] = s;
   __syncthreads();
   U base = 0, all = 0;
+#pragma unroll
   for (int w = 0; w < kFinishThreads / 64; ++w) {
-    if (w < wave) base += tmp[w];
-    all += tmp[w];
+    const U t = tmp[w];
+    if (w < wave) base += t;
+    all += t;
   }
   *total = all;
-  return base + before;
+  return base + (s - x);
 }
 
-// Sorts words in falling order, one per thread, those of the first `size`
-// threads (a power of two from 64 on; every thread takes part).
-__device__ uint64_t sort_falling(uint64_t v, int size, uint64_t* tmp) {
+// One step of a sort: words J threads apart are put in order, those of a run of
+// `size` threads falling where the run's number is even.
+template <int J>
+__device__ __forceinline__ void sort_step(uint64_t& v, int size, uint64_t* tmp) {
   const int tid = threadIdx.x;
-  for (int k = 2; k <= size; k *= 2)
-    for (int j = k / 2; j > 0; j /= 2) {
-      uint64_t other;
-      if (j >= 64) {
-        __syncthreads();
-        tmp[tid] = v;
-        __syncthreads();
-        other = tmp[tid ^ j];
-      } else {
-        other = __shfl_xor(v, j);
-      }
-      const bool larger = ((tid & j) == 0) == ((tid & k) == 0);
-      if ((other > v) == larger) v = other;
-    }
+  uint64_t other;
+  if constexpr (J >= 64) {
+    __syncthreads();
+    tmp[tid] = v;
+    __syncthreads();
+    other = tmp[tid ^ J];
+  } else {
+    other = (uint64_t)swap_lanes<J>((uint32_t)(v >> 32)) << 32 | swap_lanes<J>((uint32_t)v);
+  }
+  const bool larger = ((tid & J) == 0) == ((tid & size) == 0);
+  if ((other > v) == larger) v = other;
+}
+// Sorts words in falling order, one per thread, those of the first `n` threads
+// (a power of two from 64 on; every thread takes part).
+__device__ __forceinline__ uint64_t sort_falling(uint64_t v, int n, uint64_t* tmp) {
+#pragma unroll 1
+  for (int size = 2; size <= n; size *= 2) {
+    if (size >= 1024) sort_step<512>(v, size, tmp);
+    if (size >= 512) sort_step<256>(v, size, tmp);
+    if (size >= 256) sort_step<128>(v, size, tmp);
+    if (size >= 128) sort_step<64>(v, size, tmp);
+    if (size >= 64) sort_step<32>(v, size, tmp);
+    if (size >= 32) sort_step<16>(v, size, tmp);
+    if (size >= 16) sort_step<8>(v, size, tmp);
+    if (size >= 8) sort_step<4>(v, size, tmp);
+    if (size >= 4) sort_step<2>(v, size, tmp);
+    sort_step<1>(v, size, tmp);
+  }
   __syncthreads();
   return v;
 }
@@ -310,6 +365,7 @@ struct FinishShared {
   double slice_w[kMaxSlices];
   unsigned long long extra[kMaxSlices];    // units of a slice's tokens of the last bin above the list's
   int pick[4];
+  int first[kFinishThreads / 64], last[kFinishThreads / 64];
   uint64_t picku;
   double pickd;
 };
@@ -334,25 +390,29 @@ __device__ __forceinline__ float least_of(const Settings& s, float mx) {
 
 __device__ __forceinline__ void answer(const SampleLaunch& a, int n, int token, double p) {
   a.tokens[n] = token;
-  if (a.logprobs) a.logprobs[n] = token < 0 ? -INFINITY : (float)log(p);
+  // (close to 1 by what is missing from it)
+  if (a.logprobs) a.logprobs[n] = token < 0 ? -INFINITY : p > 0.5 ? log1pf((float)(p - 1.0)) : logf((float)p);
 }
 
 // Threads' candidates in order: the first at which the running sum, `before` plus
 // the thread's `sum`, passes `at`; of a sum that falls short by rounding, the last
 // thread with a weight.
-__device__ int pick_thread(double before, double sum, double at, FinishShared& sh) {
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    sh.pick[2] = -1;
-    sh.pick[3] = 0x7FFFFFFF;
+__device__ __forceinline__ int pick_thread(double before, double sum, double at, FinishShared& sh) {
+  const int wave = threadIdx.x >> 6;
+  const uint64_t with = __ballot(sum > 0.0), past = __ballot(sum > 0.0 && before + sum > at);
+  if ((threadIdx.x & 63) == 0) {
+    sh.first[wave] = past ? 64 * wave + __builtin_ctzll(past) : 0x7FFFFFFF;
+    sh.last[wave] = with ? 64 * wave + 63 - __builtin_clzll(with) : -1;
   }
   __syncthreads();
-  if (sum > 0.0) {
-    atomicMax(&sh.pick[2], (int)threadIdx.x);
-    if (before + sum > at) atomicMin(&sh.pick[3], (int)threadIdx.x);
+  int first = 0x7FFFFFFF, last = -1;
+#pragma unroll
+  for (int w = 0; w < kFinishThreads / 64; ++w) {
+    first = min(first, sh.first[w]);
+    last = max(last, sh.last[w]);
   }
   __syncthreads();
-  return sh.pick[3] == 0x7FFFFFFF ? sh.pick[2] : sh.pick[3];
+  return first == 0x7FFFFFFF ? last : first;
 }
 
 // The draw among the kept tokens of a slice, of which the one is wanted at which
@@ -730,9 +790,9 @@ __device__ __forceinline__ bool finish_bins(const SampleLaunch& a, int n, int n_
   const double before = above_w + block_scan(keep ? w : 0.0, &sum, sh.tmp);
   keep = keep && (before < target || (tid == 0 && above == 0)) && logit_of(v) >= least;
   const int n_kept = __syncthreads_count(keep);  // they come first
-  double total;
-  block_scan(keep ? w : 0.0, &total, sh.tmp);
-  total += above_w;
+  if (tid == max(n_kept - 1, 0)) sh.pickd = n_kept ? before + w : above_w;
+  __syncthreads();
+  const double total = sh.pickd;
   const double at = u > 0.f ? (double)u * total : 0.0;
 
   if (whole) {
