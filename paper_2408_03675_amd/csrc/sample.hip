@@ -26,6 +26,7 @@ constexpr int kBins = 256;                               // 32 powers of two bel
 constexpr int kMaxSlices = NACL_MAX_V / (2 * kMinSlice);
 constexpr int kFinishThreads = 1024;
 constexpr int kList = kFinishThreads;                    // tokens that the finish sorts, one per thread
+constexpr int kWide = 6144;                              // tokens of a bin that it holds
 constexpr int kKeep = 128;                               // tokens that a slice lists
 constexpr float kUnit = 0x1p22f;                         // a weight over its bin's edge, in units
 constexpr int kCountShift = 43;                          // of a bin word: count above, weight units below
@@ -290,15 +291,14 @@ __device__ __forceinline__ U block_scan(U x, U* total, U* tmp) {
   __syncthreads();
   if (lane == 63) tmp[wave] = s;
   __syncthreads();
-  U base = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < kFinishThreads / 64; ++w) {
-    const U t = tmp[w];
-    if (w < wave) base += t;
-    all += t;
-  }
-  *total = all;
-  return base + (s - x);
+  const U t = tmp[lane & 15], sums = wave_scan(lane < 16 ? t : U(0));  // of the 16 waves
+  auto of = [&](int i) {
+    const uint64_t v = __builtin_bit_cast(uint64_t, sums);
+    return __builtin_bit_cast(U, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), i) << 32 |
+                                     (uint32_t)__builtin_amdgcn_readlane((int)v, i));
+  };
+  *total = of(15);
+  return (wave ? of(__builtin_amdgcn_readfirstlane(wave) - 1) : U(0)) + (s - x);
 }
 
 // One step of a sort: words J threads apart are put in order, those of a run of
@@ -319,14 +319,17 @@ __device__ __forceinline__ void sort_step(uint64_t& v, int size, uint64_t* tmp) 
   if ((other > v) == larger) v = other;
 }
 // Sorts words in falling order, one per thread, those of the first `n` threads
-// (a power of two from 64 on; every thread takes part).
-__device__ __forceinline__ uint64_t sort_falling(uint64_t v, int n, uint64_t* tmp) {
+// (a power of two from 64 on; every thread takes part, the waves past them only
+// in the barriers).
+__device__ __noinline__ uint64_t sort_falling(uint64_t v, int n, uint64_t* tmp) {
+  const bool mine = (int)(threadIdx.x & ~63u) < n;
 #pragma unroll 1
   for (int size = 2; size <= n; size *= 2) {
     if (size >= 1024) sort_step<512>(v, size, tmp);
     if (size >= 512) sort_step<256>(v, size, tmp);
     if (size >= 256) sort_step<128>(v, size, tmp);
     if (size >= 128) sort_step<64>(v, size, tmp);
+    if (!mine) continue;
     if (size >= 64) sort_step<32>(v, size, tmp);
     if (size >= 32) sort_step<16>(v, size, tmp);
     if (size >= 16) sort_step<8>(v, size, tmp);
@@ -338,8 +341,11 @@ __device__ __forceinline__ uint64_t sort_falling(uint64_t v, int n, uint64_t* tm
   return v;
 }
 
-// 2^(-j / 8).
-__device__ __forceinline__ double eighths(int j) {
+// 2^(-j / 8); root: of j from 0 to 7.
+__device__ __forceinline__ double eighths(const double* root, int j) { return ldexp(root[j & 7], -(j >> 3)); }
+// (Made of instructions: a table in memory would cost the first reader of its page
+// some microseconds.)
+__device__ __forceinline__ double root_of(int j) {
   constexpr double kRoot[8] = {1.0,
                                0.91700404320467123174,
                                0.84089641525371454303,
@@ -350,12 +356,13 @@ __device__ __forceinline__ double eighths(int j) {
                                0.54525386633262882702};
   double r = kRoot[0];
 #pragma unroll
-  for (int i = 1; i < 8; ++i) r = (j & 7) == i ? kRoot[i] : r;
-  return ldexp(r, -(j >> 3));
+  for (int i = 1; i < 8; ++i) r = j == i ? kRoot[i] : r;
+  return r;
 }
 
 struct FinishShared {
-  uint64_t list[kList];
+  uint64_t list[kList], wide[kWide];
+  double root[8];
   double tmp[kFinishThreads / 64];
   uint64_t tmpu[kFinishThreads / 64];
   unsigned long long bins[kBins];          // finish_any: a pass's; otherwise the row's
@@ -388,10 +395,13 @@ __device__ __forceinline__ float least_of(const Settings& s, float mx) {
   return (double)x < limit ? float_of_key(float_order_key(x) + 1) : x;
 }
 
-__device__ __forceinline__ void answer(const SampleLaunch& a, int n, int token, double p) {
-  a.tokens[n] = token;
+__device__ __noinline__ void answer(int32_t* token_at, float* logprob_at, int token, double p) {
+  *token_at = token;
   // (close to 1 by what is missing from it)
-  if (a.logprobs) a.logprobs[n] = token < 0 ? -INFINITY : p > 0.5 ? log1pf((float)(p - 1.0)) : logf((float)p);
+  if (logprob_at) *logprob_at = token < 0 ? -INFINITY : p > 0.5 ? log1pf((float)(p - 1.0)) : logf((float)p);
+}
+__device__ __forceinline__ void answer(const SampleLaunch& a, int n, int token, double p) {
+  answer(a.tokens + n, a.logprobs ? a.logprobs + n : nullptr, token, p);
 }
 
 // Threads' candidates in order: the first at which the running sum, `before` plus
@@ -452,7 +462,7 @@ __device__ void draw_slice(const SampleLaunch& a, int n, const T* row, int slice
 // narrows it 256-fold a pass, then the draw over the whole row.  For logits
 // beyond the grid, and where more than kList tokens share the last bin.
 template <typename T>
-__device__ void finish_any(const SampleLaunch& a, int n, const Settings& s, const T* row, float mx, FinishShared& sh) {
+__device__ void finish_any(const SampleLaunch& a, int n, const Settings& s, const T* row, float mx, float least, FinishShared& sh) {
   const int tid = threadIdx.x, V = a.V;
   const float scale = s.scale;
   // Weights in units of 2^-43 of the largest: 2^20 of them fit a word.
@@ -471,7 +481,6 @@ __device__ void finish_any(const SampleLaunch& a, int n, const Settings& s, cons
   block_scan(sum, &total, sh.tmpu);
   block_scan(count, &seen, sh.tmpu);
   uint64_t last = 0;
-  const float least = least_of(s, mx);
   for (int by_weight = 0; by_weight < 2; ++by_weight) {
     uint64_t want;
     if (by_weight) {
@@ -555,7 +564,7 @@ __device__ void finish_any(const SampleLaunch& a, int n, const Settings& s, cons
 // A row from its slices' bins; false where they do not suffice.
 template <typename T, int E>
 __device__ __forceinline__ bool finish_bins(const SampleLaunch& a, int n, int n_slices, const Settings& s, const T* row, const char* in,
-                                            float mx, int top, bool left, FinishShared& sh) {
+                                            float mx, float least, int top, bool left, bool unlisted, FinishShared& sh) {
   constexpr int kSlice = kFinishThreads * 8 * E;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const float u = a.u[n];
@@ -563,9 +572,9 @@ __device__ __forceinline__ bool finish_bins(const SampleLaunch& a, int n, int n_
   const float scale = s.scale;
   auto logit_of = [](uint64_t w) { return float_of_key((uint32_t)(w >> 32)); };
   // A weight relative to the edge of the row's top bin, in units.
-  auto weight = [=](float x) -> double {
+  auto weight = [&](float x) -> double {
     const float b = bin_of(x, scale);
-    return (double)rintf(over_edge(x, scale, b) * kUnit) * eighths(top - (int)b);
+    return (double)rintf(over_edge(x, scale, b) * kUnit) * eighths(sh.root, top - (int)b);
   };
   // Each slice's weight outside its bins, relative to the row's largest.
   auto rest_of = [&](int i) -> double {
@@ -600,7 +609,7 @@ __device__ __forceinline__ bool finish_bins(const SampleLaunch& a, int n, int n_
       }
     }
   }
-  const double here = (double)units * eighths(tid < kBins ? tid : 0);
+  const double here = (double)units * eighths(sh.root, tid < kBins ? tid : 0);
   uint64_t all_c;
   double all_w;
   const uint64_t before_c = block_scan(count, &all_c, sh.tmpu);
@@ -613,7 +622,6 @@ __device__ __forceinline__ bool finish_bins(const SampleLaunch& a, int n, int n_
       sh.before_w[kBins] = all_w;
     }
   }
-  const float least = least_of(s, mx);
   double target = INFINITY;
   if (s.k == 0 && s.p < 1.f) {
     // Of the sum of everything: the bins and the slices' rests.
@@ -639,74 +647,72 @@ __device__ __forceinline__ bool finish_bins(const SampleLaunch& a, int n, int n_
   else if (all_c < (uint64_t)s.k && !left) end = kBins - 1;  // fewer than k tokens: all of them
   if (end >= kBins) return false;  // below the bins
 
-  // Calls f(slice, logit, index) for the tokens in bins from .. to, from the
-  // slices' lists or, of slices that have such tokens and no list, from the logits.
+  // The smallest logit of bin b (counted from the grid's origin) or a higher one:
+  // a few steps around the quotient, a lane each.
+  auto first_of = [&](float b) {
+    const float x = float_of_key(float_order_key(b / (8.f * scale)) - 24 + lane);
+    const uint64_t in = __ballot(bin_of(x, scale) >= b) | 1ull << 63;
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), __builtin_ctzll(in)));
+  };
+  // Calls f(word) for the tokens in bins from .. to, from the slices' lists
+  // or, of slices that have such tokens and no list, from the logits.
   auto visit = [&](int from, int to, auto f) {
     const float first = (float)(top - from), last = (float)(top - to);
-    auto inside = [&](float x) {
-      const float b = bin_of(x, scale);
-      return b <= first && b >= last;
-    };
     for (int i = wave; i < n_slices; i += kFinishThreads / 64) {
       for (int c = lane; c < sh.info[i].n_list; c += 64) {
         const uint64_t w = words_of(i)[kBins + c];
-        if (inside(logit_of(w))) f(i, logit_of(w), ~(uint32_t)w);
+        const float b = bin_of(logit_of(w), scale);
+        if (b <= first && b >= last) f(w);
       }
     }
-    constexpr int kBatch = 8 / (int)sizeof(T);  // runs of 8 in flight per thread
-    const int n_runs = n_slices * E;
-    for (int c0 = 0; c0 < n_runs; c0 += kBatch) {
-      T raw[kBatch][8];
-      uint32_t runs = 0, mask = 0;
-      auto start = [&](int b) { return ((c0 + b) * kFinishThreads + tid) * 8; };
+    if (unlisted) {
+      // The bins' range as one of logits: one conversion and two comparisons each,
+      // which bound this.
+      const float lo = first_of(last), hi = first_of(first + 1.f);
+      auto inside = [&](float x) { return x >= lo && x < hi; };
+      constexpr int kBatch = 8 / (int)sizeof(T);  // runs of 8 in flight per thread
+      const int n_runs = n_slices * E;
+      for (int c0 = 0; c0 < n_runs; c0 += kBatch) {
+        T raw[kBatch][8];
+        uint32_t runs = 0, mask = 0;
+        auto start = [&](int b) { return ((c0 + b) * kFinishThreads + tid) * 8; };
 #pragma unroll
-      for (int b = 0; b < kBatch; ++b) {
-        const int slice = (c0 + b) / E;
-        if (slice < n_slices) {
-          const SliceInfo& g = sh.info[slice];
-          const int off = top - g.top;
-          if (g.max > -INFINITY && g.n_list < 0 && to >= off && from - off < g.n_bins) runs |= 1u << b;
-        }
-        if (runs >> b & 1 && start(b) + 8 <= a.V) __builtin_memcpy(raw[b], row + start(b), sizeof(raw[b]));
-      }
-#pragma unroll
-      for (int b = 0; b < kBatch; ++b)
-        if (runs >> b & 1) {
-          if (start(b) + 8 <= a.V) {
-#pragma unroll
-            for (int c = 0; c < 8; ++c) mask |= inside(clean((float)raw[b][c])) ? 1u << (8 * b + c) : 0u;
-          } else {
-            for (int c = 0; start(b) + c < a.V; ++c) mask |= inside(logit(row, start(b) + c)) ? 1u << (8 * b + c) : 0u;
+        for (int b = 0; b < kBatch; ++b) {
+          const int slice = (c0 + b) / E;
+          if (slice < n_slices) {
+            const SliceInfo& g = sh.info[slice];
+            const int off = top - g.top;
+            if (g.max > -INFINITY && g.n_list < 0 && to >= off && from - off < g.n_bins) runs |= 1u << b;
           }
+          if (runs >> b & 1 && start(b) + 8 <= a.V) __builtin_memcpy(raw[b], row + start(b), sizeof(raw[b]));
         }
-      for (; mask; mask &= mask - 1) {  // few
-        const int c = __builtin_ctz(mask), b = c / 8, i = start(b) + c % 8;
-        f((c0 + b) / E, logit(row, i), (uint32_t)i);
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b)
+          if (runs >> b & 1) {
+            if (start(b) + 8 <= a.V) {
+              bool any = false;
+#pragma unroll
+              for (int c = 0; c < 8; ++c) any |= inside((float)raw[b][c]);
+              if (__any(any)) {
+#pragma unroll
+                for (int c = 0; c < 8; ++c) mask |= inside((float)raw[b][c]) ? 1u << (8 * b + c) : 0u;
+              }
+            } else {
+              for (int c = 0; start(b) + c < a.V; ++c) mask |= inside(logit(row, start(b) + c)) ? 1u << (8 * b + c) : 0u;
+            }
+          }
+        for (; mask; mask &= mask - 1) {  // few
+          const int c = __builtin_ctz(mask), i = start(c / 8) + c % 8;
+          f(word_of(logit(row, i), (uint32_t)i));
+        }
       }
     }
     __syncthreads();
   };
-  // The tokens of bins from .. to with words in [lo, hi], at most kList: one
-  // word per thread in falling order (0 past their number).
-  auto collect = [&](int from, int to, uint64_t lo, uint64_t hi) -> uint64_t {
-    if (tid == 0) sh.pick[2] = 0;
-    if (tid < kMaxSlices) sh.extra[tid] = 0;
-    __syncthreads();
-    visit(from, to, [&](int slice, float x, uint32_t i) {
-      const uint64_t w = word_of(x, i);
-      if (w > hi) {
-        atomicAdd(&sh.extra[slice], (unsigned long long)rintf(over_edge(x, scale, bin_of(x, scale)) * kUnit));
-      } else if (w >= lo) {
-        const int at = atomicAdd(&sh.pick[2], 1);
-        if (at < kList) sh.list[at] = w;
-      }
-    });
-    const int m = min(sh.pick[2], kList);
-    int size = 64;
-    while (size < m) size *= 2;
-    const uint64_t w = tid < m ? sh.list[tid] : 0;
-    __syncthreads();
-    return sort_falling(w, size, sh.list);
+  auto slice_index = [](uint64_t word) { return (int)(~(uint32_t)word / kSlice); };
+  auto units_of = [=](uint64_t word) {
+    const float x = logit_of(word);
+    return (uint32_t)rintf(over_edge(x, scale, bin_of(x, scale)) * kUnit);
   };
 
   // All kept tokens, if few, or those at the end of the last bin, above which
@@ -725,61 +731,109 @@ __device__ __forceinline__ bool finish_bins(const SampleLaunch& a, int n, int n_
       __syncthreads();
       end = min(end, min(sh.pick[0], sh.pick[1]));
     }
+    const int first = whole ? 0 : end;
+    above = sh.before_c[first];
+    above_w = sh.before_w[first];
+    uint64_t n_here = sh.before_c[end + 1] - above;
+    // Too many for the list: the part of the bin in which the kept tokens end, by
+    // the bins' way of search over the words, 256 parts a pass, on the logits
+    // until the bin's tokens fit the work-group's memory.
+    bool held = false;
+    int n_held = 0;
+    // (the bin's edges, wider by what their rounding may be)
+    const float b = (float)(top - end);
+    uint64_t lo = (uint64_t)(float_order_key(b == 0.f ? -0x1p-60f : b / (8.f * scale)) - 16) << 32;
+    uint64_t hi = (uint64_t)(float_order_key((b + 1.f) / (8.f * scale)) + 16) << 32;
     uint64_t w_lo = 0, w_hi = ~(uint64_t)0;
-    if (!whole) {
-      const int e = end, k = s.k;
-      above = sh.before_c[e];
-      above_w = sh.before_w[e];
-      uint64_t n_here = sh.before_c[e + 1] - above;
-      // Too many: the part of the bin in which the kept tokens end, by the bins'
-      // way of search over the words, 256 parts a pass.
-      const float b = (float)(top - e);
-      // (the bin's edges, wider by what their rounding may be)
-      uint64_t lo = (uint64_t)(float_order_key(b == 0.f ? -0x1p-60f : b / (8.f * scale)) - 16) << 32;
-      uint64_t hi = (uint64_t)(float_order_key((b + 1.f) / (8.f * scale)) + 16) << 32;
-      for (int pass = 0; pass < 8 && n_here > kList; ++pass) {
-        const int shift = max(0, 64 - 8 - __builtin_clzll((hi - lo) | 255));
-        auto part_of = [&](uint64_t x) { return x < lo ? 0 : x > hi ? kBins - 1 : min(kBins - 1, (int)((x - lo) >> shift)); };
-        __syncthreads();
-        if (tid < kBins) sh.bins[tid] = 0;
-        if (tid == 0) sh.pick[0] = kBins - 1;
-        __syncthreads();
-        visit(e, e, [&](int, float x, uint32_t i) {
-          const uint64_t word = word_of(x, i);
-          if (word >= w_lo && word <= w_hi)
-            atomicAdd(&sh.bins[part_of(word)], (1ull << kCountShift) + (uint32_t)rintf(over_edge(x, scale, b) * kUnit));
-        });
-        const uint64_t mine = tid < kBins ? sh.bins[kBins - 1 - tid] : 0;  // from the top
-        uint64_t all;
-        const uint64_t before = block_scan(mine, &all, sh.tmpu);
-        auto c_of = [&](uint64_t x) { return above + (x >> kCountShift); };
-        auto w_of = [&](uint64_t x) { return above_w + (double)(x & kUnitMask) * eighths(e); };
-        if (tid < kBins) {
-          const bool by_k = k > 0 && c_of(before) < (uint64_t)k && c_of(before + mine) >= (uint64_t)k;
-          const bool by_p = !sum_k && w_of(before) < target && w_of(before + mine) >= target;
-          const bool by_m = !sum_k && s.m > 0.f && sh.pick[1] == e && tid == kBins - 1 - part_of((uint64_t)float_order_key(least) << 32);
-          if (by_k || by_p || by_m) atomicMin(&sh.pick[0], tid);
-        }
-        __syncthreads();
-        const int at = sh.pick[0];
-        if (tid == at) {
-          sh.picku = before;
-          sh.pickd = (double)(mine >> kCountShift);
-        }
-        __syncthreads();
-        above = c_of(sh.picku);
-        above_w = w_of(sh.picku);
-        n_here = (uint64_t)sh.pickd;
-        const int part = kBins - 1 - at;
-        const uint64_t p_lo = lo + ((uint64_t)part << shift), p_hi = p_lo + (((uint64_t)1 << shift) - 1);
-        if (part > 0) w_lo = max(w_lo, p_lo);
-        if (part < kBins - 1) w_hi = p_hi < w_hi ? p_hi : w_hi;
-        lo = max(w_lo, lo);
-        hi = w_hi < hi ? w_hi : hi;
+    __syncthreads();
+    if (tid < kMaxSlices) sh.extra[tid] = 0;
+    for (int pass = 0; pass < 10; ++pass) {
+      const bool fits = n_here <= kWide;
+      if (held && n_here <= kList) break;
+      const int shift = max(0, 64 - 8 - __builtin_clzll((hi - lo) | 255));
+      auto part_of = [&](uint64_t x) { return x < lo ? 0 : x > hi ? kBins - 1 : min(kBins - 1, (int)((x - lo) >> shift)); };
+      auto count_in = [&](uint64_t word) {
+        if (word >= w_lo && word <= w_hi) atomicAdd(&sh.bins[part_of(word)], (1ull << kCountShift) + units_of(word));
+      };
+      __syncthreads();
+      if (tid < kBins) sh.bins[tid] = 0;
+      if (tid == 0) {
+        sh.pick[0] = kBins - 1;
+        sh.pick[2] = 0;
       }
-      if (n_here > kList) return false;
+      __syncthreads();
+      if (held) {
+        for (int i = tid; i < n_held; i += kFinishThreads) count_in(sh.wide[i]);
+        __syncthreads();
+      } else {
+        visit(first, end, [&](uint64_t word) {
+          if (!fits) {
+            count_in(word);
+          } else if (word > w_hi) {
+            atomicAdd(&sh.extra[slice_index(word)], (unsigned long long)units_of(word));
+          } else if (word >= w_lo) {
+            const int at = atomicAdd(&sh.pick[2], 1);
+            if (at < kWide) sh.wide[at] = word;
+          }
+        });
+        if (fits) {
+          n_held = min(sh.pick[2], kWide);
+          held = true;
+          continue;
+        }
+      }
+      const uint64_t mine = tid < kBins ? sh.bins[kBins - 1 - tid] : 0;  // from the top
+      uint64_t all;
+      const uint64_t before = block_scan(mine, &all, sh.tmpu);
+      auto c_of = [&](uint64_t x) { return above + (x >> kCountShift); };
+      auto w_of = [&](uint64_t x) { return above_w + (double)(x & kUnitMask) * eighths(sh.root, end); };
+      if (tid < kBins) {
+        const bool by_k = s.k > 0 && c_of(before) < (uint64_t)s.k && c_of(before + mine) >= (uint64_t)s.k;
+        const bool by_p = !sum_k && w_of(before) < target && w_of(before + mine) >= target;
+        const bool by_m = !sum_k && s.m > 0.f && sh.pick[1] == end && tid == kBins - 1 - part_of((uint64_t)float_order_key(least) << 32);
+        if (by_k || by_p || by_m) atomicMin(&sh.pick[0], tid);
+      }
+      __syncthreads();
+      const int at = sh.pick[0];
+      if (tid == at) {
+        sh.picku = before;
+        sh.pickd = (double)(mine >> kCountShift);
+      }
+      __syncthreads();
+      above = c_of(sh.picku);
+      above_w = w_of(sh.picku);
+      n_here = (uint64_t)sh.pickd;
+      const int part = kBins - 1 - at;
+      const uint64_t p_lo = lo + ((uint64_t)part << shift), p_hi = p_lo + (((uint64_t)1 << shift) - 1);
+      if (part > 0) w_lo = max(w_lo, p_lo);
+      if (part < kBins - 1) w_hi = p_hi < w_hi ? p_hi : w_hi;
+      lo = max(w_lo, lo);
+      hi = w_hi < hi ? w_hi : hi;
     }
-    v = collect(whole ? 0 : end, end, w_lo, w_hi);
+    if (!held || n_here > kList) return false;
+    // Those of the range, one per thread in falling order (0 past their number).
+    int m = n_held;
+    if (n_held > kList) {
+      __syncthreads();
+      if (tid == 0) sh.pick[2] = 0;
+      __syncthreads();
+      for (int i = tid; i < n_held; i += kFinishThreads) {
+        const uint64_t word = sh.wide[i];
+        if (word > w_hi) {
+          atomicAdd(&sh.extra[slice_index(word)], (unsigned long long)units_of(word));
+        } else if (word >= w_lo) {
+          const int at = atomicAdd(&sh.pick[2], 1);
+          if (at < kList) sh.list[at] = word;
+        }
+      }
+      __syncthreads();
+      m = min(sh.pick[2], kList);
+    }
+    v = tid < m ? (n_held > kList ? sh.list : sh.wide)[tid] : 0;
+    int size = 64;
+    while (size < m) size *= 2;
+    __syncthreads();
+    v = sort_falling(v, size, sh.list);
     w = v ? weight(logit_of(v)) : 0.0;
     if (!sum_k) break;
     block_scan(above + tid < (uint64_t)s.k ? w : 0.0, &sum, sh.tmp);
@@ -818,10 +872,10 @@ __device__ __forceinline__ bool finish_bins(const SampleLaunch& a, int n, int n_
     double part = 0.0;
     if (f.max > -INFINITY) {
       for (int j = lane; j < end; j += 64)
-        if (j - off >= 0 && j - off < f.n_bins) part += (double)(words_of(i)[j - off] & kUnitMask) * eighths(j);
-      if (lane == 0) part += (double)sh.extra[i] * eighths(end);
+        if (j - off >= 0 && j - off < f.n_bins) part += (double)(words_of(i)[j - off] & kUnitMask) * eighths(sh.root, j);
+      if (lane == 0) part += (double)sh.extra[i] * eighths(sh.root, end);
       for (int j = lane; j < n_kept; j += 64)
-        if ((int)(~(uint32_t)sh.list[j] / kSlice) == i) part += weight(logit_of(sh.list[j]));
+        if (slice_index(sh.list[j]) == i) part += weight(logit_of(sh.list[j]));
     }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) part += __shfl_xor(part, d);
@@ -846,14 +900,16 @@ __global__ __launch_bounds__(kFinishThreads) void sample_finish_kernel(SampleLau
   const char* in = static_cast<const char*>(a.ws) + (int64_t)n * n_slices * kSliceBytes;
   if (tid < n_slices) sh.info[tid] = *reinterpret_cast<const SliceInfo*>(in + tid * kSliceBytes);
   if (tid < 4) sh.pick[tid] = kBins;
+  if (tid < 8) sh.root[tid] = root_of(tid);
   __syncthreads();
   float mx = -INFINITY;
   int top = -0x7FFFFFFF;
-  bool beyond = false, left = false;
+  bool beyond = false, left = false, unlisted = false;
   for (int i = 0; i < n_slices; ++i) {
     const SliceInfo& f = sh.info[i];
     mx = fmaxf(mx, f.max);
     left = left || f.left;
+    unlisted = unlisted || f.n_list < 0;
     beyond = beyond || f.n_bins < 0;
     if (f.n_bins >= 0 && f.max > -INFINITY) top = max(top, f.top);
   }
@@ -861,8 +917,9 @@ __global__ __launch_bounds__(kFinishThreads) void sample_finish_kernel(SampleLau
     if (tid == 0) answer(a, n, -1, 0.0);
     return;
   }
-  if (!beyond && finish_bins<T, E>(a, n, n_slices, s, row, in, mx, top, left, sh)) return;
-  finish_any(a, n, s, row, mx, sh);
+  const float least = least_of(s, mx);
+  if (!beyond && finish_bins<T, E>(a, n, n_slices, s, row, in, mx, least, top, left, unlisted, sh)) return;
+  finish_any(a, n, s, row, mx, least, sh);
 }
 
 }  // namespace
