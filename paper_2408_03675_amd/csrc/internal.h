@@ -252,8 +252,10 @@ struct PrefixLaunch {
   int B, H, G, T, L, row0;
   int Lp, per_group;             // rows per head of the prefix (0: none), sequences per group
   int prefix_rows, own_rows;     // rows per work-group: 16, 32 or (bf16) kPrefixTileRows
-  int prefix_blocks, prefix_split, prefix_items;  // row blocks per (group, head), most chunks, work-groups
-  int own_blocks, own_split, own_items;           // the same per (sequence, head)
+  // Row blocks and most chunks per (group, head), chunks in all, work-groups per
+  // XCD; the same per (sequence, head).
+  int prefix_blocks, prefix_split, prefix_units, prefix_slots;
+  int own_blocks, own_split, own_units, own_slots;
   int direct;                    // one chunk in all: no partials
   float c2;                      // logit scale times log2(e)
   int64_t qs[3], ks[3], vs[3], pks[3], pvs[3];  // element strides

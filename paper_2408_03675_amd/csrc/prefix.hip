@@ -255,16 +255,13 @@ struct Item {
   int split, key_lo, key_hi;
   __device__ __forceinline__ bool nothing(const PrefixLaunch& a) const { return key_lo >= key_hi && !(a.direct && split == 0); }
 };
-__device__ __forceinline__ Item item_of(const PrefixLaunch& a, bool prefix, int i, int rows) {
+__device__ __forceinline__ Item item_of(const PrefixLaunch& a, bool prefix, int i, int block, int rows) {
   Item it;
   it.prefix = prefix;
   const int n_split = prefix ? a.prefix_split : a.own_split;
-  const int n_blocks = prefix ? a.prefix_blocks : a.own_blocks;
   const int n_rows = prefix ? a.per_group * a.G * a.T : a.G * a.T;
   it.split = i % n_split;
   i /= n_split;
-  const int block = i % n_blocks;
-  i /= n_blocks;
   it.h = i % a.H;
   it.owner = i / a.H;
   it.row0 = block * rows;
@@ -533,6 +530,11 @@ __device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& i
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
+// The exponentials' reference follows a row's maximum once it is passed by this
+// much (a factor of 2^kSlack in the probabilities, whose bf16 rounding is relative
+// either way).
+constexpr float kSlack = 8.f;
+
 template <int D>
 struct TileShared {
   unsigned char k[2][kTileKeys * D * 2], v[2][kTileKeys * D * 2];
@@ -629,8 +631,8 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
     load(key_lo);
     store(0);
   }
-  int buf = 0;
-  for (int key0 = key_lo; key0 < key_hi; key0 += kTileKeys, buf ^= 1) {
+  auto tile = [&](auto buf_c, int key0) {
+    constexpr int buf = decltype(buf_c)::value;
     __syncthreads();
     const int next = key0 + kTileKeys;
     if (next < key_hi) load(next);
@@ -645,8 +647,8 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
         for (int c = 0; c < kC; ++c) t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kfrag(buf, kt, c), qf[c], t, 0, 0, 0);
         s[kt] = t;
       }
-      const bool masked = !plain || next > key_hi;
-      if (masked) {
+      if (!plain || next > key_hi) {
+        asm volatile("");  // a branch: the comparisons cost as much as the exponentials' FMAs
         const int lim = limit - key0 - 4 * hl;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
@@ -660,11 +662,18 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
 #pragma unroll
         for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[kt][i]);
       auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-      mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-      const float mn = fmaxf(m, mx * a.c2);
-      const float ref = mn == -INFINITY ? 0.f : mn;
-      const float alpha = __builtin_amdgcn_exp2f(m - ref);
-      m = mn;
+      mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * a.c2;
+      if (__any(mx > m + kSlack)) {
+        const float mn = fmaxf(m, mx);
+        const float alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        l *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[dt][i] *= alpha;
+      }
+      const float ref = m == -INFINITY ? 0.f : m;
       float sum[2] = {0.f, 0.f};
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
@@ -673,13 +682,7 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
           s[kt][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i], a.c2, -ref));
           sum[i & 1] += s[kt][i];
         }
-      l = l * alpha + (sum[0] + sum[1]);
-      if (__ballot(alpha != 1.f)) {
-#pragma unroll
-        for (int dt = 0; dt < kDt; ++dt)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[dt][i] *= alpha;
-      }
+      l += sum[0] + sum[1];
       bf16x8 pf[4];
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks)
@@ -692,6 +695,10 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
           acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vfrag(buf, ks, dt), pf[ks], acc[dt], 0, 0, 0);
     }
     if (next < key_hi) store(buf ^ 1);
+  };
+  for (int key0 = key_lo; key0 < key_hi; key0 += 2 * kTileKeys) {
+    tile(std::integral_constant<int, 0>{}, key0);
+    if (key0 + kTileKeys < key_hi) tile(std::integral_constant<int, 1>{}, key0 + kTileKeys);
   }
 
   if (causal && __syncthreads_or(odd)) {
@@ -736,9 +743,19 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixLaunch a) {
   };
   __shared__ __attribute__((aligned(16))) unsigned char smem[sizeof(Shared)];
   Shared& sh = *reinterpret_cast<Shared*>(smem);
-  const int i = blockIdx.x;
-  const bool prefix = i < a.prefix_items;
-  const Item it = item_of(a, prefix, prefix ? i : i - a.prefix_items, prefix ? PREFIX : OWN);
+  // Work-groups are dealt to the 8 XCDs in turn.  The row blocks that read the
+  // same chunk of K and V follow each other on one XCD, whose L2 they share; the
+  // prefix's chunks come first.  (Beside the own caches', which wait for memory,
+  // they take longer than both in turn: 512 rows of 8 heads to 26214 keys and 64
+  // caches of 576 rows 119 us, alternating 142, a half of them first 129.)
+  const int xcd = blockIdx.x & 7;
+  int slot = blockIdx.x >> 3;
+  const bool prefix = slot < a.prefix_slots;
+  if (!prefix) slot -= a.prefix_slots;
+  const int blocks = prefix ? a.prefix_blocks : a.own_blocks;
+  const int unit = (slot / blocks) * 8 + xcd;
+  if (unit >= (prefix ? a.prefix_units : a.own_units)) return;
+  const Item it = item_of(a, prefix, unit, slot % blocks, prefix ? PREFIX : OWN);
   if (it.nothing(a)) return;
   if constexpr (PREFIX == OWN) {
     O::run(a, it, sh.o);
@@ -748,14 +765,16 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixLaunch a) {
   }
 }
 
-// A row's chunks joined: one work-group per row, D / 4 threads per chunk.
+// A row's chunks joined, a wave per row: D / 4 lanes take a chunk's output, the
+// others the next chunks', and all loads of up to kBatch chunks a lane are under
+// way together.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void prefix_merge_kernel(PrefixLaunch a) {
-  constexpr int kPer = D / 4, kSlots = kThreads / kPer, kUnroll = 4;
-  __shared__ float so[kSlots][D], sl[kSlots], smax[kWaves];
-  const int tid = threadIdx.x, d0 = (tid % kPer) * 4, mine = tid / kPer;
-  const int64_t row = blockIdx.x;
+  constexpr int kPer = D / 4, kSlots = 64 / kPer, kBatch = 8;
+  const int lane = threadIdx.x & 63, d0 = (lane % kPer) * 4, mine = lane / kPer;
+  const int64_t row = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
   const int Hq = a.H * a.G;
+  if (row >= (int64_t)a.B * Hq * a.T) return;
   const int t = (int)(row % a.T);
   const int64_t bh = row / a.T;
   const int b = (int)(bh / Hq), e = (int)(bh % Hq) % a.G;
@@ -773,14 +792,13 @@ __global__ __launch_bounds__(kThreads) void prefix_merge_kernel(PrefixLaunch a) 
   const int64_t base = row * (a.prefix_split + a.own_split);
   const int total = np + no;
   auto slot = [&](int i) { return base + (i < np ? i : a.prefix_split + i - np); };
-  float m = -INFINITY;
-  for (int i = tid; i < total; i += kThreads) m = fmaxf(m, a.part_ml[slot(i)].x);
-  // The first chunks' outputs are on their way while the maximum is found.
-  f32x4 w[kUnroll];
-  float2 ml[kUnroll];
-  auto load = [&](int i0) {
+  f32x4 w[kBatch], o = {0.f, 0.f, 0.f, 0.f};
+  float2 ml[kBatch];
+  float m = -INFINITY, l = 0.f;
+  for (int i0 = 0; i0 < total; i0 += kBatch * kSlots) {
+    float mx = m;
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
+    for (int u = 0; u < kBatch; ++u) {
       const int i = i0 + u * kSlots + mine;
       ml[u] = float2{-INFINITY, 0.f};
       w[u] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -788,44 +806,41 @@ __global__ __launch_bounds__(kThreads) void prefix_merge_kernel(PrefixLaunch a) 
         ml[u] = a.part_ml[slot(i)];
         w[u] = *reinterpret_cast<const f32x4*>(a.part_o + slot(i) * D + d0);
       }
+      mx = fmaxf(mx, ml[u].x);
     }
-  };
-  load(0);
+    const float ref = mx == -INFINITY ? 0.f : mx;  // of the lane's chunks
+    const float alpha = __builtin_amdgcn_exp2f(m - ref);
+    l *= alpha;
+    o *= alpha;
+    m = mx;
 #pragma unroll
-  for (int x = 1; x < 64; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
-  if ((tid & 63) == 0) smax[tid >> 6] = m;
-  __syncthreads();
-#pragma unroll
-  for (int x = 0; x < kWaves; ++x) m = fmaxf(m, smax[x]);
-  const float ref = m == -INFINITY ? 0.f : m;
-  float l = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int i0 = 0; i0 < total; i0 += kUnroll * kSlots) {
-    if (i0) load(i0);
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
+    for (int u = 0; u < kBatch; ++u) {
       const float c = __builtin_amdgcn_exp2f(ml[u].x - ref);
       l += c * ml[u].y;
       o += c * w[u];
     }
   }
-  *reinterpret_cast<f32x4*>(&so[mine][d0]) = o;
-  if (d0 == 0) sl[mine] = l;
-  __syncthreads();
-  if (tid >= D) return;
-  float lt = 0.f, x = 0.f;
+  // The lanes of the same entries.
 #pragma unroll
-  for (int i = 0; i < kSlots; ++i) {
-    lt += sl[i];
-    x += so[i][tid];
+  for (int x = kPer; x < 64; x *= 2) {
+    const float m2 = __shfl_xor(m, x), l2 = __shfl_xor(l, x), mx = fmaxf(m, m2), ref = mx == -INFINITY ? 0.f : mx;
+    const float c = __builtin_amdgcn_exp2f(m - ref), c2 = __builtin_amdgcn_exp2f(m2 - ref);
+    l = c * l + c2 * l2;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = c * o[i] + c2 * __shfl_xor(o[i], x);
+    m = mx;
   }
-  reinterpret_cast<T*>(a.out)[row * D + tid] = (T)(lt == 0.f ? 0.f : x / lt);
-  if (a.lse && tid == 0) a.lse[row] = lt == 0.f ? -INFINITY : (m + log2f(lt)) * 0.69314718055994531f;
+  if (mine) return;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  T* dst = reinterpret_cast<T*>(a.out) + row * D + d0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) dst[i] = (T)(o[i] * inv);
+  if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }
 
 template <typename T, int D>
 hipError_t launch_t(const PrefixLaunch& a, hipStream_t stream) {
-  const dim3 grid((unsigned)(a.prefix_items + a.own_items));
+  const dim3 grid(8u * (unsigned)(a.prefix_slots + a.own_slots));
   auto run = [&](auto kernel) { kernel<<<grid, kThreads, 0, stream>>>(a); };
   const int own = a.own_rows, prefix = std::max(a.prefix_rows, own);
   if constexpr (std::is_same_v<T, __bf16>) {
@@ -839,7 +854,7 @@ hipError_t launch_t(const PrefixLaunch& a, hipStream_t stream) {
     else run(prefix_kernel<T, D, 16, 16>);
   }
   if (hipError_t e = hipGetLastError()) return e;
-  if (!a.direct) prefix_merge_kernel<T, D><<<(unsigned)((int64_t)a.B * a.H * a.G * a.T), kThreads, 0, stream>>>(a);
+  if (!a.direct) prefix_merge_kernel<T, D><<<(unsigned)(((int64_t)a.B * a.H * a.G * a.T + kWaves - 1) / kWaves), kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 

@@ -74,7 +74,7 @@ struct Plan {
   int per_group = 1, Lp = 0;
   int prefix_rows = 16, own_rows = 16;
   int prefix_blocks = 0, prefix_split = 0, own_blocks = 0, own_split = 0;
-  int64_t prefix_items = 0, own_items = 0, rows = 0;
+  int64_t prefix_units = 0, prefix_slots = 0, own_units = 0, own_slots = 0, rows = 0;
   bool direct = false;
   size_t ml = 0, total = 0;  // byte offset of part_ml, workspace bytes
 };
@@ -95,16 +95,18 @@ Plan plan_of(const nacl_problem* p, const nacl_step* s, const nacl_prefix* x) {
   auto up = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
   a.own_blocks = (int)up(own_rows, a.own_rows);
   a.prefix_blocks = x ? (int)up(prefix_rows, a.prefix_rows) : 0;
-  const int64_t own_units = (int64_t)p->B * p->H * a.own_blocks, prefix_units = (int64_t)groups * p->H * a.prefix_blocks;
+  const int64_t own_blocks = (int64_t)p->B * p->H * a.own_blocks, prefix_blocks = (int64_t)groups * p->H * a.prefix_blocks;
   // Chunks of about the same number of keys in both, four work-groups per CU in
   // all; a prefix read by tiles in chunks that fill the chip twice over.
   const bool tiles = x && a.prefix_rows == nacl::kPrefixTileRows;
-  const int64_t keys = own_units * p->L + (tiles ? 0 : prefix_units * a.Lp);
+  const int64_t keys = own_blocks * p->L + (tiles ? 0 : prefix_blocks * a.Lp);
   const int64_t chunk = std::max<int64_t>(nacl::kPrefixMinChunk, up(keys, 4 * kPlanCus));
   a.own_split = (int)up(p->L, chunk);
-  a.prefix_split = (int)up(a.Lp, tiles ? std::max<int64_t>(256, up(prefix_units * a.Lp, 2 * kPlanCus)) : chunk);
-  a.own_items = own_units * a.own_split;
-  a.prefix_items = prefix_units * a.prefix_split;
+  a.prefix_split = (int)up(a.Lp, tiles ? std::max<int64_t>(256, up(prefix_blocks * a.Lp, 2 * kPlanCus)) : chunk);
+  a.own_units = (int64_t)p->B * p->H * a.own_split;
+  a.prefix_units = x ? (int64_t)groups * p->H * a.prefix_split : 0;
+  a.own_slots = up(a.own_units, 8) * a.own_blocks;
+  a.prefix_slots = up(a.prefix_units, 8) * a.prefix_blocks;
   a.direct = !x && a.own_split == 1;
   const size_t slots = a.direct ? 0 : (size_t)a.rows * (a.own_split + a.prefix_split);
   a.ml = align_up(slots * p->D * sizeof(float));
@@ -114,8 +116,8 @@ Plan plan_of(const nacl_problem* p, const nacl_step* s, const nacl_prefix* x) {
 
 int check_planned(const Plan& a) {
   if (a.rows >= (int64_t)1 << 26) return fail_status(NACL_ERR_UNSUPPORTED, "B * H * q_group * T reaches 2^26");
-  if (a.own_items + a.prefix_items >= (int64_t)1 << 24)
-    return fail_status(NACL_ERR_UNSUPPORTED, "%lld work-groups, at most 2^24", (long long)(a.own_items + a.prefix_items));
+  if (8 * (a.own_slots + a.prefix_slots) >= (int64_t)1 << 24)
+    return fail_status(NACL_ERR_UNSUPPORTED, "%lld work-groups, at most 2^24", (long long)(8 * (a.own_slots + a.prefix_slots)));
   return NACL_OK;
 }
 
@@ -290,10 +292,12 @@ int nacl_prefix_attention(const nacl_problem* p, const nacl_step* s, const nacl_
   a.own_rows = plan.own_rows;
   a.prefix_blocks = plan.prefix_blocks;
   a.prefix_split = plan.prefix_split;
-  a.prefix_items = (int)plan.prefix_items;
+  a.prefix_units = (int)plan.prefix_units;
+  a.prefix_slots = (int)plan.prefix_slots;
   a.own_blocks = plan.own_blocks;
   a.own_split = plan.own_split;
-  a.own_items = (int)plan.own_items;
+  a.own_units = (int)plan.own_units;
+  a.own_slots = (int)plan.own_slots;
   a.direct = plan.direct ? 1 : 0;
   a.c2 = (float)((double)p->sm_scale * 1.4426950408889634);
   for (int i = 0; i < 3; ++i) {
