@@ -248,10 +248,11 @@ hipError_t launch_rotate_append(RotateLaunch a, int dtype, int D, int cus, hipSt
 // Attention of a step's queries to the cache and a shared prefix (prefix.hip).
 constexpr int kPrefixMinChunk = 128;  // keys per chunk at least
 constexpr int kPrefixTileRows = 128;
+constexpr int kPrefixWideRows = 256;
 struct PrefixLaunch {
   int B, H, G, T, L, row0;
   int Lp, per_group;             // rows per head of the prefix (0: none), sequences per group
-  int prefix_rows, own_rows;     // rows per work-group: 16, 32 or (bf16) kPrefixTileRows
+  int prefix_rows, own_rows;     // rows per work-group: 16, 32, (bf16) kPrefixTileRows, (the prefix's) kPrefixWideRows
   // Row blocks and most chunks per (group, head), chunks in all, work-groups per
   // XCD; the same per (sequence, head).
   int prefix_blocks, prefix_split, prefix_units, prefix_slots;

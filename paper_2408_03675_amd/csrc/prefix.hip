@@ -22,7 +22,8 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
-constexpr int kTileRows = kPrefixTileRows, kTileKeys = 64;
+constexpr int kTileRows = kPrefixTileRows, kWideRows = kPrefixWideRows, kTileKeys = 64;
+constexpr int kMergeBatch = 8;
 constexpr int kRsrcWord3 = 0x00020000;
 
 __device__ __forceinline__ float group_max(float x) {
@@ -332,7 +333,7 @@ __device__ __forceinline__ void odd_item(const PrefixLaunch& a, const Item& it) 
   const int64_t* vs = it.prefix ? a.pvs : a.vs;
   const T* kh = reinterpret_cast<const T*>(it.prefix ? a.pk : a.k) + (int64_t)it.owner * ks[0] + (int64_t)it.h * ks[1];
   const T* vh = reinterpret_cast<const T*>(it.prefix ? a.pv : a.v) + (int64_t)it.owner * vs[0] + (int64_t)it.h * vs[1];
-  for (int row = it.row0 + (threadIdx.x >> 6); row < it.row1; row += kWaves) {
+  for (int row = it.row0 + (threadIdx.x >> 6); row < it.row1; row += blockDim.x >> 6) {
     const RowAt x = row_at(a, it.prefix, it.owner, it.h, row);
     const T* q = query_of<T>(a, x);
     const int end = min(x.limit, it.key_hi);
@@ -520,7 +521,7 @@ __device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& i
 }
 
 // ---------------------------------------------------------------------------
-// Many rows (bf16): 32 per wave, 128 per work-group, whose waves share tiles of
+// Many rows (bf16): 32 per wave, 128 or 256 per work-group, whose waves share tiles of
 // 64 keys in LDS (two of each of K and V, one barrier per tile; the next tile's
 // rows wait in registers while the one in hand is used).  v_mfma_f32_32x32x16_bf16
 // with the roles as above: lane (hl, n) = (lane / 32, lane mod 32) holds logits of
@@ -534,16 +535,18 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 // much (a factor of 2^kSlack in the probabilities, whose bf16 rounding is relative
 // either way).
 constexpr float kSlack = 8.f;
+constexpr int kAhead = 2;
 
 template <int D>
 struct TileShared {
   unsigned char k[2][kTileKeys * D * 2], v[2][kTileKeys * D * 2];
 };
 
-template <int D>
+template <int D, int ROWS>
 __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it, TileShared<D>& sh) {
   constexpr int kRowBytes = D * 2, kChunks = kRowBytes / 16, kSwz = kChunks - 1;
   constexpr int kC = D / 16, kDt = D / 32;
+  constexpr int kThreads = 2 * ROWS;
   constexpr int kUnits = kTileKeys * kChunks / kThreads;  // 16-byte pieces of a tile per thread
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int hl = lane >> 5, n = lane & 31;
@@ -639,13 +642,24 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
     if (!idle) {
       f32x16 s[2];
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt) {
-        f32x16 t;
+      for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) t[i] = 0.f;
+        for (int i = 0; i < 16; ++i) s[kt][i] = 0.f;
+      // K's fragments are read kAhead steps (of two MFMAs) before their use, and
+      // fenced there: left alone, each pair is read right before it.
+      bf16x8 kf[kAhead + 1][2];
 #pragma unroll
-        for (int c = 0; c < kC; ++c) t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kfrag(buf, kt, c), qf[c], t, 0, 0, 0);
-        s[kt] = t;
+      for (int c = 0; c < kC + kAhead; ++c) {
+        if (c < kC) {
+#pragma unroll
+          for (int kt = 0; kt < 2; ++kt) kf[c % (kAhead + 1)][kt] = kfrag(buf, kt, c);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (c >= kAhead) {
+#pragma unroll
+          for (int kt = 0; kt < 2; ++kt)
+            s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[(c - kAhead) % (kAhead + 1)][kt], qf[c - kAhead], s[kt], 0, 0, 0);
+        }
       }
       if (!plain || next > key_hi) {
         asm volatile("");  // a branch: the comparisons cost as much as the exponentials' FMAs
@@ -730,13 +744,20 @@ struct Part {
 template <int D>
 struct Part<__bf16, D, kTileRows> {
   using Shared = TileShared<D>;
-  static __device__ __forceinline__ void run(const PrefixLaunch& a, const Item& it, Shared& sh) { tile_item<D>(a, it, sh); }
+  static __device__ __forceinline__ void run(const PrefixLaunch& a, const Item& it, Shared& sh) { tile_item<D, kTileRows>(a, it, sh); }
 };
+template <int D>
+struct Part<__bf16, D, kWideRows> {
+  using Shared = TileShared<D>;
+  static __device__ __forceinline__ void run(const PrefixLaunch& a, const Item& it, Shared& sh) { tile_item<D, kWideRows>(a, it, sh); }
+};
+constexpr int threads_of(int rows) { return rows >= kTileRows ? 2 * rows : kThreads; }
 
+// (0: none of them in this launch, so that the code of the other alone is there.)
 template <typename T, int D, int PREFIX, int OWN>
-__global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixLaunch a) {
-  using P = Part<T, D, PREFIX>;
-  using O = Part<T, D, OWN>;
+__global__ __launch_bounds__(threads_of(PREFIX > OWN ? PREFIX : OWN), 2) void prefix_kernel(PrefixLaunch a) {
+  using P = Part<T, D, PREFIX ? PREFIX : OWN>;
+  using O = Part<T, D, OWN ? OWN : PREFIX>;
   union Shared {
     typename P::Shared p;
     typename O::Shared o;
@@ -745,19 +766,17 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixLaunch a) {
   Shared& sh = *reinterpret_cast<Shared*>(smem);
   // Work-groups are dealt to the 8 XCDs in turn.  The row blocks that read the
   // same chunk of K and V follow each other on one XCD, whose L2 they share; the
-  // prefix's chunks come first.  (Beside the own caches', which wait for memory,
-  // they take longer than both in turn: 512 rows of 8 heads to 26214 keys and 64
-  // caches of 576 rows 119 us, alternating 142, a half of them first 129.)
+  // prefix's chunks come first.
   const int xcd = blockIdx.x & 7;
   int slot = blockIdx.x >> 3;
-  const bool prefix = slot < a.prefix_slots;
-  if (!prefix) slot -= a.prefix_slots;
+  const bool prefix = OWN == 0 || (PREFIX != 0 && slot < a.prefix_slots);
+  if (PREFIX && !prefix) slot -= a.prefix_slots;
   const int blocks = prefix ? a.prefix_blocks : a.own_blocks;
   const int unit = (slot / blocks) * 8 + xcd;
   if (unit >= (prefix ? a.prefix_units : a.own_units)) return;
   const Item it = item_of(a, prefix, unit, slot % blocks, prefix ? PREFIX : OWN);
   if (it.nothing(a)) return;
-  if constexpr (PREFIX == OWN) {
+  if constexpr (PREFIX == OWN || PREFIX == 0 || OWN == 0) {
     O::run(a, it, sh.o);
   } else {
     if (prefix) P::run(a, it, sh.p);
@@ -765,14 +784,18 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixLaunch a) {
   }
 }
 
-// A row's chunks joined, a wave per row: D / 4 lanes take a chunk's output, the
+// A row's chunks joined, W waves per row: D / 4 lanes take a chunk's output, the
 // others the next chunks', and all loads of up to kBatch chunks a lane are under
-// way together.
-template <typename T, int D>
+// way together.  One wave where that takes all chunks or the rows fill the chip
+// (4096 rows of 18 chunks: 9.8 us, by four waves a row 12.4), otherwise four (32
+// rows of 128 chunks: the whole call 99 us, by one wave 105).
+template <typename T, int D, int W>
 __global__ __launch_bounds__(kThreads) void prefix_merge_kernel(PrefixLaunch a) {
-  constexpr int kPer = D / 4, kSlots = 64 / kPer, kBatch = 8;
+  constexpr int kPer = D / 4, kSlots = 64 / kPer, kBatch = kMergeBatch;
+  __shared__ float so[W][D], sm[W], sl[W];
   const int lane = threadIdx.x & 63, d0 = (lane % kPer) * 4, mine = lane / kPer;
-  const int64_t row = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+  const int wave = threadIdx.x >> 6;
+  const int64_t row = W == 1 ? (int64_t)blockIdx.x * kWaves + wave : (int64_t)blockIdx.x;
   const int Hq = a.H * a.G;
   if (row >= (int64_t)a.B * Hq * a.T) return;
   const int t = (int)(row % a.T);
@@ -795,7 +818,7 @@ __global__ __launch_bounds__(kThreads) void prefix_merge_kernel(PrefixLaunch a) 
   f32x4 w[kBatch], o = {0.f, 0.f, 0.f, 0.f};
   float2 ml[kBatch];
   float m = -INFINITY, l = 0.f;
-  for (int i0 = 0; i0 < total; i0 += kBatch * kSlots) {
+  for (int i0 = W == 1 ? 0 : wave * kBatch * kSlots; i0 < total; i0 += W * kBatch * kSlots) {
     float mx = m;
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
@@ -830,6 +853,27 @@ __global__ __launch_bounds__(kThreads) void prefix_merge_kernel(PrefixLaunch a) 
     for (int i = 0; i < 4; ++i) o[i] = c * o[i] + c2 * __shfl_xor(o[i], x);
     m = mx;
   }
+  if constexpr (W > 1) {
+    if (mine == 0) *reinterpret_cast<f32x4*>(&so[wave][d0]) = o;
+    if (lane == 0) {
+      sm[wave] = m;
+      sl[wave] = l;
+    }
+    __syncthreads();
+    if (wave) return;
+    m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < W; ++i) m = fmaxf(m, sm[i]);
+    const float ref = m == -INFINITY ? 0.f : m;
+    l = 0.f;
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      const float c = __builtin_amdgcn_exp2f(sm[i] - ref);
+      l += c * sl[i];
+      o += c * *reinterpret_cast<const f32x4*>(&so[i][d0]);
+    }
+  }
   if (mine) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   T* dst = reinterpret_cast<T*>(a.out) + row * D + d0;
@@ -840,21 +884,36 @@ __global__ __launch_bounds__(kThreads) void prefix_merge_kernel(PrefixLaunch a) 
 
 template <typename T, int D>
 hipError_t launch_t(const PrefixLaunch& a, hipStream_t stream) {
-  const dim3 grid(8u * (unsigned)(a.prefix_slots + a.own_slots));
-  auto run = [&](auto kernel) { kernel<<<grid, kThreads, 0, stream>>>(a); };
-  const int own = a.own_rows, prefix = std::max(a.prefix_rows, own);
+  PrefixLaunch own = a;
+  auto run = [&](auto kernel, const PrefixLaunch& x, int threads = kThreads) {
+    kernel<<<8u * (unsigned)(x.prefix_slots + x.own_slots), threads, 0, stream>>>(x);
+  };
   if constexpr (std::is_same_v<T, __bf16>) {
-    if (own == kTileRows) run(prefix_kernel<T, D, kTileRows, kTileRows>);
-    else if (prefix == kTileRows && own == 32) run(prefix_kernel<T, D, kTileRows, 32>);
-    else if (prefix == kTileRows) run(prefix_kernel<T, D, kTileRows, 16>);
+    // The prefix's tiles have a launch of their own, so that the own caches'
+    // chunks, which wait for memory, run at their own occupancy.  (Both in one,
+    // alternating: 142 us for 512 rows of 8 heads to 26214 keys beside 64 caches of
+    // 576 rows; the caches' last 119.)
+    if (a.prefix_slots && a.prefix_rows >= kTileRows) {
+      PrefixLaunch prefix = a;
+      prefix.own_slots = 0;
+      if (a.prefix_rows == kTileRows) run(prefix_kernel<T, D, kTileRows, 0>, prefix);
+      else run(prefix_kernel<T, D, kWideRows, 0>, prefix, threads_of(kWideRows));
+      if (hipError_t e = hipGetLastError()) return e;
+      own.prefix_slots = 0;
+    }
+    if (a.own_rows == kTileRows) run(prefix_kernel<T, D, 0, kTileRows>, own);
+
   }
-  if (prefix < kTileRows) {
-    if (own == 32) run(prefix_kernel<T, D, 32, 32>);
-    else if (prefix == 32) run(prefix_kernel<T, D, 32, 16>);
-    else run(prefix_kernel<T, D, 16, 16>);
-  }
+  if (a.own_rows == 32) run(prefix_kernel<T, D, 32, 32>, own);
+  else if (a.own_rows == 16 && own.prefix_slots && a.prefix_rows == 32) run(prefix_kernel<T, D, 32, 16>, own);
+  else if (a.own_rows == 16) run(prefix_kernel<T, D, 16, 16>, own);
   if (hipError_t e = hipGetLastError()) return e;
-  if (!a.direct) prefix_merge_kernel<T, D><<<(unsigned)(((int64_t)a.B * a.H * a.G * a.T + kWaves - 1) / kWaves), kThreads, 0, stream>>>(a);
+  if (a.direct) return hipSuccess;
+  const int64_t rows = (int64_t)a.B * a.H * a.G * a.T;
+  if (rows > 2048 || a.prefix_split + a.own_split <= kMergeBatch * (256 / D))
+    prefix_merge_kernel<T, D, 1><<<(unsigned)((rows + kWaves - 1) / kWaves), kThreads, 0, stream>>>(a);
+  else
+    prefix_merge_kernel<T, D, kWaves><<<(unsigned)rows, kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 

@@ -92,17 +92,23 @@ Plan plan_of(const nacl_problem* p, const nacl_step* s, const nacl_prefix* x) {
   };
   a.own_rows = block(own_rows);
   a.prefix_rows = x ? block(prefix_rows) : a.own_rows;
+  // Of a prefix 256 rows share a tile where there are as many: half the reads per
+  // row (8 heads, 26214 keys: 512 rows 93 and 79 us, 2048 rows 267 and 233, 256 rows
+  // 56 and 51).  Not of the own caches, whose work-groups are fewer (4 caches of
+  // 4096 rows, 8 heads, 256 rows: 54 us, by 256 rows 83).
+  if (x && a.prefix_rows == nacl::kPrefixTileRows && prefix_rows > nacl::kPrefixTileRows) a.prefix_rows = nacl::kPrefixWideRows;
   auto up = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
   a.own_blocks = (int)up(own_rows, a.own_rows);
   a.prefix_blocks = x ? (int)up(prefix_rows, a.prefix_rows) : 0;
   const int64_t own_blocks = (int64_t)p->B * p->H * a.own_blocks, prefix_blocks = (int64_t)groups * p->H * a.prefix_blocks;
   // Chunks of about the same number of keys in both, four work-groups per CU in
   // all; a prefix read by tiles in chunks that fill the chip twice over.
-  const bool tiles = x && a.prefix_rows == nacl::kPrefixTileRows;
+  const bool tiles = x && a.prefix_rows >= nacl::kPrefixTileRows;
+  const int per_cu = a.prefix_rows == nacl::kPrefixTileRows ? 2 : 1;
   const int64_t keys = own_blocks * p->L + (tiles ? 0 : prefix_blocks * a.Lp);
   const int64_t chunk = std::max<int64_t>(nacl::kPrefixMinChunk, up(keys, 4 * kPlanCus));
   a.own_split = (int)up(p->L, chunk);
-  a.prefix_split = (int)up(a.Lp, tiles ? std::max<int64_t>(256, up(prefix_blocks * a.Lp, 2 * kPlanCus)) : chunk);
+  a.prefix_split = (int)up(a.Lp, tiles ? std::max<int64_t>(256, up(prefix_blocks * a.Lp, per_cu * kPlanCus)) : chunk);
   a.own_units = (int64_t)p->B * p->H * a.own_split;
   a.prefix_units = x ? (int64_t)groups * p->H * a.prefix_split : 0;
   a.own_slots = up(a.own_units, 8) * a.own_blocks;

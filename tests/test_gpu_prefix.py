@@ -279,3 +279,15 @@ def test_hidden_values_in_larger_blocks(G, T, B, Lp):
     odd = torch.isnan(out[0, G, T // 3:T - 1])
     assert odd[:, 5].all() and not odd[:, :5].any() and not odd[:, 6:].any()
     assert torch.isnan(lse[B - 1, G:, T - 1]).all()
+
+
+@pytest.mark.parametrize("B,G,T,D,Lp,groups", [(65, 2, 1, 128, 901, 1), (43, 3, 2, 64, 640, 1), (80, 7, 1, 128, 77, 2)])
+def test_blocks_of_256_rows(B, G, T, D, Lp, groups):
+    """One block and a bit, full blocks, groups, chunks that end inside a tile."""
+    H, L = 2, T + 20
+    q, k, v, kp, vp, lens, plens = _make(B, H, G, T, L, D, "bf16", groups, Lp, seed=B)
+    prob = nacl.Problem(B, H, L, D, "bf16", [L - 1], q_group=G)
+    prefix = nacl.Prefix(prob, kp, vp, lens=plens.to(DEV))
+    out, lse = nacl.prefix_attention(prob, nacl.Step(prob, T, lens=lens.to(DEV)), q, k, v, prefix=prefix)
+    torch.cuda.synchronize()
+    check_rows(q, k, v, kp, vp, lens, plens, out, lse, prob.c.sm_scale, _rows(B, H * G, T, 300))
