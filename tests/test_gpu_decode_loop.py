@@ -1,0 +1,185 @@
+"""The decoding step's operators together with the eviction, as a program uses
+them: a prompt rotated into its cache, attended, evicted; then steps that rotate
+one token each into the evicted cache, attend to it and to a shared document,
+and draw the next token; then a generation-phase eviction that takes the step's
+log-sum-exp.  Every step against the float64 references, and a captured step
+against the eager one."""
+
+import numpy as np
+import pytest
+import torch
+
+nacl = pytest.importorskip("paper_2408_03675_amd.nacl")
+from oracle import proxy_scores_grouped
+from oracle.step import draw_token, rotate
+from test_gpu_prefix import check_rows
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+B, H, G, D, V = 3, 2, 2, 128, 500
+HQ = H * G
+L0, P, C, M, LP = 200, 8, 48, 6, 77  # prompt, proxies, budget, steps, document
+
+
+def _f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+class Program:
+    """A layer's worth of a language model with random weights: each token's
+    projections come from a table, the logits from the attention's output."""
+
+    def __init__(self, seed=0):
+        g = torch.Generator().manual_seed(seed)
+        r = lambda *s: torch.randn(s, generator=g).to(torch.bfloat16).to(DEV)
+        self.table = r(V, HQ + 2 * H, D)
+        self.head = r(HQ * D, V) * 0.1
+        self.wq, self.wk = (1 + 0.2 * r(D) for _ in range(2))
+        self.inv_freq = (10000.0 ** (-torch.arange(D // 2, dtype=torch.float64) / (D // 2))).float().to(DEV)
+        self.prompt = torch.randint(0, V, (B, L0), generator=g).to(DEV)
+        self.kp, self.vp = r(1, H, LP, D), r(1, H, LP, D)
+        self.u = torch.rand((M, B), generator=g).to(DEV)
+        self.prob = nacl.Problem(B, H, C + M, D, "bf16", [C + M - 1], q_group=G, q_stride=(HQ * D, D, 0))
+        self.k, self.v = (torch.zeros((B, H, C + M, D), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        self.lens = torch.full((B,), C, dtype=torch.int32, device=DEV)
+        self.pos = torch.full((B, 1), L0, dtype=torch.int32, device=DEV)
+        self.token = self.prompt[:, -1].clone()
+        self.step = nacl.Step(self.prob, 1, lens=self.lens)
+        self.rotation = nacl.Rotation(self.prob, self.inv_freq, self.wq, self.wk, eps=1e-5)
+        self.document = nacl.Prefix(self.prob, self.kp, self.vp)
+        self.q = torch.empty((B, HQ, 1, D), dtype=torch.bfloat16, device=DEV)
+        self.out, self.lse = torch.empty_like(self.q), torch.empty((B, HQ, 1), device=DEV)
+        self.ws = nacl.prefix_workspace(self.prob, self.step, self.document, DEV)
+        self.sws = nacl.sample_workspace(B, V, DEV)
+        self.u_now = torch.empty((B,), device=DEV)
+        self.setting = [torch.full((B,), x, device=DEV) for x in (0.8, 0.95, 0.01)]
+        self.top_k = torch.full((B,), 40, dtype=torch.int32, device=DEV)
+
+    def split(self, tokens):
+        x = self.table[tokens].permute(0, 2, 1, 3)  # [B, heads, T, D]
+        return x[:, :HQ], x[:, HQ:HQ + H], x[:, HQ + H:]
+
+    def prefill(self):
+        """The prompt's cache, evicted to C rows; the keep sets."""
+        q, kn, vn = self.split(self.prompt)
+        k, v = (torch.empty((B, H, L0, D), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        pos = list(range(L0 - P, L0))
+        shape = nacl.Problem(B, H, L0, D, "bf16", pos, q_group=G, proxy_pos_dev=torch.tensor(pos, dtype=torch.int32, device=DEV))
+        at = torch.arange(L0, dtype=torch.int32, device=DEV)
+        qr = nacl.rotate_append(shape, nacl.Step(shape, L0), self.rotation, at, q, kn, vn, k, v)
+        out, lse, lp = nacl.attention(shape, qr, k, v, lse_proxy=True)
+        ws = nacl.workspace(shape, DEV)
+        F = nacl.score(shape, qr, k, ws, lse=lp)
+        keep = nacl.select(shape, F, C, 10, seed=3, ws=ws)
+        ko, vo = nacl.compact(shape, k, v, keep)
+        self.k[:, :, :C], self.v[:, :, :C] = ko, vo
+        return qr, k, v, F, keep, out, lse
+
+    def one(self):
+        q, kn, vn = self.split(self.token[:, None])
+        nacl.rotate_append(self.prob, self.step, self.rotation, self.pos, q, kn, vn, self.k, self.v, q_out=self.q)
+        nacl.prefix_attention(self.prob, self.step, self.q, self.k, self.v, prefix=self.document, out=self.out, lse=self.lse, ws=self.ws)
+        self.logits = self.out.view(B, HQ * D) @ self.head
+        self.tokens, self.logprobs = nacl.sample(self.logits, self.u_now, self.setting[0], self.top_k, self.setting[1],
+                                                 self.setting[2], ws=self.sws)
+        self.token.copy_(self.tokens)
+        self.lens += 1
+        self.pos += 1
+
+
+def _turned(p, x, at, w):
+    return rotate(_f64(x), at, p.inv_freq.cpu().numpy(), _f64(w), 1e-5)
+
+
+def test_prompt_then_steps_then_eviction():
+    p = Program()
+    qr, k, v, F, keep, out, lse = p.prefill()
+    torch.cuda.synchronize()
+    # The prompt's cache, its attention and its scores.
+    q, kn, vn = p.split(p.prompt)
+    assert torch.equal(v, vn)
+    half = 2.0 ** -8
+    for b, h in ((0, 0), (2, 1)):
+        ref = _turned(p, kn[b, h], np.arange(L0), p.wk)
+        size = np.abs(ref) + np.abs(np.roll(ref, D // 2, axis=1))
+        assert (np.abs(_f64(k[b, h]) - ref) <= half * np.abs(ref) + 2.0 ** -18 * size).all()
+    rows = [(b, hq, t) for b in range(B) for hq in range(HQ) for t in (0, 63, 64, L0 - 1)]
+    check_rows(qr, k, v, None, None, torch.zeros(B, dtype=torch.int32), None, out, lse, p.prob.c.sm_scale, rows)
+    for b in range(B):
+        for h in range(H):
+            ref = proxy_scores_grouped(_f64(qr[b:b + 1, h * G:(h + 1) * G]), _f64(k[b:b + 1, h:h + 1]), list(range(L0 - P, L0)),
+                                       p.prob.c.sm_scale, G)[0][0, 0]
+            assert (np.abs(_f64(F[b, h]) - ref) <= 1e-3 * ref + 1e-30).all()
+            at = keep[b, h].long()
+            assert torch.equal(p.k[b, h, :C], k[b, h, at]) and torch.equal(p.v[b, h, :C], v[b, h, at])
+
+    for i in range(M):
+        before_k, before_v, token = p.k.clone(), p.v.clone(), p.token.clone()
+        p.u_now.copy_(p.u[i])
+        p.one()
+        torch.cuda.synchronize()
+        q, kn, vn = p.split(token[:, None])
+        for b in range(B):
+            for hq in range(HQ):
+                ref = _turned(p, q[b, hq], [L0 + i], p.wq)
+                size = np.abs(ref) + np.abs(np.roll(ref, D // 2, axis=1))
+                assert (np.abs(_f64(p.q[b, hq]) - ref) <= half * np.abs(ref) + 2.0 ** -18 * size).all()
+        before_v[:, :, C + i] = vn[:, :, 0]
+        before_k[:, :, C + i] = p.k[:, :, C + i]
+        assert torch.equal(p.v, before_v) and torch.equal(p.k, before_k)
+        lens = torch.full((B,), C + i, dtype=torch.int32)
+        check_rows(p.q, p.k, p.v, p.kp, p.vp, lens, torch.tensor([LP]), p.out, p.lse, p.prob.c.sm_scale,
+                   [(b, hq, 0) for b in range(B) for hq in range(HQ)])
+        x, d = p.logits.double().cpu().numpy(), 2.0 ** -18
+        f = [float(np.float32(s)) for s in (0.8, 0.95, 0.01)]
+        for b in range(B):
+            u = float(p.u[i, b])
+            ok = {draw_token(x[b], min(max(u + e, 0), 1), f[0], 40, f[1] + c, f[2])[0] for e in (-d, 0, d) for c in (-d, 0, d)}
+            assert int(p.tokens[b]) in ok
+
+    # The round's eviction: the current token is the proxy, and its log-sum-exp
+    # over document and cache the score's.
+    ws = nacl.workspace(p.prob, DEV)
+    F = nacl.score(p.prob, p.q.expand(B, HQ, C + M, D), p.k, ws, lse=p.lse)
+    a = (p.q.double().view(B, H, G, D) @ p.k.double().transpose(2, 3).contiguous()) * p.prob.c.sm_scale
+    ref = (a - p.lse.double().view(B, H, G, 1)).exp().sum(dim=2)
+    assert ((F.double() - ref).abs() <= 1e-3 * ref + 1e-30).all()
+    keep = nacl.select(p.prob, F, C, 10, seed=4, ws=ws)
+    old_k, old_v = p.k.clone(), p.v.clone()
+    slot = nacl.compact_slots(p.prob, p.k, p.v, keep).long()
+    assert torch.equal(slot.sort(dim=-1).values, keep.long())
+    assert torch.equal(p.k[:, :, :C], old_k.gather(2, slot[..., None].expand(-1, -1, -1, D)))
+    assert torch.equal(p.v[:, :, :C], old_v.gather(2, slot[..., None].expand(-1, -1, -1, D)))
+    # The next round appends behind the kept rows.
+    p.lens.fill_(C)
+    p.u_now.copy_(p.u[0])
+    p.one()
+    torch.cuda.synchronize()
+    check_rows(p.q, p.k, p.v, p.kp, p.vp, torch.full((B,), C, dtype=torch.int32), torch.tensor([LP]), p.out, p.lse,
+               p.prob.c.sm_scale, [(b, hq, 0) for b in range(B) for hq in range(HQ)])
+
+
+def test_captured_steps_equal_eager_ones():
+    eager, captured = Program(1), Program(1)
+    for p in (eager, captured):
+        p.prefill()
+    saved = [t.clone() for t in (captured.k, captured.v, captured.lens, captured.pos, captured.token)]
+    captured.u_now.copy_(captured.u[0])
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        captured.one()  # allocations and library handles before the capture
+    torch.cuda.current_stream().wait_stream(stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured.one()
+    for t, s in zip((captured.k, captured.v, captured.lens, captured.pos, captured.token), saved):
+        t.copy_(s)
+    for i in range(M):
+        eager.u_now.copy_(eager.u[i])
+        captured.u_now.copy_(captured.u[i])
+        eager.one()
+        graph.replay()
+        torch.cuda.synchronize()
+        for name in ("q", "k", "v", "out", "lse", "tokens", "logprobs", "lens", "pos"):
+            assert torch.equal(getattr(eager, name), getattr(captured, name)), (i, name)
