@@ -334,8 +334,8 @@ size_t nacl_prefix_workspace_bytes(const nacl_problem* p, const nacl_step* s, co
  * D; query head hq reads K/V head hq / q_group.
  * out: device [B, H*q_group, T, D] contiguous, of the problem's dtype: the
  * softmax of sm_scale <q, k_j> over the visible rows times their values (fp32
- * accumulation; for bf16 the probabilities are rounded to bf16 for the value
- * product as in nacl_attention, the row once).  lse: optional device fp32
+ * accumulation; for bf16 the row is rounded once, and where more than 32 rows
+ * read the same keys the probabilities are too, for the value product).  lse: optional device fp32
  * [B, H*q_group, T], the natural log-sum-exp of the row's scaled logits; for
  * T = 1 it is the lse argument of nacl_score with the current token as the
  * proxy.  A row that sees nothing (padding among them, which sees nothing) and
