@@ -375,6 +375,7 @@ size_t nacl_sample_workspace_bytes(const nacl_draw* d);
  * evenly; a row without a logit above -infinity gives token -1 and logprob -infinity.   Weights
  * are fp32 exponentials; their sums are 64-bit integers or fp64 in an order
  * that V fixes, so a row's result depends on the row and its settings alone.
+ * (Of the top k <= 1024, a token below 2^-32 of the largest counts as nothing.)
  * tokens: device int32 [N]; logprobs: device fp32 [N]. */
 int nacl_sample(const nacl_draw* d, const void* logits, const float* u, int32_t* tokens, float* logprobs, void* ws,
                 size_t ws_bytes, void* stream);

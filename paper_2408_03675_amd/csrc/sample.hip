@@ -31,6 +31,8 @@ constexpr int kKeep = 128;                               // tokens that a slice 
 constexpr float kUnit = 0x1p22f;                         // a weight over its bin's edge, in units
 constexpr int kCountShift = 43;                          // of a bin word: count above, weight units below
 constexpr uint64_t kUnitMask = ((uint64_t)1 << kCountShift) - 1;
+constexpr int kFaint = 1024;                             // top-k: as many tokens below the bins (2^-32 of the
+                                                         // largest each) weigh no more than fp32's rounding
 constexpr float kMaxBin = 0x1p20f;                       // bins beyond are too coarse to use
 static_assert(NACL_MAX_V < (1 << (64 - kCountShift)) && NACL_MAX_V * 1.1 * 0x1p22 < 0x1p43, "bin words");
 
@@ -472,12 +474,20 @@ __device__ void finish_any(const SampleLaunch& a, int n, const Settings& s, cons
     return (uint64_t)rintf(__builtin_amdgcn_exp2f((x - mx) * scale) * 0x1p43f);
   };
   auto weight = [=](float x) -> double { return (double)units(x); };
+  // Calls f(logit, index) for every token (and with -infinity past the last).
+  auto every = [&](auto f) {
+    for (int i0 = tid * 8; i0 < V; i0 += kFinishThreads * 8) {
+      float x[8];
+      load_run<T, 1>(row, i0, 0, V, x);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) f(x[c], (uint32_t)(i0 + c));
+    }
+  };
   uint64_t sum = 0, count = 0, total, seen;
-  for (int i = tid; i < V; i += kFinishThreads) {
-    const float x = logit(row, i);
+  every([&](float x, uint32_t) {
     sum += units(x);
     count += x > -INFINITY;
-  }
+  });
   block_scan(sum, &total, sh.tmpu);
   block_scan(count, &seen, sh.tmpu);
   uint64_t last = 0;
@@ -497,12 +507,11 @@ __device__ void finish_any(const SampleLaunch& a, int n, const Settings& s, cons
       __syncthreads();
       for (int i = tid; i < kBins; i += kFinishThreads) sh.bins[i] = 0;
       __syncthreads();
-      for (int i = tid; i < V; i += kFinishThreads) {
-        const float x = logit(row, i);
+      every([&](float x, uint32_t i) {
         const uint64_t w = word_of(x, i);
         if (x > -INFINITY && w >= lo && w <= hi && w >= last)
           atomicAdd(&sh.bins[(w - lo) >> shift], (unsigned long long)(by_weight ? units(x) : 1));
-      }
+      });
       __syncthreads();
       // Bins from the top, a thread each.
       uint64_t all;
@@ -527,10 +536,9 @@ __device__ void finish_any(const SampleLaunch& a, int n, const Settings& s, cons
     last = max(last, lo);
     if (!by_weight && s.p < 1.f) {
       sum = 0;
-      for (int i = tid; i < V; i += kFinishThreads) {
-        const float x = logit(row, i);
+      every([&](float x, uint32_t i) {
         if (word_of(x, i) >= last) sum += units(x);
-      }
+      });
       block_scan(sum, &total, sh.tmpu);
     }
   }
@@ -644,7 +652,7 @@ __device__ __forceinline__ bool finish_bins(const SampleLaunch& a, int n, int n_
   __syncthreads();
   int end = sh.pick[0];
   if (s.k == 0) end = min(end, sh.pick[1]);
-  else if (all_c < (uint64_t)s.k && !left) end = kBins - 1;  // fewer than k tokens: all of them
+  else if (all_c < (uint64_t)s.k && (!left || s.k <= kFaint)) end = kBins - 1;  // fewer than k tokens, or faint ones
   if (end >= kBins) return false;  // below the bins
 
   // The smallest logit of bin b (counted from the grid's origin) or a higher one:

@@ -190,3 +190,27 @@ def test_shapes_of_rows(V, dtype, kind):
     for n in range(N):
         ok = _allowed(ref[n], u[n], t[n], k[n], p[n], m[n])
         assert _right(ref[n], got[n], lps[n], ok, t[n]), (n, got[n], lps[n], ok)
+
+
+def test_an_outlier_and_low_temperatures():
+    """Top-k whose end lies far below the largest logit, temperatures that leave
+    the bins' grid, a thousand equal logits."""
+    g = torch.Generator().manual_seed(9)
+    V = 131072
+    x = torch.randn((8, V), generator=g) * 2
+    x[0, 777] = 60.0
+    x[1, 778] = 25.0
+    x[2, 779] = 9000.0
+    x[6, 1000:2500] = 12.0
+    t = [1.0, 0.05, 1.0, 1e-5, 1e-7, 0.01, 1.0, 1e-4]
+    k = [70, 50, 900, 50, 0, 0, 3000, 5]
+    p = [1.0, 0.9, 1.0, 0.9, 0.9, 1.0, 0.5, 1.0]
+    m = [0.0] * 8
+    t = [float(np.float32(i)) for i in t]
+    p = [float(np.float32(i)) for i in p]
+    u = [float(i) for i in torch.rand((8,), generator=g)]
+    got, lps = _sample(x.to(DEV), u, t, k, p, m)
+    ref = x.double().numpy()
+    for n in range(8):
+        ok = _allowed(ref[n], u[n], t[n], k[n], p[n], m[n])
+        assert _right(ref[n], got[n], lps[n], ok, t[n]), (n, got[n], lps[n], ok)
