@@ -427,6 +427,10 @@ __device__ __forceinline__ int pick_thread(double before, double sum, double at,
   return first == 0x7FFFFFFF ? last : first;
 }
 
+// A number of the caller's, at most the largest below 1 (at 1 the rounding of the
+// sum would decide); a NaN stays one.
+__device__ __forceinline__ float below_one(float u) { return u < 0x1.fffffep-1f ? u : u >= 1.f ? 0x1.fffffep-1f : u; }
+
 // The draw among the kept tokens of a slice, of which the one is wanted at which
 // the sum of the weights passes `at`.  A thread takes a run of 8 E tokens.
 template <typename T, int E, class W>
@@ -443,7 +447,7 @@ __device__ void draw_slice(const SampleLaunch& a, int n, const T* row, int slice
   double all;
   const double before = block_scan(sum, &all, sh.tmp);
   // That thread's tokens again, a lane each.
-  const int thread = pick_thread(before, sum, at, sh);
+  const int thread = max(0, pick_thread(before, sum, at, sh));
   if ((int)threadIdx.x == thread) sh.pickd = before;
   __syncthreads();
   if (threadIdx.x >= 64) return;
@@ -462,7 +466,8 @@ __device__ void draw_slice(const SampleLaunch& a, int n, const T* row, int slice
 
 // Any row, slowly: the last kept token by a search over the words' range that
 // narrows it 256-fold a pass, then the draw over the whole row.  For logits
-// beyond the grid, and where more than kList tokens share the last bin.
+// beyond the grid, and where the slices' bins do not suffice (a top-k or top-p that
+// ends below them, more tokens of equal keys at its end than a list takes).
 template <typename T>
 __device__ void finish_any(const SampleLaunch& a, int n, const Settings& s, const T* row, float mx, float least, FinishShared& sh) {
   const int tid = threadIdx.x, V = a.V;
@@ -551,7 +556,7 @@ __device__ void finish_any(const SampleLaunch& a, int n, const Settings& s, cons
     if (kept(x, i)) part += weight(x);
   }
   const double before = block_scan(part, &all, sh.tmp);
-  const float u = a.u[n];
+  const float u = below_one(a.u[n]);
   const double at = u > 0.f ? (double)u * all : 0.0;
   if (tid == pick_thread(before, part, at, sh)) {
     double cum = before, w_of = 0.0;
@@ -575,7 +580,7 @@ __device__ __forceinline__ bool finish_bins(const SampleLaunch& a, int n, int n_
                                             float mx, float least, int top, bool left, bool unlisted, FinishShared& sh) {
   constexpr int kSlice = kFinishThreads * 8 * E;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const float u = a.u[n];
+  const float u = below_one(a.u[n]);
   auto words_of = [&](int i) { return reinterpret_cast<const unsigned long long*>(in + i * kSliceBytes + sizeof(SliceInfo)); };
   const float scale = s.scale;
   auto logit_of = [](uint64_t w) { return float_of_key((uint32_t)(w >> 32)); };
@@ -584,10 +589,12 @@ __device__ __forceinline__ bool finish_bins(const SampleLaunch& a, int n, int n_
     const float b = bin_of(x, scale);
     return (double)rintf(over_edge(x, scale, b) * kUnit) * eighths(sh.root, top - (int)b);
   };
-  // Each slice's weight outside its bins, relative to the row's largest.
+  // Each slice's weight outside its bins, relative to the row's largest (of a
+  // slice whose tokens' fp32 weights may all be 0: nothing).
   auto rest_of = [&](int i) -> double {
-    return i < n_slices && sh.info[i].max > -INFINITY ? sh.info[i].rest * exp2(((double)sh.info[i].max - (double)mx) * (double)scale)
-                                                      : 0.0;
+    if (i >= n_slices || sh.info[i].max == -INFINITY) return 0.0;
+    const double x = ((double)sh.info[i].max - (double)mx) * (double)scale;
+    return x < -120.0 ? 0.0 : sh.info[i].rest * exp2(x);
   };
 
   if (s.k == 0 && s.p >= 1.f && s.m == 0.f) {
@@ -605,7 +612,7 @@ __device__ __forceinline__ bool finish_bins(const SampleLaunch& a, int n, int n_
   }
 
   // The row's bins.
-  uint64_t units = 0, count = 0;
+  uint64_t units = 0, count = 0, under = 0;  // (`under` the row's bins: a slice's lower ones)
   if (tid < kBins) {
     for (int i = 0; i < n_slices; ++i) {
       const SliceInfo& f = sh.info[i];
@@ -615,6 +622,7 @@ __device__ __forceinline__ bool finish_bins(const SampleLaunch& a, int n, int n_
         count += x >> kCountShift;
         units += x & kUnitMask;
       }
+      if (f.max > -INFINITY && j + kBins >= 0 && j + kBins < f.n_bins) under += words_of(i)[j + kBins] & kUnitMask;
     }
   }
   const double here = (double)units * eighths(sh.root, tid < kBins ? tid : 0);
@@ -634,8 +642,9 @@ __device__ __forceinline__ bool finish_bins(const SampleLaunch& a, int n, int n_
   if (s.k == 0 && s.p < 1.f) {
     // Of the sum of everything: the bins and the slices' rests.
     double all_rest;
-    block_scan(rest_of(tid), &all_rest, sh.tmp);
-    target = (double)s.p * (all_w + all_rest * (kUnit * exp2((double)mx * (double)scale - 0.125 * top)));
+    block_scan(rest_of(tid) * (kUnit * exp2((double)mx * (double)scale - 0.125 * top)) + (double)under * eighths(sh.root, (tid & 255) + kBins),
+               &all_rest, sh.tmp);
+    target = (double)s.p * (all_w + all_rest);
   }
   __syncthreads();
   // The first bin, from the top, down to which the top k lie (or the top-p
@@ -925,6 +934,8 @@ __global__ __launch_bounds__(kFinishThreads) void sample_finish_kernel(SampleLau
     if (tid == 0) answer(a, n, -1, 0.0);
     return;
   }
+  for (int i = 0; i < n_slices; ++i)  // a slice's lower bins may lie below the row's
+    left = left || (sh.info[i].max > -INFINITY && top - sh.info[i].top + sh.info[i].n_bins > kBins);
   const float least = least_of(s, mx);
   if (!beyond && finish_bins<T, E>(a, n, n_slices, s, row, in, mx, least, top, left, unlisted, sh)) return;
   finish_any(a, n, s, row, mx, least, sh);

@@ -214,3 +214,41 @@ def test_an_outlier_and_low_temperatures():
     for n in range(8):
         ok = _allowed(ref[n], u[n], t[n], k[n], p[n], m[n])
         assert _right(ref[n], got[n], lps[n], ok, t[n]), (n, got[n], lps[n], ok)
+
+
+@pytest.mark.parametrize("V", [9000, 70000])
+def test_faint_slices(V):
+    """Stretches of the vocabulary whose weights vanish beside the others', at
+    the start and at the end, drawn from with u = 0 and just below 1."""
+    x = torch.full((8, V), -300.0)
+    x[:, V // 2:V // 2 + 40] = 50.0 + torch.arange(40) / 8
+    u = [0.0, 0.0, 0.0, 0.0, 1 - 2.0 ** -24, 1 - 2.0 ** -24, 1.0, 0.5]
+    k = [0, 0, 60, 2000, 0, 3000, 0, 0]
+    p = [1.0, 0.75, 1.0, 1.0, 1.0, 0.75, 1.0, 1.0]
+    m = [0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.125]
+    got, lps = _sample(x.to(DEV), u, [1.0] * 8, k, p, m)
+    ref = x.double().numpy()
+    for n in range(8):
+        ok = _allowed(ref[n], min(u[n], 1 - 2.0 ** -24), 1.0, k[n], p[n], m[n])
+        # with u = 0 a weight of e^-355 is the first in the order; fp32 has none
+        assert V // 2 <= got[n] < V // 2 + 40 and lps[n] < 0
+        if u[n]:
+            assert _right(ref[n], got[n], lps[n], ok, 1.0)
+        else:
+            assert got[n] == V // 2 or p[n] < 1
+
+
+def test_many_tokens_far_below():
+    """Top-p over a row whose other tokens lie 2^-30 below the largest but weigh
+    something together, in slices of very different heights."""
+    V = 262144
+    x = torch.full((3, V), -20.5)
+    x[:, 5] = 0.0
+    x[1, 100000:] = -22.5
+    x[2, :100000] = -23.0
+    p = [float(np.float32(i)) for i in (0.9999, 0.99999, 0.5)]
+    u = [0.25, 0.75, 0.9]
+    got, lps = _sample(x.to(DEV), u, [1.0] * 3, [0] * 3, p, [0.0] * 3)
+    ref = x.double().numpy()
+    for n in range(3):
+        assert _right(ref[n], got[n], lps[n], _allowed(ref[n], u[n], 1.0, 0, p[n], 0.0), 1.0)
