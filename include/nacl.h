@@ -299,7 +299,8 @@ typedef struct nacl_rotation {
  * rot is 0).  q_out: device, [B, H*q_group, T, D] with q_out_stride; it may be
  * q_new with the same strides (in place), and overlaps nothing else.  k, v: the
  * cache, [B,H,L,D] with the problem's strides, K and V disjoint and apart from
- * the new tokens.  Padding tokens (t >= n_new[b]) are not
+ * the new tokens, no two rows of them at one place (strides of at least D).
+ * Padding tokens (t >= n_new[b]) are not
  * read, and q_out and the cache keep what they hold in their places.  A
  * token whose row lies outside [0, L) joins no cache (its q_out is written).
  * Sequences may not share cache rows.  Base pointers 16-byte aligned, strides
@@ -372,8 +373,8 @@ size_t nacl_sample_workspace_bytes(const nacl_draw* d);
  *   up to and with i exceed u times their sum.
  * logprobs (optional): ln of the probability it was drawn with, w_i over the
  * kept weights' sum.  A NaN logit counts as -infinity; infinite logits share a row
- * evenly; a row without a logit above -infinity gives token -1 and logprob -infinity.   Weights
- * are fp32 exponentials; their sums are 64-bit integers or fp64 in an order
+ * evenly; a row without a logit above -infinity gives token -1 and logprob -infinity.
+ * Weights are fp32 exponentials; their sums are 64-bit integers or fp64 in an order
  * that V fixes, so a row's result depends on the row and its settings alone.
  * (Of the top k <= 1024, a token below 2^-32 of the largest counts as nothing.)
  * tokens: device int32 [N]; logprobs: device fp32 [N]. */

@@ -743,7 +743,7 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
 }
 
 // What takes the prefix's items and the own caches' (rows per work-group: 16,
-// 32 or 128).  The prefix's come first: they are the longer ones.
+// 32, 128 or 256).  The prefix's come first: they are the longer ones.
 template <typename T, int D, int ROWS>
 struct Part {
   using Shared = StreamShared<D, ROWS / 16>;
@@ -912,7 +912,6 @@ hipError_t launch_t(const PrefixLaunch& a, hipStream_t stream) {
       own.prefix_slots = 0;
     }
     if (a.own_rows == kTileRows) run(prefix_kernel<T, D, 0, kTileRows>, own);
-
   }
   if (a.own_rows == 32) run(prefix_kernel<T, D, 32, 32>, own);
   else if (a.own_rows == 16 && own.prefix_slots && a.prefix_rows == 32) run(prefix_kernel<T, D, 32, 16>, own);

@@ -195,6 +195,8 @@ int nacl_rotate_append(const nacl_problem* p, const nacl_step* s, const nacl_rot
     if (t->meets(kc) || t->meets(vc)) return fail_status(NACL_ERR_INVALID_ARG, "the new tokens or q_out overlap the cache");
   const bool in_place = q_out == q_new;
   if (in_place) {
+    if (q_new == k_new || q_new == v_new)
+      return fail_status(NACL_ERR_INVALID_ARG, "in place (q_out == q_new), k_new and v_new must lie elsewhere");
     for (int i = 0; i < 3; ++i)
       if (s->q_out_stride[i] != s->q_stride[i])
         return fail_status(NACL_ERR_INVALID_ARG, "in place (q_out == q_new), q_out_stride must be q_stride");
@@ -206,6 +208,10 @@ int nacl_rotate_append(const nacl_problem* p, const nacl_step* s, const nacl_rot
   for (int i = 0; i < 3; ++i)
     if (dims[i] > 1 && s->q_out_stride[i] < p->D)
       return fail_status(NACL_ERR_INVALID_ARG, "q_out_stride[%d] must be at least D", i);
+  const int64_t cache_dims[3] = {p->B, p->H, p->L};
+  for (int i = 0; i < 3; ++i)
+    if (cache_dims[i] > 1 && (p->k_stride[i] < p->D || p->v_stride[i] < p->D))
+      return fail_status(NACL_ERR_INVALID_ARG, "K and V need strides of at least D (k_stride, v_stride [%d])", i);
   nacl::RotateLaunch a{};
   a.B = p->B;
   a.H = p->H;

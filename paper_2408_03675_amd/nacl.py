@@ -549,6 +549,8 @@ class Step:
                 _gpu(t, name, t.device, (prob.B,), torch.int32, contiguous=True)
         if lens is not None and n_new is not None and lens.device != n_new.device:
             raise ValueError("lens and n_new are on different devices")
+        if not -2 ** 31 <= min(int(T), int(row0)) <= max(int(T), int(row0)) < 2 ** 31:
+            raise ValueError("T and row0 must fit 32 bits")
         self.prob, self.T, self.lens, self.n_new = prob, int(T), lens, n_new
         self.dev = next((t.device for t in (lens, n_new) if t is not None), None)
         B, H, L, D, Hq = prob.B, prob.H, prob.L, prob.D, prob.H * max(1, prob.q_group)
@@ -723,6 +725,8 @@ def prefix_attention(prob, step, q, k, v, prefix=None, out=None, lse=None, ws=No
 
 
 def _draw(N, V, dtype=torch.float32, stride=None):
+    if max(N, V) >= 2 ** 31:
+        raise ValueError("N and V must fit 32 bits")
     d = _Draw()
     d.N, d.V, d.dtype = int(N), int(V), NACL_F32 if dtype == torch.float32 else NACL_BF16
     d.stride = d.V if stride is None else int(stride)
@@ -755,6 +759,8 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, toke
         raise ValueError("logits must have a contiguous last dimension")
     if N > 1 and stride < V:
         raise ValueError("rows of logits must not overlap")
+    if V >= 2 ** 31:
+        raise ValueError("V must fit 32 bits")
     rows = (N,)
     _like(u, "u", dev, rows, torch.float32)
     d = _Draw(N, V, NACL_F32 if logits.dtype == torch.float32 else NACL_BF16, stride if N > 1 else V)

@@ -195,3 +195,27 @@ def test_the_binding_refuses_host_tensors():
                  lambda: nacl.sample(torch.zeros((2, 5)), torch.zeros(2))):
         with pytest.raises(ValueError, match="on the GPU"):
             call()
+
+
+@pytest.mark.parametrize("i", [0, 1, 2])
+@pytest.mark.parametrize("name", ["k_stride", "v_stride"])
+def test_rotate_needs_cache_rows_apart(lib, name, i):
+    st = [H * L * D, L * D, D]
+    for low in (0, D - 8):
+        st[i] = low
+        assert _rotate(lib, _prob(**{name: tuple(st)})) == INVALID and lib.nacl_last_error_detail()
+
+
+def test_rotate_in_place_needs_its_own_memory(lib):
+    assert _rotate(lib, qo=at(0), kn=at(0)) == INVALID
+    assert _rotate(lib, qo=at(0), vn=at(0)) == INVALID
+
+
+def test_sizes_past_32_bits_are_refused():
+    p = _prob()
+    for kw in (dict(T=2 ** 32 + 1), dict(row0=2 ** 32), dict(row0=-2 ** 31 - 1)):
+        with pytest.raises(ValueError, match="32 bits"):
+            nacl.Step(p, **kw)
+    for n, v in ((2 ** 32 + 1, 100), (1, 2 ** 32 + 100)):
+        with pytest.raises(ValueError, match="32 bits"):
+            nacl.sample_workspace(n, v)
