@@ -36,8 +36,10 @@ constexpr int kFaint = 1024;                             // top-k: as many token
 constexpr float kMaxBin = 0x1p20f;                       // bins beyond are too coarse to use
 static_assert(NACL_MAX_V < (1 << (64 - kCountShift)) && NACL_MAX_V * 1.1 * 0x1p22 < 0x1p43, "bin words");
 
-// Long vocabularies take longer slices: a work-group then has more in flight.
-// (Short ones need the work-groups.)
+// Long vocabularies take longer slices: a work-group then has more in flight, and
+// the finish joins fewer (256 x 131072, top-k 50 47.7 us, by short slices 54.3; top-p
+// 0.9 79.4 and 82.2).  Short ones need the work-groups (1 x 32000, top-p 0.9 30.5 us,
+// by long slices 33.9; 32 x 50257 37.3 and 40.5).
 constexpr int slice_of(int V) { return V > 65536 ? 2 * kMinSlice : kMinSlice; }
 static_assert(65536 / kMinSlice <= kMaxSlices, "slices");
 
@@ -49,7 +51,7 @@ struct SliceInfo {
   int left;      // top-k: a token above -infinity lies below the bins
   double rest;   // weights outside the bins over the largest one's
   int n_list;    // tokens in the bins, as words; -1: too many for the list
-  int pad;
+  int first;     // top-k of 1: the first token of the largest logit
 };
 constexpr int kSliceBytes = sizeof(SliceInfo) + (kBins + kKeep) * 8;
 
@@ -118,6 +120,9 @@ __device__ __forceinline__ void load_run(const T* row, int i0, int apart, int en
   }
 }
 
+// 256 x 131072 bf16 in 32 us (67 MB: 2.1 TB/s): vector instructions bound it, about
+// 21 per token (half of the issue slots) besides the LDS atomics of the binned tokens.
+// 1 x 32000: 5 us, the launch and the chain of loads, maximum, bins and sums.
 template <typename T, int E>
 __global__ __launch_bounds__(kSliceThreads) void sample_slices_kernel(SampleLaunch a, int n_slices) {
   constexpr int kPer = 8 * E, kSlice = kSliceThreads * kPer;
@@ -139,7 +144,10 @@ __global__ __launch_bounds__(kSliceThreads) void sample_slices_kernel(SampleLaun
     bins[tid] = 0;
     tops[tid] = 0;
   }
-  if (tid == 0) listed = 0;
+  if (tid == 0) {
+    listed = 0;
+    need = 0x7FFFFFFF;
+  }
   float tmax = x[0];
 #pragma unroll
   for (int i = 1; i < kPer; ++i) tmax = fmaxf(tmax, x[i]);
@@ -152,6 +160,18 @@ __global__ __launch_bounds__(kSliceThreads) void sample_slices_kernel(SampleLaun
   for (int w = 0; w < kSliceThreads / 64; ++w) mx = fmaxf(mx, wmax[w]);
 
   SliceInfo* info = reinterpret_cast<SliceInfo*>(static_cast<char*>(a.ws) + ((int64_t)n * n_slices + slice) * kSliceBytes);
+  if (s.k == 1) {
+    // No bins: the first of the largest (1 x 32000 6.2 us, by bins 19.1; 256 x
+    // 131072 19.7 and 41.0).
+    int at = 0x7FFFFFFF;
+#pragma unroll
+    for (int i = kPer - 1; i >= 0; --i)
+      if (x[i] == mx) at = i0 + (i / 8) * kSliceThreads * 8 + i % 8;
+    if (at != 0x7FFFFFFF) atomicMin(&need, at);
+    __syncthreads();
+    if (tid == 0) *info = SliceInfo{mx, 0, 0, 0, 0.0, 0, need};
+    return;
+  }
   const float top = bin_of(mx, s.scale);
   // All hidden, or beyond the grid (infinite and NaN products among that).
   if (mx == -INFINITY || !(__builtin_fabsf(top) < kMaxBin) || s.scale < 0x1p-60f) {
@@ -908,6 +928,10 @@ __device__ __forceinline__ bool finish_bins(const SampleLaunch& a, int n, int n_
   return true;
 }
 
+// A work-group per row, so a chain of dependent steps over some kilobytes bounds it:
+// 14 us for 1 x 32000 with top-k, top-p and a temperature, 47 for 256 x 131072 bf16,
+// where one work-group per CU waits for the rows whose last bin holds more tokens
+// than a slice lists (their logits are read again, 24 MB in all).
 template <typename T, int E>
 __global__ __launch_bounds__(kFinishThreads) void sample_finish_kernel(SampleLaunch a, int n_slices) {
   __shared__ FinishShared sh;
@@ -932,6 +956,14 @@ __global__ __launch_bounds__(kFinishThreads) void sample_finish_kernel(SampleLau
   }
   if (mx == -INFINITY) {
     if (tid == 0) answer(a, n, -1, 0.0);
+    return;
+  }
+  if (s.k == 1) {
+    if (tid == 0) {
+      int i = 0;
+      while (sh.info[i].max != mx) ++i;
+      answer(a, n, sh.info[i].first, 1.0);
+    }
     return;
   }
   for (int i = 0; i < n_slices; ++i)  // a slice's lower bins may lie below the row's

@@ -252,3 +252,27 @@ def test_many_tokens_far_below():
     ref = x.double().numpy()
     for n in range(3):
         assert _right(ref[n], got[n], lps[n], _allowed(ref[n], u[n], 1.0, 0, p[n], 0.0), 1.0)
+
+
+@pytest.mark.parametrize("V", [1, 2, 100, 8192, 65537, 1 << 18])
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+def test_first_of_the_largest(V, dt):
+    """Greedy by temperature, by top_k = 1 and by top_p <= 0: the first of equal
+    largest logits, also of zeros of both signs and of infinite ones."""
+    g = torch.Generator().manual_seed(V)
+    x = torch.randn(6, V, generator=g).round_(decimals=1)
+    x[3] = -x[3].abs()
+    x[3, V // 2:] = torch.where(torch.arange(V - V // 2) % 2 == 0, -0.0, 0.0)
+    x[4, V // 3::5] = float("inf")
+    x[5, :] = float("-inf")
+    x[5, V - 1] = -3e38
+    x[0, 0] = float("nan")
+    x = x.to(dt)
+    want = torch.where(x.isnan(), float("-inf"), x.float()) + 0.0
+    first = want.argmax(1).tolist()
+    if V == 1:
+        first[0] = -1
+    for t, k, p in ((0.0, 0, 1.0), (0.7, 1, 1.0), (2.0, 0, 0.0), (-1.0, 5, 0.5), (1.0, 1, 0.25)):
+        got, lps = _sample(x.to(DEV), [0.9] * 6, [t] * 6, [k] * 6, [p] * 6, [0.5] * 6)
+        assert got == first
+        assert [lp for lp, i in zip(lps, first) if i >= 0] == [0.0] * sum(i >= 0 for i in first)
