@@ -183,3 +183,39 @@ def test_captured_steps_equal_eager_ones():
         torch.cuda.synchronize()
         for name in ("q", "k", "v", "out", "lse", "tokens", "logprobs", "lens", "pos"):
             assert torch.equal(getattr(eager, name), getattr(captured, name)), (i, name)
+
+
+def test_two_programs_on_two_streams():
+    """Two programs of one process, each on a stream and with workspaces of its
+    own, under way at once: the same results as one after the other."""
+    def made(seed):
+        p = Program(seed)
+        p.prefill()
+        p.u_now.copy_(p.u[0])
+        return p
+
+    def steps(p):
+        log = []
+        for i in range(M):
+            p.u_now.copy_(p.u[i])
+            p.one()
+            log.append((p.out.clone(), p.lse.clone(), p.tokens, p.logprobs))
+        return log
+
+    alone = [steps(made(seed)) for seed in (1, 2)]
+    programs = [made(seed) for seed in (1, 2)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for st in streams:
+        st.wait_stream(torch.cuda.current_stream())
+    logs = [[], []]
+    for i in range(M):
+        for p, st, log in zip(programs, streams, logs):
+            with torch.cuda.stream(st):
+                p.u_now.copy_(p.u[i])
+                p.one()
+                log.append((p.out.clone(), p.lse.clone(), p.tokens, p.logprobs))
+    torch.cuda.synchronize()
+    for log, ref in zip(logs, alone):
+        for got, want in zip(log, ref):
+            for x, y in zip(got, want):
+                assert torch.equal(x, y)
