@@ -540,8 +540,7 @@ __device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& i
 // rows wait in registers while the one in hand is used).  v_mfma_f32_32x32x16_bf16
 // with the roles as above: lane (hl, n) = (lane / 32, lane mod 32) holds logits of
 // query n, keys 8 (i / 4) + 4 hl + i mod 4, and the output's entries likewise.
-// K's 16-byte pieces are swizzled by row so that a fragment's 32 rows fall on
-// distinct banks; V stays in rows and is read transposed (ds_read_b64_tr_b16).
+// V stays in rows and is read transposed (ds_read_b64_tr_b16).
 // 512 rows of 8 heads to 26214 keys: 68 us (0.81 PFLOP/s; a large product of the
 // library 1.21).  The matrix cores are busy for 0.36 of the cycles; the softmax
 // between the two products takes about as many, and two waves per SIMD that meet at
@@ -564,7 +563,7 @@ struct TileShared {
 
 template <int D, int ROWS>
 __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it, TileShared<D>& sh) {
-  constexpr int kRowBytes = D * 2, kChunks = kRowBytes / 16, kSwz = kChunks - 1;
+  constexpr int kRowBytes = D * 2, kChunks = kRowBytes / 16;
   constexpr int kC = D / 16, kDt = D / 32;
   constexpr int kThreads = 2 * ROWS;
   constexpr int kUnits = kTileKeys * kChunks / kThreads;  // 16-byte pieces of a tile per thread
@@ -592,6 +591,12 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
   const __amdgpu_buffer_rsrc_t vr = it.prefix ? rows_of<__bf16>(a.pv, a.pvs, it, key_hi) : rows_of<__bf16>(a.v, a.vs, it, key_hi);
   const uint32_t krow = (uint32_t)(it.prefix ? a.pks[2] : a.ks[2]) * 2, vrow = (uint32_t)(it.prefix ? a.pvs[2] : a.vs[2]) * 2;
 
+  // Pieces of 16 bytes are permuted by row: the 16 rows of a K fragment's half and
+  // the four rows by four pieces of a V fragment's fall on all 64 banks (two rows of
+  // D = 64 share a line of banks).  No conflicts, which were 0.29 of the LDS's busy
+  // cycles with V permuted within 128 bytes.
+  auto kswz = [](int key) { return kChunks == 16 ? key & 15 : (key >> 1) & 7; };
+  auto vswz = [](int key) { return kChunks == 16 ? (key & 3) << 2 : (key & 2) << 1; };
   const bool causal = !it.prefix && a.T > 1;
   bool odd = false;  // as for few rows
   u32x4 kreg[kUnits], vreg[kUnits];
@@ -611,8 +616,8 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
       const int p = tid + kThreads * u, r = p / kChunks, x = p % kChunks;
-      *reinterpret_cast<u32x4*>(sh.k[buf] + r * kRowBytes + ((x ^ (r & kSwz)) * 16)) = kreg[u];
-      *reinterpret_cast<u32x4*>(sh.v[buf] + r * kRowBytes + ((x ^ ((r & 3) << 1)) * 16)) = vreg[u];
+      *reinterpret_cast<u32x4*>(sh.k[buf] + r * kRowBytes + ((x ^ kswz(r)) * 16)) = kreg[u];
+      *reinterpret_cast<u32x4*>(sh.v[buf] + r * kRowBytes + ((x ^ vswz(r)) * 16)) = vreg[u];
       if (causal) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) odd = odd || (vreg[u][c] & 0x7F800000u) == 0x7F800000u || (vreg[u][c] & 0x7F80u) == 0x7F80u;
@@ -623,13 +628,13 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
   // dt + n, the keys that the lane's logits of step ks hold).
   auto kfrag = [&](int buf, int kt, int c) {
     return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(sh.k[buf] + (32 * kt + n) * kRowBytes +
-                                                                      (((2 * c + hl) ^ (n & kSwz)) * 16)));
+                                                                      (((2 * c + hl) ^ kswz(n)) * 16)));
   };
   const int i16 = lane & 15, vkey = 4 * hl + (i16 >> 2);
   uint32_t va[kDt];
 #pragma unroll
   for (int dt = 0; dt < kDt; ++dt)
-    va[dt] = (uint32_t)(vkey * kRowBytes + (((4 * dt + 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1)) ^ ((vkey & 3) << 1)) * 16) +
+    va[dt] = (uint32_t)(vkey * kRowBytes + (((4 * dt + 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1)) ^ vswz(vkey)) * 16) +
                         (i16 & 1) * 8);
   auto vfrag = [&](int buf, int ks, int dt) {
     typedef short s16x4 __attribute__((ext_vector_type(4)));
