@@ -104,16 +104,18 @@ Plan plan_of(const nacl_problem* p, const nacl_step* s, const nacl_prefix* x) {
   // Chunks of about the same number of keys in both, as many as run together:
   // three work-groups per CU of 16 rows, two of 32 (32 rows of 8 heads to 26214
   // keys: two 30 us, three 35, four 38; 32 caches of 8256 rows by 16 rows: 207, 188
-  // and 197).  A prefix read by tiles in chunks that fill the chip once; own caches
+  // and 197).  A prefix read by tiles in one chunk per CU (128 rows
+  // of 8 heads to 26214 keys: 40 us, by two per CU, with twice the partial outputs to
+  // write and join, 45; 64 rows 34.5 and 37) of at least 256 keys (128 rows of one head
+  // to 26214: 23 us, with 128 keys 26, with 512 26); own caches
   // read by tiles in twice as many, as causal blocks differ in length (512 tokens,
   // 64 query heads over 8192 rows: 207 us, by 1.5 times as many 227).
   const bool tiles = x && a.prefix_rows >= nacl::kPrefixTileRows;
-  const int tiles_per_cu = a.prefix_rows == nacl::kPrefixTileRows ? 2 : 1;
   const int64_t keys = own_blocks * p->L + (tiles ? 0 : prefix_blocks * a.Lp);
   const int per_cu = a.own_rows == nacl::kPrefixTileRows ? 4 : a.own_rows == 32 || a.prefix_rows == 32 ? 2 : 3;
   const int64_t chunk = std::max<int64_t>(nacl::kPrefixMinChunk, up(keys, per_cu * kPlanCus));
   a.own_split = (int)up(p->L, chunk);
-  a.prefix_split = (int)up(a.Lp, tiles ? std::max<int64_t>(256, up(prefix_blocks * a.Lp, tiles_per_cu * kPlanCus)) : chunk);
+  a.prefix_split = (int)up(a.Lp, tiles ? std::max<int64_t>(256, up(prefix_blocks * a.Lp, kPlanCus)) : chunk);
   a.own_units = (int64_t)p->B * p->H * a.own_split;
   a.prefix_units = x ? (int64_t)groups * p->H * a.prefix_split : 0;
   a.own_slots = up(a.own_units, 8) * a.own_blocks;
