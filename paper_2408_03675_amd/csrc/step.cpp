@@ -102,20 +102,25 @@ Plan plan_of(const nacl_problem* p, const nacl_step* s, const nacl_prefix* x) {
   a.prefix_blocks = x ? (int)up(prefix_rows, a.prefix_rows) : 0;
   const int64_t own_blocks = (int64_t)p->B * p->H * a.own_blocks, prefix_blocks = (int64_t)groups * p->H * a.prefix_blocks;
   // Chunks of about the same number of keys in both, as many as run together:
-  // three work-groups per CU of 16 rows, two of 32 (32 rows of 8 heads to 26214
-  // keys: two 30 us, three 35, four 38; 32 caches of 8256 rows by 16 rows: 207, 188
-  // and 197).  A prefix read by tiles in one chunk per CU (128 rows
-  // of 8 heads to 26214 keys: 40 us, by two per CU, with twice the partial outputs to
-  // write and join, 45; 64 rows 34.5 and 37) of at least 256 keys (128 rows of one head
-  // to 26214: 23 us, with 128 keys 26, with 512 26); own caches
-  // read by tiles in twice as many, as causal blocks differ in length (512 tokens,
-  // 64 query heads over 8192 rows: 207 us, by 1.5 times as many 227).
+  // three work-groups per CU of 16 rows (32 caches of 8256 rows: 188 us, two 207, four
+  // 197), two of 32 (3 caches of 5000 rows, 8 heads: 21.5 us, one 25; fp32, 32 rows of 8
+  // heads to 8000 keys beside 32 caches of 2000: 135 and 158), four of 128, as causal
+  // blocks differ in length (512 tokens, 64 query heads over 8192 rows: 207 us, three
+  // 227).  Where most keys are a bf16 prefix's, one: fewer partial outputs to write and
+  // join (32 rows of 8 heads to 26214 keys: 26 us, two 30, three 35; 8 sequences, 32
+  // heads, a prefix of 6553 rows and 576 of their own: 33 us, three 35.5; but 32 caches
+  // of 4000 rows beside 8 prefixes of 2000: 123 us, three 115).  A prefix read by tiles
+  // has chunks of its own, one per CU (128 rows of 8 heads to 26214 keys: 40 us, two
+  // per CU 45; 64 rows 34.5 and 37) of at least 256 keys (128 rows of one head to
+  // 26214: 23 us, with 128 keys 26, with 512 26).
   const bool tiles = x && a.prefix_rows >= nacl::kPrefixTileRows;
-  const int64_t keys = own_blocks * p->L + (tiles ? 0 : prefix_blocks * a.Lp);
-  const int per_cu = a.own_rows == nacl::kPrefixTileRows ? 4 : a.own_rows == 32 || a.prefix_rows == 32 ? 2 : 3;
+  const int64_t own_keys = own_blocks * p->L, prefix_keys = prefix_blocks * a.Lp;
+  const int64_t keys = own_keys + (tiles ? 0 : prefix_keys);
+  const bool mostly_prefix = !tiles && p->dtype == NACL_BF16 && prefix_keys >= own_keys;
+  const int per_cu = a.own_rows == nacl::kPrefixTileRows ? 4 : mostly_prefix ? 1 : a.own_rows == 32 || a.prefix_rows == 32 ? 2 : 3;
   const int64_t chunk = std::max<int64_t>(nacl::kPrefixMinChunk, up(keys, per_cu * kPlanCus));
   a.own_split = (int)up(p->L, chunk);
-  a.prefix_split = (int)up(a.Lp, tiles ? std::max<int64_t>(256, up(prefix_blocks * a.Lp, kPlanCus)) : chunk);
+  a.prefix_split = (int)up(a.Lp, tiles ? std::max<int64_t>(256, up(prefix_keys, kPlanCus)) : chunk);
   a.own_units = (int64_t)p->B * p->H * a.own_split;
   a.prefix_units = x ? (int64_t)groups * p->H * a.prefix_split : 0;
   a.own_slots = up(a.own_units, 8) * a.own_blocks;
