@@ -385,7 +385,7 @@ __device__ __forceinline__ void odd_item(const PrefixLaunch& a, const Item& it) 
 // each with a softmax of its own; K and V go from memory to the fragments' registers.
 // Memory bounds it: 32 ragged caches of up to 8256 rows, 8 heads, 4 query heads each,
 // 690 MB in 138 us (5.0 TB/s); 8 sequences over a prefix of 6553 rows and up to 576 of
-// their own, 32 heads, 158 MB in 28 us (5.7 TB/s).  One token over 2112 rows: 5.6 us,
+// their own, 32 heads, 158 MB in 27 us (5.9 TB/s).  One token over 2112 rows: 5.6 us,
 // one load latency after the other.
 
 template <int D, int R>
