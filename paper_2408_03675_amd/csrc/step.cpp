@@ -104,7 +104,8 @@ Plan plan_of(const nacl_problem* p, const nacl_step* s, const nacl_prefix* x) {
   // Chunks of about the same number of keys in both, as many as run together:
   // three work-groups per CU of 16 rows (32 caches of 8256 rows: 188 us, two 207, four
   // 197), two of 32 (3 caches of 5000 rows, 8 heads: 21.5 us, one 25; fp32, 32 rows of 8
-  // heads to 8000 keys beside 32 caches of 2000: 135 and 158), four of 128, as causal
+  // heads to 8000 keys beside 32 caches of 2000: 135 and 158) and of 16 beside a prefix
+  // read by tiles (64 caches of 576 rows, the whole call 111 us, three 116), four of 128, as causal
   // blocks differ in length (512 tokens, 64 query heads over 8192 rows: 207 us, three
   // 227).  Where most keys are a bf16 prefix's, one: fewer partial outputs to write and
   // join (32 rows of 8 heads to 26214 keys: 26 us, two 30, three 35; 8 sequences, 32
@@ -117,7 +118,7 @@ Plan plan_of(const nacl_problem* p, const nacl_step* s, const nacl_prefix* x) {
   const int64_t own_keys = own_blocks * p->L, prefix_keys = prefix_blocks * a.Lp;
   const int64_t keys = own_keys + (tiles ? 0 : prefix_keys);
   const bool mostly_prefix = !tiles && p->dtype == NACL_BF16 && prefix_keys >= own_keys;
-  const int per_cu = a.own_rows == nacl::kPrefixTileRows ? 4 : mostly_prefix ? 1 : a.own_rows == 32 || a.prefix_rows == 32 ? 2 : 3;
+  const int per_cu = a.own_rows == nacl::kPrefixTileRows ? 4 : mostly_prefix ? 1 : tiles || a.own_rows == 32 || a.prefix_rows == 32 ? 2 : 3;
   const int64_t chunk = std::max<int64_t>(nacl::kPrefixMinChunk, up(keys, per_cu * kPlanCus));
   a.own_split = (int)up(p->L, chunk);
   a.prefix_split = (int)up(a.Lp, tiles ? std::max<int64_t>(256, up(prefix_keys, kPlanCus)) : chunk);
