@@ -810,9 +810,9 @@ __global__ __launch_bounds__(threads_of(PREFIX > OWN ? PREFIX : OWN), 2) void pr
 }
 
 // A row's chunks joined (the workspace's bytes bound it: 4096 rows of 18 chunks 38 MB,
-// written and read back by way of the caches), W waves per row: D / 4 lanes take a chunk's output, the
-// others the next chunks', and all loads of up to kBatch chunks a lane are under
-// way together.  One wave where that takes all chunks or the rows fill the chip
+// written and read back by way of the caches), W waves per row: D / 4 lanes take a
+// chunk's output, the others the next chunks', and all loads of up to kBatch chunks a
+// lane are under way together.  One wave where that takes all chunks or the rows fill the chip
 // (4096 rows of 18 chunks: 9.8 us, by four waves a row 12.4), otherwise four (32
 // rows of 128 chunks: the whole call 99 us, by one wave 105).
 template <typename T, int D, int W>

@@ -93,8 +93,8 @@ Plan plan_of(const nacl_problem* p, const nacl_step* s, const nacl_prefix* x) {
   a.own_rows = block(own_rows);
   a.prefix_rows = x ? block(prefix_rows) : a.own_rows;
   // Of a prefix 256 rows share a tile where there are as many: half the reads per
-  // row (8 heads, 26214 keys: 512 rows 93 and 79 us, 2048 rows 267 and 233, 256 rows
-  // 56 and 51).  Not of the own caches, whose work-groups are fewer (4 caches of
+  // row (8 heads, 26214 keys: 512 rows 89 us, by tiles of 128 97, 2048 rows 246 and
+  // 271, 256 rows 54 and 58, 160 rows 43 and 48).  Not of the own caches, whose work-groups are fewer (4 caches of
   // 4096 rows, 8 heads, 256 rows: 54 us, by 256 rows 83).
   if (x && a.prefix_rows == nacl::kPrefixTileRows && prefix_rows > nacl::kPrefixTileRows) a.prefix_rows = nacl::kPrefixWideRows;
   auto up = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
@@ -105,9 +105,9 @@ Plan plan_of(const nacl_problem* p, const nacl_step* s, const nacl_prefix* x) {
   // three work-groups per CU of 16 rows (32 caches of 8256 rows: 188 us, two 207, four
   // 197), two of 32 (3 caches of 5000 rows, 8 heads: 21.5 us, one 25; fp32, 32 rows of 8
   // heads to 8000 keys beside 32 caches of 2000: 135 and 158) and of 16 beside a prefix
-  // read by tiles (64 caches of 576 rows, the whole call 111 us, three 116), four of 128, as causal
-  // blocks differ in length (512 tokens, 64 query heads over 8192 rows: 207 us, three
-  // 227).  Where most keys are a bf16 prefix's, one: fewer partial outputs to write and
+  // read by tiles (64 caches of 576 rows, the whole call 111 us, three 116), four of
+  // 128, as causal blocks differ in length (512 tokens, 64 query heads over 8192 rows:
+  // 207 us, three 227).  Where most keys are a bf16 prefix's, one: fewer partial outputs to write and
   // join (32 rows of 8 heads to 26214 keys: 26 us, two 30, three 35; 8 sequences, 32
   // heads, a prefix of 6553 rows and 576 of their own: 33 us, three 35.5; but 32 caches
   // of 4000 rows beside 8 prefixes of 2000: 123 us, three 115).  A prefix read by tiles
