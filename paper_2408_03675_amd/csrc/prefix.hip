@@ -901,10 +901,11 @@ __global__ __launch_bounds__(kThreads) void prefix_merge_kernel(PrefixLaunch a) 
     }
   }
   if (mine) return;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float inv = 1.f / l;
   T* dst = reinterpret_cast<T*>(a.out) + row * D + d0;
+  // (A row without weight may hold 0 times an infinite value.)
 #pragma unroll
-  for (int i = 0; i < 4; ++i) dst[i] = (T)(o[i] * inv);
+  for (int i = 0; i < 4; ++i) dst[i] = (T)(l == 0.f ? 0.f : o[i] * inv);
   if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }
 
