@@ -538,21 +538,35 @@ def _raw_stream(dev):
     return torch._C._cuda_getCurrentRawStream(dev.index)
 
 
-class Step:
+class _Keeper:
+    """Keeps tensors and their addresses between calls.  A tensor may get a new
+    storage meanwhile (a module's parameters do when it is moved), so every call
+    compares the addresses and has the tensors checked and taken again."""
+
+    def _take(self):
+        """Checks the tensors (before anything is changed), fills the struct and
+        calls _keep."""
+        raise NotImplementedError
+
+    def _keep(self, *tensors):
+        self._kept = tuple((t.data_ptr, t.data_ptr()) for t in tensors if t is not None)
+
+    def current(self):
+        for address, at in self._kept:
+            if address() != at:
+                self._take()
+                break
+
+
+class Step(_Keeper):
     """nacl_step: T new tokens per sequence, token t of sequence b in cache row
     row0 + lens[b] + t.  lens, n_new: optional int32 [B] GPU tensors, read when
     the calls run (a program may advance them in place)."""
 
     def __init__(self, prob, T=1, lens=None, row0=0, n_new=None):
-        for t, name in ((lens, "lens"), (n_new, "n_new")):
-            if t is not None:
-                _gpu(t, name, t.device, (prob.B,), torch.int32, contiguous=True)
-        if lens is not None and n_new is not None and lens.device != n_new.device:
-            raise ValueError("lens and n_new are on different devices")
         if not -2 ** 31 <= min(int(T), int(row0)) <= max(int(T), int(row0)) < 2 ** 31:
             raise ValueError("T and row0 must fit 32 bits")
         self.prob, self.T, self.lens, self.n_new = prob, int(T), lens, n_new
-        self.dev = next((t.device for t in (lens, n_new) if t is not None), None)
         B, H, L, D, Hq = prob.B, prob.H, prob.L, prob.D, prob.H * max(1, prob.q_group)
         self.dtype = prob.torch_dtype
         self.q_shape, self.new_shape = (B, Hq, self.T, D), (B, H, self.T, D)
@@ -561,17 +575,29 @@ class Step:
         self.k_stride, self.v_stride = tuple(prob.c.k_stride) + (1,), tuple(prob.c.v_stride) + (1,)
         s = _Step()
         s.T, s.row0 = self.T, int(row0)
-        s.lens = None if lens is None else lens.data_ptr()
-        s.n_new = None if n_new is None else n_new.data_ptr()
         dense = (Hq * self.T * D, self.T * D, D)
         s.q_stride[:] = s.q_out_stride[:] = dense
         s.k_stride[:] = s.v_stride[:] = (H * self.T * D, self.T * D, D)
         self.c = s
+        self._take()
+
+    def _take(self):
+        lens, n_new = self.lens, self.n_new
+        for t, name in ((lens, "lens"), (n_new, "n_new")):
+            if t is not None:
+                _gpu(t, name, t.device, (self.prob.B,), torch.int32, contiguous=True)
+        if lens is not None and n_new is not None and lens.device != n_new.device:
+            raise ValueError("lens and n_new are on different devices")
+        self.dev = next((t.device for t in (lens, n_new) if t is not None), None)
+        self.c.lens = None if lens is None else lens.data_ptr()
+        self.c.n_new = None if n_new is None else n_new.data_ptr()
         self._strided = {}  # nacl_step by the strides of the call's tensors
+        self._keep(lens, n_new)
 
     def on(self, prob, dev):
         if prob is not self.prob:
             raise ValueError("the step was made for another problem")
+        self.current()
         if self.dev is not None and self.dev != dev:
             raise ValueError(f"the step's lengths are on {self.dev}, the call runs on {dev}")
 
@@ -589,32 +615,40 @@ class Step:
         return s
 
 
-class Rotation:
+class Rotation(_Keeper):
     """nacl_rotation: the angles' frequencies, inv_freq fp32 [rot / 2] (None: no
     rotation), the optional norm weights [D] of the problem's dtype, and how
     entries pair (interleaved: 2i with 2i + 1, else i with i + rot / 2)."""
 
     def __init__(self, prob, inv_freq=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False):
+        self.inv_freq, self.q_weight, self.k_weight = inv_freq, q_weight, k_weight
+        self.fits = (prob.D, prob.torch_dtype)
+        self.c = _Rotation()
+        self.c.interleaved, self.c.eps = int(bool(interleaved)), float(eps)
+        self._take()
+
+    def _take(self):
+        inv_freq, q_weight, k_weight = self.inv_freq, self.q_weight, self.k_weight
+        D, dtype = self.fits
         if inv_freq is not None:
             _gpu(inv_freq, "inv_freq", inv_freq.device, dtype=torch.float32, contiguous=True)
             if inv_freq.dim() != 1:
                 raise ValueError("inv_freq must be one-dimensional")
         for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
             if t is not None:
-                _gpu(t, name, t.device, (prob.D,), prob.torch_dtype, contiguous=True)
-        self.tensors = tuple(t for t in (inv_freq, q_weight, k_weight) if t is not None)
-        self.dev = self.tensors[0].device if self.tensors else None
-        self.fits = (prob.D, prob.torch_dtype)
-        if any(t.device != self.dev for t in self.tensors):
+                _gpu(t, name, t.device, (D,), dtype, contiguous=True)
+        tensors = tuple(t for t in (inv_freq, q_weight, k_weight) if t is not None)
+        dev = tensors[0].device if tensors else None
+        if any(t.device != dev for t in tensors):
             raise ValueError("the rotation's tensors are on different devices")
-        r = _Rotation()
+        self.tensors, self.dev = tensors, dev
+        r = self.c
         r.rot = 0 if inv_freq is None else 2 * inv_freq.numel()
-        r.interleaved, r.eps = int(bool(interleaved)), float(eps)
         r.q_weight = None if q_weight is None else q_weight.data_ptr()
         r.k_weight = None if k_weight is None else k_weight.data_ptr()
         r.inv_freq = None if inv_freq is None else inv_freq.data_ptr()
-        self.c = r
         self._by_stride = {}  # nacl_rotation by pos_stride
+        self._keep(*self.tensors)
 
     def with_stride(self, n):
         r = self._by_stride.get(n)
@@ -625,26 +659,32 @@ class Rotation:
         return r
 
 
-class Prefix:
+class Prefix(_Keeper):
     """nacl_prefix: k, v [G, H, L, D], shared by B / G consecutive sequences
     each; lens: optional int32 [G] rows in use."""
 
     def __init__(self, prob, k, v, lens=None):
+        self.k, self.v, self.lens = k, v, lens
+        self.fits = (prob.H, prob.D, prob.torch_dtype)
+        self._take()
+
+    def _take(self):
+        k, v, lens = self.k, self.v, self.lens
+        H, D, dtype = self.fits
         if not isinstance(k, torch.Tensor) or k.dim() != 4:
             raise ValueError("the prefix's k must be [G, H, L, D]")
         G, _, L, _ = k.shape
         x = _Prefix()
         x.G, x.L = G, L
-        self.dev = _gpu(k, "the prefix's k", k.device).device
-        x.k_stride[:] = _rows4(k, "the prefix's k", self.dev, (G, prob.H, L, prob.D), prob.torch_dtype)[:3]
-        x.v_stride[:] = _rows4(v, "the prefix's v", self.dev, (G, prob.H, L, prob.D), prob.torch_dtype)[:3]
+        dev = _gpu(k, "the prefix's k", k.device).device
+        x.k_stride[:] = _rows4(k, "the prefix's k", dev, (G, H, L, D), dtype)[:3]
+        x.v_stride[:] = _rows4(v, "the prefix's v", dev, (G, H, L, D), dtype)[:3]
         if lens is not None:
-            _gpu(lens, "the prefix's lens", self.dev, (G,), torch.int32, contiguous=True)
-        self.k, self.v, self.lens = k, v, lens
-        self.fits = (prob.H, prob.D, prob.torch_dtype)
+            _gpu(lens, "the prefix's lens", dev, (G,), torch.int32, contiguous=True)
         x.k, x.v = k.data_ptr(), v.data_ptr()
         x.lens = None if lens is None else lens.data_ptr()
-        self.c = x
+        self.c, self.dev = x, dev
+        self._keep(k, v, lens)
 
 
 def rotate_append(prob, step, rotation, positions, q_new, k_new, v_new, k, v, q_out=None):
@@ -660,6 +700,7 @@ def rotate_append(prob, step, rotation, positions, q_new, k_new, v_new, k, v, q_
     step.on(prob, dev)
     if rotation.fits != step.fits[1:]:
         raise ValueError("the rotation was made for another head size or dtype")
+    rotation.current()
     if rotation.dev is not None and rotation.dev != dev:
         raise ValueError(f"the rotation's tensors are on {rotation.dev}, the call runs on {dev}")
     dt = step.dtype
@@ -682,6 +723,8 @@ def rotate_append(prob, step, rotation, positions, q_new, k_new, v_new, k, v, q_
 def prefix_workspace(prob, step, prefix=None, device="cuda"):
     """A workspace for prefix_attention calls of these sizes."""
     lib = load_library()
+    if prefix is not None:
+        prefix.current()
     n = int(lib.nacl_prefix_workspace_bytes(prob.ref(), ctypes.byref(step.c),
                                             None if prefix is None else ctypes.byref(prefix.c)))
     if n == 0:
@@ -699,9 +742,11 @@ def prefix_attention(prob, step, q, k, v, prefix=None, out=None, lse=None, ws=No
     _cache(k, "k", dev, step, step.k_stride)
     _cache(v, "v", dev, step, step.v_stride)
     step.on(prob, dev)
-    if prefix is not None and (prefix.dev != dev or prefix.fits != step.fits):
-        raise ValueError(f"the prefix is on {prefix.dev} with (heads, D, dtype) {prefix.fits}, the call's are on {dev} "
-                         f"with {step.fits}")
+    if prefix is not None:
+        prefix.current()
+        if prefix.dev != dev or prefix.fits != step.fits:
+            raise ValueError(f"the prefix is on {prefix.dev} with (heads, D, dtype) {prefix.fits}, the call's are on {dev} "
+                             f"with {step.fits}")
     s = step.strided(_rows4(q, "q", dev, step.q_shape, step.dtype))
     if out is None:
         out = torch.empty(step.q_shape, dtype=step.dtype, device=dev)

@@ -1,0 +1,96 @@
+"""A step's, a rotation's and a prefix's tensors that get a new storage
+between two calls (as a module's parameters do when it is moved): the calls read
+the new one, and refuse one that does not fit.  The old storages are kept, so that
+a call that read them would only be wrong."""
+
+import pytest
+import torch
+
+nacl = pytest.importorskip("paper_2408_03675_amd.nacl")
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+B, H, G, T, L, D = 3, 2, 2, 2, 40, 64
+BF = torch.bfloat16
+
+
+def _ints(*x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def _randn(seed, *shape):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn(shape, generator=g).to(BF).to(DEV)
+
+
+class Case:
+    def __init__(self, seed):
+        self.prob = nacl.Problem(B, H, L, D, "bf16", [L - 1], q_group=G)
+        self.lens, self.n_new = _ints(3 + seed, 11, 20 - seed), _ints(T, 1 + seed % 2, T)
+        self.inv_freq = (10.0 + seed) ** (-torch.arange(D // 2, device=DEV) / (D // 2))
+        self.wq, self.wk = _randn(seed + 10, D), _randn(seed + 20, D)
+        self.kp, self.vp, self.plens = _randn(seed + 30, 1, H, 33, D), _randn(seed + 40, 1, H, 33, D), _ints(20 + seed)
+        self.make()
+
+    def make(self):
+        self.step = nacl.Step(self.prob, T, lens=self.lens, n_new=self.n_new)
+        self.rotation = nacl.Rotation(self.prob, self.inv_freq, self.wq, self.wk)
+        self.prefix = nacl.Prefix(self.prob, self.kp, self.vp, lens=self.plens)
+
+    def tensors(self):
+        return dict(lens=self.lens, n_new=self.n_new, inv_freq=self.inv_freq, wq=self.wq, wk=self.wk, kp=self.kp,
+                    vp=self.vp, plens=self.plens)
+
+    def run(self):
+        q, kn, vn = _randn(1, B, H * G, T, D), _randn(2, B, H, T, D), _randn(3, B, H, T, D)
+        k, v = _randn(4, B, H, L, D), _randn(5, B, H, L, D)
+        pos = _ints(*range(100, 100 + T))
+        out = torch.zeros_like(q)
+        nacl.rotate_append(self.prob, self.step, self.rotation, pos, q, kn, vn, k, v, q_out=out)
+        att, lse = nacl.prefix_attention(self.prob, self.step, q, k, v, prefix=self.prefix)
+        torch.cuda.synchronize()
+        return out, k, v, att, lse
+
+
+@pytest.mark.parametrize("which", ["lens", "n_new", "inv_freq", "wq", "wk", "kp", "vp", "plens"])
+def test_calls_read_a_new_storage(which):
+    a, other = Case(0), Case(1)
+    first = a.run()
+    t = a.tensors()[which]
+    old = t.data
+    t.data = other.tensors()[which].clone()
+    got = a.run()
+    a.make()
+    want = a.run()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    assert not all(torch.equal(x, y) for x, y in zip(got, first))
+    t.data = old
+    assert all(torch.equal(x, y) for x, y in zip(a.run(), first))
+
+
+@pytest.mark.parametrize("which", ["lens", "n_new", "inv_freq", "wq", "wk", "kp", "vp", "plens"])
+def test_calls_refuse_a_storage_that_does_not_fit(which):
+    a = Case(0)
+    first = a.run()
+    t = a.tensors()[which]
+    old = t.data
+    for bad in (old.cpu(), old.repeat_interleave(2, 0)[::2], torch.cat((old, old))):
+        if bad.is_cuda and bad.shape == old.shape and bad.is_contiguous():
+            continue  # one entry: contiguous at any stride
+        if which == "inv_freq" and bad.is_cuda and bad.is_contiguous():
+            continue  # another number of rotated entries
+        t.data = bad
+        with pytest.raises(ValueError):
+            a.run()
+    t.data = old
+    assert all(torch.equal(x, y) for x, y in zip(a.run(), first))
+
+
+def test_a_rotation_may_change_its_frequencies_number():
+    a = Case(0)
+    a.run()
+    old = a.inv_freq.data
+    a.inv_freq.data = old[:16].clone()
+    got = a.run()
+    a.make()
+    assert all(torch.equal(x, y) for x, y in zip(got, a.run()))
