@@ -202,15 +202,18 @@ class Problem:
         s.k_stride[:] = k_stride or dense
         s.v_stride[:] = v_stride or dense
         s.proxy_pos = ctypes.cast(self._pos, ctypes.POINTER(ctypes.c_int32))
-        if proxy_pos_dev is not None:
-            if not (isinstance(proxy_pos_dev, torch.Tensor) and proxy_pos_dev.is_cuda and
-                    proxy_pos_dev.dtype == torch.int32 and proxy_pos_dev.is_contiguous() and
-                    proxy_pos_dev.numel() == len(pos)):
-                raise ValueError("proxy_pos_dev must be a contiguous int32 GPU tensor with one entry per proxy")
-        self._pos_dev = proxy_pos_dev
-        s.proxy_pos_dev = None if proxy_pos_dev is None else proxy_pos_dev.data_ptr()
         s.q_group = self.q_group
         self.c = s
+        self._pos_dev = proxy_pos_dev
+        if proxy_pos_dev is not None:
+            self._take_pos_dev()
+
+    def _take_pos_dev(self):
+        t = self._pos_dev
+        if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and
+                t.numel() == len(self.proxy_pos)):
+            raise ValueError("proxy_pos_dev must be a contiguous int32 GPU tensor with one entry per proxy")
+        self.c.proxy_pos_dev = t.data_ptr()
 
     @classmethod
     def from_tensors(cls, q, k, v, proxy_pos, n_protect=None, sm_scale=None, proxy_pos_dev=None):
@@ -242,6 +245,10 @@ class Problem:
         return torch.float32 if self.c.dtype == NACL_F32 else torch.bfloat16
 
     def ref(self):
+        """The struct for a call.  proxy_pos_dev may have got a new storage since
+        the last one (a module's buffer does when it is moved)."""
+        if self._pos_dev is not None and self._pos_dev.data_ptr() != self.c.proxy_pos_dev:
+            self._take_pos_dev()
         return ctypes.byref(self.c)
 
     # Shapes the entry points expect.

@@ -1,4 +1,4 @@
-"""A step's, a rotation's and a prefix's tensors that get a new storage
+"""A step's, a rotation's, a prefix's and a problem's tensors that get a new storage
 between two calls (as a module's parameters do when it is moved): the calls read
 the new one, and refuse one that does not fit.  The old storages are kept, so that
 a call that read them would only be wrong."""
@@ -94,3 +94,26 @@ def test_a_rotation_may_change_its_frequencies_number():
     got = a.run()
     a.make()
     assert all(torch.equal(x, y) for x, y in zip(got, a.run()))
+
+
+def test_the_problem_s_positions():
+    n = 600
+    pos = list(range(n - 256, n, 2))  # 128 of them: their positions are read on the device
+    dev = torch.tensor(pos, dtype=torch.int32, device=DEV)
+    prob = nacl.Problem(1, H, n, D, "bf16", pos, proxy_pos_dev=dev)
+    q, k = _randn(6, 1, H, n, D), _randn(7, 1, H, n, D)
+    ws = nacl.workspace(prob, DEV)
+    want = nacl.score(prob, q, k, ws).clone()
+    old = dev.data
+    dev.data = dev.clone()
+    old.copy_(_ints(*range(128)))
+    got = nacl.score(prob, q, k, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+    for bad in (old[:2].clone(), old.cpu(), old.long()):
+        try:
+            dev.data = bad
+        except RuntimeError:  # torch does not take another dtype
+            continue
+        with pytest.raises(ValueError):
+            nacl.score(prob, q, k, ws)
