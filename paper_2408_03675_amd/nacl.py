@@ -681,6 +681,8 @@ class Prefix(_Keeper):
         if not isinstance(k, torch.Tensor) or k.dim() != 4:
             raise ValueError("the prefix's k must be [G, H, L, D]")
         G, _, L, _ = k.shape
+        if max(G, L) >= 2 ** 31:
+            raise ValueError("the prefix's groups and rows must fit 32 bits")
         x = _Prefix()
         x.G, x.L = G, L
         dev = _gpu(k, "the prefix's k", k.device).device
@@ -802,17 +804,17 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, toke
     lib = _lib or load_library()
     if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("logits must be [N, V] of fp32 or bf16")
+    N, V = logits.shape
+    if max(N, V) >= 2 ** 31:
+        raise ValueError("N and V must fit 32 bits")
     dev = logits.device
     if not logits.is_cuda:
         _gpu(logits, "logits", dev)
-    N, V = logits.shape
     stride, one = logits.stride()
     if V > 1 and one != 1:
         raise ValueError("logits must have a contiguous last dimension")
     if N > 1 and stride < V:
         raise ValueError("rows of logits must not overlap")
-    if V >= 2 ** 31:
-        raise ValueError("V must fit 32 bits")
     rows = (N,)
     _like(u, "u", dev, rows, torch.float32)
     d = _Draw(N, V, NACL_F32 if logits.dtype == torch.float32 else NACL_BF16, stride if N > 1 else V)

@@ -219,3 +219,13 @@ def test_sizes_past_32_bits_are_refused():
     for n, v in ((2 ** 32 + 1, 100), (1, 2 ** 32 + 100)):
         with pytest.raises(ValueError, match="32 bits"):
             nacl.sample_workspace(n, v)
+
+
+def test_rows_and_groups_past_32_bits_are_refused():
+    """2^32 + 1 of them would pass for one."""
+    n = 2 ** 32 + 1
+    with pytest.raises(ValueError, match="32 bits"):
+        nacl.sample(torch.empty((n, 1), device="meta"), torch.empty(n, device="meta"))
+    k = torch.empty((1, 2, 64, 64), dtype=torch.bfloat16, device="meta").expand(n, 2, 64, 64)
+    with pytest.raises(ValueError, match="32 bits"):
+        nacl.Prefix(nacl.Problem(1, 2, 64, 64, "bf16", [63]), k, k)
