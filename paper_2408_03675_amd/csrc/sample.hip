@@ -495,7 +495,7 @@ __device__ void finish_any(const SampleLaunch& a, int n, const Settings& s, cons
   // Weights in units of 2^-43 of the largest: 2^20 of them fit a word.
   auto units = [=](float x) -> uint64_t {
     if (x == mx) return 1ull << 43;
-    if (x == -INFINITY) return 0;
+    if (x == -INFINITY || mx == INFINITY) return 0;  // (an infinite temperature's 0 times infinity: NaN)
     return (uint64_t)rintf(__builtin_amdgcn_exp2f((x - mx) * scale) * 0x1p43f);
   };
   auto weight = [=](float x) -> double { return (double)units(x); };
