@@ -359,8 +359,9 @@ typedef struct nacl_draw {
 } nacl_draw;
 #define NACL_MAX_V (1 << 20)
 
-/* Workspace bytes of nacl_sample (0 on invalid input).  Device memory, 256-byte
- * aligned; its contents need no initialisation. */
+/* Workspace bytes of nacl_sample (0 on invalid input), the same for both
+ * dtypes.  Device memory, 256-byte aligned; its contents need no
+ * initialisation. */
 size_t nacl_sample_workspace_bytes(const nacl_draw* d);
 
 /* The next token of every row of logits [N, V] (row stride d->stride, element

@@ -289,7 +289,7 @@ struct SampleLaunch {
   float* logprobs;               // or nullptr
   void* ws;
 };
-size_t sample_workspace(int N, int V, int dtype);
+size_t sample_workspace(int N, int V);
 hipError_t launch_sample(const SampleLaunch& a, int dtype, hipStream_t stream);
 
 }  // namespace nacl

@@ -32,7 +32,7 @@ constexpr float kUnit = 0x1p22f;                         // a weight over its bi
 constexpr int kCountShift = 43;                          // of a bin word: count above, weight units below
 constexpr uint64_t kUnitMask = ((uint64_t)1 << kCountShift) - 1;
 constexpr int kFaint = 1024;                             // top-k: as many tokens below the bins (2^-32 of the
-                                                         // largest each) weigh no more than fp32's rounding
+                                                         // largest each) weigh less than one unit, 2^-22 of it
 constexpr float kMaxBin = 0x1p20f;                       // bins beyond are too coarse to use
 static_assert(NACL_MAX_V < (1 << (64 - kCountShift)) && NACL_MAX_V * 1.1 * 0x1p22 < 0x1p43, "bin words");
 
@@ -487,7 +487,7 @@ __device__ void draw_slice(const SampleLaunch& a, int n, const T* row, int slice
 // Any row, slowly: the last kept token by a search over the words' range that
 // narrows it 256-fold a pass, then the draw over the whole row.  For logits
 // beyond the grid, and where the slices' bins do not suffice (a top-k or top-p that
-// ends below them, more tokens of equal keys at its end than a list takes).
+// ends below them).
 template <typename T>
 __device__ void finish_any(const SampleLaunch& a, int n, const Settings& s, const T* row, float mx, float least, FinishShared& sh) {
   const int tid = threadIdx.x, V = a.V;
@@ -847,6 +847,8 @@ __device__ __forceinline__ bool finish_bins(const SampleLaunch& a, int n, int n_
       lo = max(w_lo, lo);
       hi = w_hi < hi ? w_hi : hi;
     }
+    // (Eight passes reach a single word; a bin's tokens outside the edges' margin
+    // above would not be narrowed.)
     if (!held || n_here > kList) return false;
     // Those of the range, one per thread in falling order (0 past their number).
     int m = n_held;
@@ -975,7 +977,7 @@ __global__ __launch_bounds__(kFinishThreads) void sample_finish_kernel(SampleLau
 
 }  // namespace
 
-size_t sample_workspace(int N, int V, int) { return (size_t)N * ((V + slice_of(V) - 1) / slice_of(V)) * kSliceBytes; }
+size_t sample_workspace(int N, int V) { return (size_t)N * ((V + slice_of(V) - 1) / slice_of(V)) * kSliceBytes; }
 
 hipError_t launch_sample(const SampleLaunch& a, int dtype, hipStream_t stream) {
   const int slice = slice_of(a.V), n_slices = (a.V + slice - 1) / slice;

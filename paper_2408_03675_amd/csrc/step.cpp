@@ -350,7 +350,7 @@ int nacl_prefix_attention(const nacl_problem* p, const nacl_step* s, const nacl_
 size_t nacl_sample_workspace_bytes(const nacl_draw* d) {
   nacl::clear_detail();
   if (check_draw(d) != NACL_OK) return 0;
-  return align_up(std::max<size_t>(nacl::sample_workspace(d->N, d->V, d->dtype), 1));
+  return align_up(std::max<size_t>(nacl::sample_workspace(d->N, d->V), 1));
 }
 
 int nacl_sample(const nacl_draw* d, const void* logits, const float* u, int32_t* tokens, float* logprobs, void* ws,

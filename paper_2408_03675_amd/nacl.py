@@ -778,19 +778,18 @@ def prefix_attention(prob, step, q, k, v, prefix=None, out=None, lse=None, ws=No
     return out, lse
 
 
-def _draw(N, V, dtype=torch.float32, stride=None):
+def _draw(N, V):
     if max(N, V) >= 2 ** 31:
         raise ValueError("N and V must fit 32 bits")
     d = _Draw()
-    d.N, d.V, d.dtype = int(N), int(V), NACL_F32 if dtype == torch.float32 else NACL_BF16
-    d.stride = d.V if stride is None else int(stride)
+    d.N, d.V, d.dtype, d.stride = int(N), int(V), NACL_F32, int(V)
     return d
 
 
 def sample_workspace(N, V, device="cuda"):
     """A workspace for sample calls of N rows over a vocabulary of V, of either dtype."""
     lib = load_library()
-    n = max(int(lib.nacl_sample_workspace_bytes(ctypes.byref(_draw(N, V, t)))) for t in (torch.float32, torch.bfloat16))
+    n = int(lib.nacl_sample_workspace_bytes(ctypes.byref(_draw(N, V))))
     if n == 0:
         raise NaclError(NACL_ERR_INVALID_ARG, lib.nacl_last_error_detail().decode())
     return torch.empty(n, dtype=torch.uint8, device=device)
