@@ -502,19 +502,15 @@ def evict_noalloc(prob, q, k, v, C, Cr, sampling=SAMPLE_SOFTMAX, seed=0, layer=0
 
 # The decoding step between two evictions (Algorithm 1, generation phase).
 
-class _On:
-    """Makes a tensor's device the current one for a launch on its stream."""
-
-    def __init__(self, dev):
-        self.guard = torch.cuda.device(dev) if dev.index != torch.cuda.current_device() else None
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _launch(dev, call, *args):
+    """call(*args, stream) on dev's current stream, with dev the current device."""
+    if dev.index == torch._C._cuda_getDevice():
+        status = call(*args, _raw_stream(dev))
+    else:
+        with torch.cuda.device(dev):
+            status = call(*args, _raw_stream(dev))
+    if status != NACL_OK:
+        _check(status)
 
 
 def _like(t, name, dev, shape, dtype):
@@ -723,9 +719,8 @@ def rotate_append(prob, step, rotation, positions, q_new, k_new, v_new, k, v, q_
         _like(positions, "positions", dev, (prob.B, step.T) if per_row else (step.T,), torch.int32)
         pos = positions.data_ptr()
     r = rotation.with_stride(step.T if pos is not None and per_row else 0)
-    with _On(dev):
-        _check(lib.nacl_rotate_append(prob.ref(), s, r, pos, q_new.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
-                                      q_out.data_ptr(), k.data_ptr(), v.data_ptr(), _raw_stream(dev)))
+    _launch(dev, lib.nacl_rotate_append, prob.ref(), s, r, pos, q_new.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
+            q_out.data_ptr(), k.data_ptr(), v.data_ptr())
     return q_out
 
 
@@ -771,10 +766,8 @@ def prefix_attention(prob, step, q, k, v, prefix=None, out=None, lse=None, ws=No
         ws = prefix_workspace(prob, step, prefix, dev)
     n = ws.numel()
     _like(ws, "ws", dev, (n,), torch.uint8)
-    with _On(dev):
-        _check(lib.nacl_prefix_attention(prob.ref(), s, None if prefix is None else prefix.c, q.data_ptr(), k.data_ptr(),
-                                         v.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
-                                         ws.data_ptr(), n, _raw_stream(dev)))
+    _launch(dev, lib.nacl_prefix_attention, prob.ref(), s, None if prefix is None else prefix.c, q.data_ptr(), k.data_ptr(),
+            v.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(), ws.data_ptr(), n)
     return out, lse
 
 
@@ -843,7 +836,6 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, toke
         ws = sample_workspace(N, V, dev)
     n = ws.numel()
     _like(ws, "ws", dev, (n,), torch.uint8)
-    with _On(dev):
-        _check(lib.nacl_sample(d, logits.data_ptr(), u.data_ptr(), tokens.data_ptr(),
-                               None if logprobs is None else logprobs.data_ptr(), ws.data_ptr(), n, _raw_stream(dev)))
+    _launch(dev, lib.nacl_sample, d, logits.data_ptr(), u.data_ptr(), tokens.data_ptr(),
+            None if logprobs is None else logprobs.data_ptr(), ws.data_ptr(), n)
     return tokens, logprobs
