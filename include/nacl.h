@@ -375,6 +375,8 @@ size_t nacl_sample_workspace_bytes(const nacl_draw* d);
  * logprobs (optional): ln of the probability it was drawn with, w_i over the
  * kept weights' sum.  A NaN logit counts as -infinity; infinite logits share a row
  * evenly; a row without a logit above -infinity gives token -1 and logprob -infinity.
+ * (Hide tokens by -infinity: logits near the type's lowest value, or by a large finite
+ * amount below the others, give the same tokens by a path several times slower.)
  * Weights are fp32 exponentials; their sums are 64-bit integers or fp64 in an order
  * that V fixes, so a row's result depends on the row and its settings alone.
  * (Of the top k <= 1024, a token below 2^-32 of the largest counts as nothing.)

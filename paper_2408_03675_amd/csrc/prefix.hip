@@ -384,9 +384,11 @@ __device__ __forceinline__ void odd_item(const PrefixLaunch& a, const Item& it) 
 // Few rows: 16 R per work-group, whose waves take the chunk's tiles in turn,
 // each with a softmax of its own; K and V go from memory to the fragments' registers.
 // Memory bounds it: 32 ragged caches of up to 8256 rows, 8 heads, 4 query heads each,
-// 690 MB in 138 us (5.0 TB/s); 8 sequences over a prefix of 6553 rows and up to 576 of
-// their own, 32 heads, 158 MB in 27 us (5.9 TB/s).  One token over 2112 rows: 5.6 us,
-// one load latency after the other.
+// 690 MB in 137 us at best, 147 on average (5.0 and 4.7 TB/s; reads alone of as many
+// bytes reach 5.9); 8 sequences over a prefix of 6553 rows and up to 576 of their own,
+// 32 heads, 158 MB in 27 us (5.9 TB/s); fp32, 32 caches of 4128 rows, 1.08 GB in a call
+// of 191 us (5.7 TB/s).  One token over 2112 rows: 5.6 to 6 us, one load latency after
+// the other.
 
 template <int D, int R>
 struct StreamShared {
@@ -541,10 +543,10 @@ __device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& i
 // with the roles as above: lane (hl, n) = (lane / 32, lane mod 32) holds logits of
 // query n, keys 8 (i / 4) + 4 hl + i mod 4, and the output's entries likewise.
 // V stays in rows and is read transposed (ds_read_b64_tr_b16).
-// 512 rows of 8 heads to 26214 keys: 68 us (0.81 PFLOP/s; a large product of the
-// library 1.21).  The matrix cores are busy for 0.36 of the cycles; the softmax
-// between the two products takes about as many, and two waves per SIMD that meet at
-// each tile's barrier overlap the two in part.
+// 512 rows of 8 heads to 26214 keys: 67.5 us (0.82 PFLOP/s; a large product of the
+// library 1.21).  The matrix cores are busy for 0.35 of the cycles (the LDS for 0.22,
+// without conflicts); the softmax between the two products takes about as many, and two
+// waves per SIMD that meet at each tile's barrier overlap the two in part.
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -553,7 +555,8 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 // it is passed by 2^8 spares most rescales: 512 rows of 8 heads to 26214 keys 80.0 us
 // instead of 83.6, but with logits of standard deviation 1 / 2 / 3 an error of 2.26 /
 // 2.10 / 1.94e-3 of the output's size instead of 2.14 / 1.75 / 1.68e-3; the output's
-// own rounding is 1.66e-3.  The probabilities as two bf16 reach that at 101.0 us.)
+// own rounding is 1.66e-3.  The probabilities as two bf16 reach that at 101.0 us; one,
+// as in the prefill's attention, is what matrix cores as busy as here are worth.)
 constexpr int kAhead = 2;
 
 template <int D>
@@ -809,12 +812,13 @@ __global__ __launch_bounds__(threads_of(PREFIX > OWN ? PREFIX : OWN), 2) void pr
   }
 }
 
-// A row's chunks joined (the workspace's bytes bound it: 4096 rows of 18 chunks 38 MB,
+// A row's chunks joined (the workspace's bytes bound it: 4096 rows of 17 chunks 36 MB,
 // written and read back by way of the caches), W waves per row: D / 4 lanes take a
 // chunk's output, the others the next chunks', and all loads of up to kBatch chunks a
 // lane are under way together.  One wave where that takes all chunks or the rows fill the chip
-// (4096 rows of 18 chunks: 9.8 us, by four waves a row 12.4), otherwise four (32
-// rows of 128 chunks: the whole call 99 us, by one wave 105).
+// (4096 rows of 17 chunks: 9.6 us, by four waves a row 12.8; of 2560 rows of 43 chunks
+// the whole call 45.7 and 45.7), otherwise four (32 rows of 128 chunks: the whole call
+// 99 us, by one wave 105).
 template <typename T, int D, int W>
 __global__ __launch_bounds__(kThreads) void prefix_merge_kernel(PrefixLaunch a) {
   constexpr int kPer = D / 4, kSlots = 64 / kPer, kBatch = kMergeBatch;

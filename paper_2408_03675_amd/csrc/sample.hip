@@ -28,7 +28,9 @@ constexpr int kFinishThreads = 1024;
 constexpr int kList = kFinishThreads;                    // tokens that the finish sorts, one per thread
 constexpr int kWide = 6144;                              // tokens of a bin that it holds
 constexpr int kKeep = 128;                               // tokens that a slice lists
-constexpr float kUnit = 0x1p22f;                         // a weight over its bin's edge, in units
+constexpr float kUnit = 0x1p22f;                         // a weight over its bin's edge, in units: rounded by 2^-23
+                                                         // of it as an fp32 exponential is, so that sums of
+                                                         // integers need no order (log-probabilities good to 1.4e-7)
 constexpr int kCountShift = 43;                          // of a bin word: count above, weight units below
 constexpr uint64_t kUnitMask = ((uint64_t)1 << kCountShift) - 1;
 constexpr int kFaint = 1024;                             // top-k: as many tokens below the bins (2^-32 of the
