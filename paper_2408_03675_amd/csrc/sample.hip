@@ -687,9 +687,11 @@ __device__ __forceinline__ bool finish_bins(const SampleLaunch& a, int n, int n_
   if (end >= kBins) return false;  // below the bins
 
   // The smallest logit of bin b (counted from the grid's origin) or a higher one:
-  // a few steps around the quotient, a lane each.
+  // a few steps around the quotient, a lane each.  (Bin 0 begins below 0, where the
+  // product vanishes: at half of the smallest denormal.)
   auto first_of = [&](float b) {
-    const float x = float_of_key(float_order_key(b / (8.f * scale)) - 24 + lane);
+    const float q = b == 0.f ? -0x1p-149f / (16.f * scale) : b / (8.f * scale);
+    const float x = float_of_key(float_order_key(q) - 24 + lane);
     const uint64_t in = __ballot(bin_of(x, scale) >= b) | 1ull << 63;
     return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), __builtin_ctzll(in)));
   };

@@ -111,3 +111,17 @@ def test_infinite_temperature_and_infinite_logits():
     assert got[:4] == [100, 400, 400, 400]
     assert all(abs(lp - math.log(0.5)) < 1e-6 for lp in lps[:4])
     assert got[4] == 301 and abs(lps[4] + math.log(598)) < 1e-6  # 598 equal tokens, 7 and 8 hidden
+
+
+@pytest.mark.parametrize("sign", [-1, 1])
+@pytest.mark.parametrize("t", [1.0, 3e3, 1e6, 1e12])
+def test_denormal_logits(t, sign):
+    """Logits of less than 2^-126, whose products with the temperature's
+    reciprocal vanish: still in order, with equal weights."""
+    V = 3000
+    x = sign * 1e-42 * torch.rand((6, V), generator=torch.Generator().manual_seed(V))
+    s = ([0.1, 0.5, 0.9, 0.3, 0.7, 0.5], [t] * 6, [0, 0, 0, 900, 2000, 0], [0.5, 0.25, 0.875, 1.0, 0.5, 1.0], [0.0] * 5 + [0.5])
+    got, lps = _sample(x.to(DEV), *s)
+    ref = x.double().numpy()
+    for n in range(6):
+        check_draw(ref[n], got[n], lps[n], *(i[n] for i in s))
