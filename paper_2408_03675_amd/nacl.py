@@ -171,6 +171,8 @@ def _gpu(t, name, dev, shape=None, dtype=None, strides=None, contiguous=False):
         raise ValueError(f"{name} has strides {tuple(t.stride())}, the problem has {tuple(strides)} (+ 1)")
     if contiguous and not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
+    if t.data_ptr() == 0 and t.numel():  # (a null address would mean that it was not given)
+        raise ValueError(f"{name} has no memory")
     return t
 
 

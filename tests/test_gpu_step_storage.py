@@ -96,6 +96,22 @@ def test_a_rotation_may_change_its_frequencies_number():
     assert all(torch.equal(x, y) for x, y in zip(got, a.run()))
 
 
+@pytest.mark.parametrize("which", ["lens", "n_new", "inv_freq", "wq", "wk", "kp", "vp", "plens"])
+def test_calls_refuse_a_freed_storage(which):
+    """A storage resized to nothing, as sharded parameters have between uses,
+    is not the same as a tensor that was not given."""
+    a = Case(0)
+    first = a.run()
+    t = a.tensors()[which]
+    saved, n = t.clone(), t.untyped_storage().nbytes()
+    t.untyped_storage().resize_(0)
+    with pytest.raises((ValueError, nacl.NaclError), match="no memory|non-NULL"):
+        a.run()
+    t.untyped_storage().resize_(n)
+    t.copy_(saved)
+    assert all(torch.equal(x, y) for x, y in zip(a.run(), first))
+
+
 def test_the_problem_s_positions():
     n = 600
     pos = list(range(n - 256, n, 2))  # 128 of them: their positions are read on the device
