@@ -101,20 +101,20 @@ Plan plan_of(const nacl_problem* p, const nacl_step* s, const nacl_prefix* x) {
   a.own_blocks = (int)up(own_rows, a.own_rows);
   a.prefix_blocks = x ? (int)up(prefix_rows, a.prefix_rows) : 0;
   const int64_t own_blocks = (int64_t)p->B * p->H * a.own_blocks, prefix_blocks = (int64_t)groups * p->H * a.prefix_blocks;
-  // Chunks of about the same number of keys in both, as many as run together:
-  // three work-groups per CU of 16 rows (32 caches of 8256 rows: 188 us, two 207, four
-  // 197), two of 32 (3 caches of 5000 rows, 8 heads: 21.5 us, one 25; fp32, 32 rows of 8
-  // heads to 8000 keys beside 32 caches of 2000: 135 and 158) and of 16 beside a prefix
-  // read by tiles (whole calls with 40 caches of 300 rows: 35.8 us, three 37.0, one 36.6;
-  // 16 of 4000: 80.1, 81.3, 79.7; 48 of 1500: 63.0, 62.3, 70.0; from 64 of 2000 on within
-  // 0.3 % of each other), four of 128, as causal blocks differ in length (512 tokens, 64
-  // query heads over 8192 rows: 207 us, three 227).  Where most keys are a bf16 prefix's,
-  // one: fewer partial outputs to write and join (32 rows of 8 heads to 26214 keys: 26 us, two 30, three 35; 8 sequences, 32
-  // heads, a prefix of 6553 rows and 576 of their own: 33 us, three 35.5; but 32 caches
-  // of 4000 rows beside 8 prefixes of 2000: 123 us, three 115).  A prefix read by tiles
-  // has chunks of its own, one per CU (128 rows of 8 heads to 26214 keys: 40 us, two
-  // per CU 45; 64 rows 34.5 and 37) of at least 256 keys (128 rows of one head to
-  // 26214: 23 us, with 128 keys 26, with 512 26).
+  // Chunks of about the same number of keys in both, as many as run together: three
+  // work-groups per CU of 16 rows (32 caches of 8256 rows: 188 us, two 207, four 197), two of
+  // 32 (3 caches of 5000 rows, 8 heads: 21.5 us, one 25; fp32, 32 rows of 8 heads to 8000 keys
+  // beside 32 caches of 2000: 135 and 158) and of 16 beside a prefix read by tiles (whole
+  // calls with 40 caches of 300 rows: 35.8 us, three 37.0, one 36.6; 16 of 4000: 80.1, 81.3,
+  // 79.7; 48 of 1500: 63.0, 62.3, 70.0; 64 of 2000 and 128 of 1000 within 0.3 %), four
+  // of 128, as causal blocks differ in length (512 tokens, 64 query heads over 8192 rows: 207
+  // us, three 227).  Where most keys are a bf16 prefix's, one: fewer partial outputs to write
+  // and join (32 rows of 8 heads to 26214 keys: 26 us, two 30, three 35; 8 sequences, 32
+  // heads, a prefix of 6553 rows and 576 of their own: 33 us, three 35.5; but 32 caches of
+  // 4000 rows beside 8 prefixes of 2000: 123 us, three 115).  A prefix read by tiles has
+  // chunks of its own, one per CU (128 rows of 8 heads to 26214 keys: 40 us, two per CU 45; 64
+  // rows 34.5 and 37) of at least 256 keys (128 rows of one head to 26214: 23 us, with 128
+  // keys 26, with 512 26).
   const bool tiles = x && a.prefix_rows >= nacl::kPrefixTileRows;
   const int64_t own_keys = own_blocks * p->L, prefix_keys = prefix_blocks * a.Lp;
   const int64_t keys = own_keys + (tiles ? 0 : prefix_keys);
