@@ -384,6 +384,130 @@ size_t nacl_sample_workspace_bytes(const nacl_draw* d);
 int nacl_sample(const nacl_draw* d, const void* logits, const float* u, int32_t* tokens, float* logprobs, void* ws,
                 size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Decoding over a paged cache, and beam search.  Evicted sequences are of very
+ * different lengths and give rows back, so the caches of a batch can share a
+ * pool of pages instead of holding L rows each: a table names the pages of every
+ * sequence, row j of it being row j mod page of page table[b, j / page].  A step
+ * takes the pages that its new tokens need (nacl_pages_assign), writes the
+ * tokens into them (nacl_paged_append) and attends (nacl_paged_attention); where
+ * sequences are beams, the best continuations are picked (nacl_beam_select) and
+ * the beams take over what their parents hold (nacl_beam_reorder).
+ * The problem describes the caches as for the decoding step; L is the most rows
+ * that a sequence may hold, and the problem's k_stride and v_stride are validated
+ * and not used.
+ * ------------------------------------------------------------------------ */
+
+typedef struct nacl_pages {
+  int32_t n_pages, page;   /* pages of the pool and rows per page; n_pages * page below 2^31 */
+  int32_t entries;         /* pages per sequence that the table has room for */
+  int64_t table_stride;    /* elements between two sequences' entries, at least entries */
+  int64_t k_stride[3];     /* element strides of the pools for page, h, row; multiples of 16 bytes */
+  int64_t v_stride[3];
+  void* k;                 /* DEVICE [n_pages, H, page, D] of the problem's dtype, 16-byte aligned */
+  void* v;
+  int32_t* table;          /* DEVICE [B, entries] */
+} nacl_pages;
+
+/* Pages for a step's new tokens, and their slots.  Sequence b holds the first
+ * held[b] entries of its table row (clamped to [0, entries]) and needs
+ *   want[b] = ceil(min(L, row0 + lens[b] + min(T, n_new[b])) / page)   (at most entries; 0 below 0).
+ * The free pages are a stack, free [n_pages], of which the first n_free are in
+ * use.  First, entries want[b] .. held[b] - 1 of every sequence go back to it, in
+ * order of b and of the entry; those below shared[b] do not (pages that another
+ * sequence gives back).  Then sequences, in order, take want[b] - held[b]
+ * pages off its top where they hold fewer, each all of its pages or none: those
+ * whose pages, with those of the sequences before, are more than the stack
+ * has get none.  held_out[b] is want[b], or held[b] of a sequence that got none;
+ * table entries past it keep what they hold.  n_free_out: the pages left;
+ * missing (optional): the pages by which the stack fell short, 0 if none.
+ *   slots[b, t] = table[b, j / page] * page + j mod page,  j = row0 + lens[b] + t,
+ * and -1 for padding (t >= n_new[b]), for rows outside [0, L) and for rows without
+ * a page of the pool.  (A program that finds missing above 0 frees memory, by an
+ * eviction or by ending a sequence, and calls again with held_out and n_free_out.)
+ * x->k, x->v and their strides are not used.  held, held_out, shared (optional):
+ * int32 [B]; n_free, n_free_out, missing: int32 [1]; slots: int32 [B, T]; all
+ * DEVICE and contiguous.  held_out may be held and n_free_out n_free; what is
+ * written overlaps nothing else.  Nobody else may use the stack meanwhile. */
+int nacl_pages_assign(const nacl_problem* p, const nacl_step* s, const nacl_pages* x, const int32_t* held,
+                      const int32_t* shared, int32_t* free, const int32_t* n_free, int32_t* held_out,
+                      int32_t* n_free_out, int32_t* slots, int32_t* missing, void* stream);
+
+/* nacl_rotate_append into pages: token t of sequence b goes to row slots[b, t] mod
+ * page of page slots[b, t] / page.  slots: device int32 [B, T] contiguous; a
+ * slot outside [0, n_pages * page) joins no cache (q_out is written).  Tokens may
+ * not share slots.  The step's lens and row0, and the table, are not used.  The
+ * pools may be one buffer in which K and V take turns (by page, row or head), if
+ * their strides are the same. */
+int nacl_paged_append(const nacl_problem* p, const nacl_step* s, const nacl_rotation* r, const int32_t* positions,
+                      const void* q_new, const void* k_new, const void* v_new, const nacl_pages* x,
+                      const int32_t* slots, void* q_out, void* stream);
+
+/* Workspace bytes of nacl_paged_attention (0 on invalid input).  Device memory,
+ * 256-byte aligned; its contents need no initialisation. */
+size_t nacl_paged_workspace_bytes(const nacl_problem* p, const nacl_step* s, const nacl_pages* x);
+
+/* Attention of the step's queries to their sequence's pages: query row (b, hq, t)
+ * sees the rows j < row0 + lens[b] + t + 1 of its sequence, at most L and as far
+ * as the table goes (entries * page).  Rows of pages outside the pool (an entry
+ * that is not in [0, n_pages)) are not seen.  q, out, lse and the results are
+ * those of nacl_prefix_attention without a prefix, B * H * q_group * T below 2^26;
+ * pages may be shared by sequences, and hold anything in rows that are not seen. */
+int nacl_paged_attention(const nacl_problem* p, const nacl_step* s, const nacl_pages* x, const void* q, void* out,
+                         float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Beams of a group: B groups of W, whose logits are rows b * W + w. */
+typedef struct nacl_beams {
+  int32_t B, W;            /* 1 <= W <= NACL_MAX_W; B * W at most 65535 */
+  int32_t V, K;            /* tokens of the vocabulary, continuations wanted, 1 <= K <= NACL_MAX_W */
+  int32_t dtype;           /* nacl_dtype of the logits */
+  int64_t stride;          /* elements between rows, at least V */
+  int32_t end_token;       /* in [0, V): what an ended beam goes on with (unused without ended) */
+  const int32_t* ended;    /* optional DEVICE [B, W]: not 0 for a beam that has ended */
+} nacl_beams;
+#define NACL_MAX_W 64
+
+/* Workspace bytes of nacl_beam_select (0 on invalid input), the same for both
+ * dtypes.  Device memory, 256-byte aligned; its contents need no initialisation. */
+size_t nacl_beam_workspace_bytes(const nacl_beams* d);
+
+/* The best continuations of every group: of all beams w and tokens v the K largest
+ *   value(w, v) = scores[b, w] + x[b * W + w, v] - ln sum over u of exp x[b * W + w, u],
+ * largest first, equal ones by beam, then token.  An ended beam has one
+ * continuation, end_token, with its score as the value, and its logits are not
+ * read.  A beam whose score is infinite or NaN has none (so the first step of a
+ * search gives one beam a score and the others -infinity).  A NaN logit counts as
+ * -infinity, which has no continuation; infinite logits share a row
+ * evenly.  parents, tokens: device int32 [B, K]; out: device fp32 [B, K], the
+ * values (-infinity past fp32's range); where there are fewer than K, -1, -1 and
+ * -infinity follow.
+ * logits: device [B * W, V], element alignment; scores: device fp32 [B, W].
+ * Exponentials are fp32, their sums and the values fp64 in an order that V and the
+ * row's alignment fix.  V at most NACL_MAX_V, and W times the row's slices
+ * of 8192 tokens at most 1024 (about 2^23 tokens in a group). */
+int nacl_beam_select(const nacl_beams* d, const void* logits, const float* scores, int32_t* parents,
+                     int32_t* tokens, float* out, void* ws, size_t ws_bytes, void* stream);
+
+/* The beams of every group take over what their parents hold: B / W groups of W
+ * consecutive sequences (the problem's B); beam i of a group goes on from beam
+ * parents[group, i] of it.  The first beam of a parent takes its table row; every
+ * other one takes the table row of a beam without a child (in order), and the
+ * rows j < lens[parent] are copied into its pages where they differ from the
+ * parent's (pages that both hold, of a prompt that the group shares, are not
+ * touched).  A parent outside [0, W) is none: such a beam takes a table row that
+ * is left, and holds no rows.
+ * table_out [B, entries] (row stride out_stride, at least entries), lens_out [B]
+ * (the parent's length, at most L and what the pages hold), held_out [B] (of the
+ * table row taken; with held, else NULL): device int32, overlapping nothing else.
+ * lens, held: device int32 [B]; without held every row of the table is taken to be
+ * full.  A page that the beams of a group do not share belongs to one of them.
+ * Entries outside [0, n_pages) are passed over.  The calls of a model's layers
+ * differ in x->k and x->v alone; their tables come out the same.  The pools are as
+ * for nacl_paged_append.  Bit copies. */
+int nacl_beam_reorder(const nacl_problem* p, const nacl_pages* x, int32_t W, const int32_t* parents,
+                      const int32_t* lens, const int32_t* held, int32_t* table_out, int64_t out_stride,
+                      int32_t* lens_out, int32_t* held_out, void* stream);
+
 /* Static text for a status code. */
 const char* nacl_status_string(int status);
 

@@ -19,8 +19,8 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libnacl.so")
 ARCH = "gfx950"
 
-SOURCES = ["score.hip", "select.hip", "compact.hip", "attention.hip", "rotate.hip", "prefix.hip", "sample.hip",
-           "api.cpp", "step.cpp", "noalloc.hip"]
+SOURCES = ["score.hip", "select.hip", "compact.hip", "attention.hip", "rotate.hip", "prefix.hip", "sample.hip", "pages.hip", "beam.hip",
+           "api.cpp", "step.cpp", "paged.cpp", "noalloc.hip"]
 
 # Packed fp32 arithmetic stays off: the kernels are written for plain fp32
 # VALU ops.

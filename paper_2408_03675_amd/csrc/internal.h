@@ -242,6 +242,8 @@ struct RotateLaunch {
   void* q_out;
   void* k;
   void* v;
+  const int32_t* slots;          // [B, T] (paged: ks, vs are for page, h, row), or nullptr
+  int page, n_pages;
 };
 hipError_t launch_rotate_append(RotateLaunch a, int dtype, int D, int cus, hipStream_t stream);
 
@@ -272,8 +274,70 @@ struct PrefixLaunch {
   float* lse;                    // or nullptr
   float* part_o;                 // workspace [rows, prefix_split + own_split, D]
   float2* part_ml;               // workspace [rows, prefix_split + own_split]: maximum (base 2), sum
+  // Paged caches: ks, vs are for page, h, row.
+  const int32_t* table;          // [B, entries]
+  int64_t table_stride;
+  int page, n_pages;
+  uint32_t page_inv;             // (2^32 - 1) / page
 };
 hipError_t launch_prefix(const PrefixLaunch& a, int dtype, int D, hipStream_t stream);
+hipError_t launch_paged(const PrefixLaunch& a, int dtype, int D, hipStream_t stream);
+
+// Page tables and slots of a step (pages.hip).
+struct AssignLaunch {
+  int B, T, L, row0;
+  int page, n_pages, entries;
+  int64_t table_stride;
+  const int32_t* lens;           // [B] or nullptr
+  const int32_t* n_new;          // [B] or nullptr
+  const int32_t* shared;         // [B] or nullptr
+  const int32_t* held;
+  const int32_t* n_free;
+  int32_t* table;
+  int32_t* free;
+  int32_t* held_out;
+  int32_t* n_free_out;
+  int32_t* slots;
+  int32_t* missing;              // or nullptr
+};
+hipError_t launch_assign(const AssignLaunch& a, hipStream_t stream);
+
+// What beams hold, taken over from their parents (pages.hip).
+struct ReorderLaunch {
+  int groups, W, H, L;
+  int page, n_pages, entries;
+  int64_t table_stride, out_stride;
+  int64_t ks[3], vs[3];          // element strides for page, h, row
+  const int32_t* table;
+  const int32_t* parents;
+  const int32_t* lens;
+  const int32_t* held;           // or nullptr
+  int32_t* table_out;
+  int32_t* lens_out;
+  int32_t* held_out;             // or nullptr
+  void* k;
+  void* v;
+  int heads_per_item, wgs;       // set by the launcher
+};
+hipError_t launch_reorder(ReorderLaunch a, int dtype, int D, int cus, hipStream_t stream);
+
+// The best continuations of every group's beams (beam.hip).
+constexpr int kBeamSlice = 8192;   // tokens per work-group
+constexpr int kBeamLists = 1024;   // slices of a group's beams at most
+struct BeamLaunch {
+  int B, W, V, K, S;
+  int64_t stride;
+  const void* logits;
+  const float* scores;
+  const int32_t* ended;          // or nullptr
+  int end_token;
+  int32_t* parents;
+  int32_t* tokens;
+  float* out;
+  uint64_t* keys;                // workspace [B * W, S, K]
+  double* sums;                  // workspace [B * W, S, 2]: maximum, sum
+};
+hipError_t launch_beam(const BeamLaunch& a, int dtype, hipStream_t stream);
 
 // The next token of each row of logits (sample.hip).
 struct SampleLaunch {

@@ -1,6 +1,7 @@
 // Attention of a decoding step: the new tokens' queries against their own
 // sequence's cache and against a prefix that a group of sequences shares
-// (nacl_prefix_attention).
+// (nacl_prefix_attention), or against their sequence's pages
+// (nacl_paged_attention).
 //
 // The rows that read the same K and V are taken together: for the prefix the
 // queries of every sequence, query head and token of a group (rows of one K/V
@@ -83,6 +84,45 @@ __device__ __forceinline__ RowAt row_at(const PrefixLaunch& a, bool prefix, int 
   return r;
 }
 
+// Keys key0 .. key0 + N - 1 of a paged cache: lane i looks key key0 + i mod N up,
+// a tile ahead of the loads that need it, and gives its rows' places to the
+// lanes that load them.
+template <int N>
+struct PageTile {
+  int page = 0, row = 0;
+  bool in = false;
+  int64_t k = 0, v = 0;  // the key's row in the pools, in elements
+  uint64_t ok = 0;       // bit i: key key0 + i is there
+
+  // (A product with 2^32 / page, rounded down, is at most one short of j / page.)
+  static __device__ __forceinline__ int entry_of(const PrefixLaunch& a, int j) {
+    const int e = (int)__umulhi((uint32_t)j, a.page_inv);
+    return j - e * a.page >= a.page ? e + 1 : e;
+  }
+  __device__ __forceinline__ void lookup(const PrefixLaunch& a, const int32_t* table, int key0, int key_hi, int lane) {
+    const int j = key0 + (lane & (N - 1));
+    in = j < key_hi;
+    const int e = entry_of(a, in ? j : key_hi - 1);
+    row = j - e * a.page;
+    page = table[e];
+  }
+  // What lies past key_hi or in a page outside the pool is loaded from the pool's
+  // first row, and hidden.
+  __device__ __forceinline__ void resolve(const PrefixLaunch& a) {
+    const bool there = in && (uint32_t)page < (uint32_t)a.n_pages;
+    ok = __ballot(there);
+    if constexpr (N < 64) ok &= (1ull << N) - 1;
+    k = there ? (int64_t)page * a.ks[0] + (int64_t)row * a.ks[2] : 0;
+    v = there ? (int64_t)page * a.vs[0] + (int64_t)row * a.vs[2] : 0;
+  }
+  static constexpr uint64_t kAll = N < 64 ? (1ull << (N & 63)) - 1 : ~0ull;
+};
+__device__ __forceinline__ int64_t from_lane(int64_t x, int lane) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * lane, (int)(uint32_t)x);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * lane, (int)(uint32_t)(x >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
 // K, V and Q fragments by type.  Lane (g, r) = (lane / 16, lane mod 16).
 //
 // S^T = K Q^T, keys as MFMA rows: the lane holds logits of query r (keys 4 g ..
@@ -139,6 +179,37 @@ struct Frag<__bf16, D> {
           for (int c = 0; c < 2; ++c) vw[4 * e + i][c] = w[c];
         }
       }
+  }
+  // The same of a paged cache, the rows at k and v of the lanes that looked them up.
+  __device__ __forceinline__ void load_k(const __bf16* head, int64_t k, int g, int r) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const __bf16* p = head + from_lane(k, 16 * e + r) + 8 * g;
+#pragma unroll
+      for (int kb = 0; kb < kKb; ++kb) kf[e][kb] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(p + 32 * kb));
+    }
+  }
+  __device__ __forceinline__ void load_v(const __bf16* head, int64_t v, int g, int r) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const __bf16* p = head + from_lane(v, 16 * e + 4 * g + i) + r * kDt;
+        if constexpr (kDt == 8) {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) vw[4 * e + i][c] = w[c];
+        } else {
+          const u32x2 w = *reinterpret_cast<const u32x2*>(p);
+#pragma unroll
+          for (int c = 0; c < 2; ++c) vw[4 * e + i][c] = w[c];
+        }
+      }
+  }
+  __device__ __forceinline__ void zero_v(int e, int i) {
+#pragma unroll
+    for (int c = 0; c < kDt / 2; ++c) vw[4 * e + i][c] = 0;
   }
   // Logits of the tile: s[e][i] of key 16 e + 4 g + i.
   __device__ __forceinline__ void logits(const Query& q, f32x4 (&s)[2]) const {
@@ -232,6 +303,27 @@ struct Frag<float, D> {
 #pragma unroll
         for (int x = 0; x < 4; ++x) vw[i][4 * c + x] = w[x];
       }
+  }
+  __device__ __forceinline__ void load_k(const float* head, int64_t k, int g, int r) {
+    const float* p = head + from_lane(k, r) + 4 * g;
+#pragma unroll
+    for (int c = 0; c < kC; ++c) kf[c] = *reinterpret_cast<const f32x4*>(p + 16 * c);
+  }
+  __device__ __forceinline__ void load_v(const float* head, int64_t v, int g, int r) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float* p = head + from_lane(v, 4 * g + i) + r * kDt;
+#pragma unroll
+      for (int c = 0; c < kDt / 4; ++c) {
+        const f32x4 w = *reinterpret_cast<const f32x4*>(p + 4 * c);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) vw[i][4 * c + x] = w[x];
+      }
+    }
+  }
+  __device__ __forceinline__ void zero_v(int, int i) {
+#pragma unroll
+    for (int dt = 0; dt < kDt; ++dt) vw[i][dt] = 0.f;
   }
   __device__ __forceinline__ void logits(const Query& q, f32x4 (&s)[1]) const {
     f32x4 t = {0.f, 0.f, 0.f, 0.f};
@@ -335,14 +427,25 @@ __device__ __forceinline__ void put(const PrefixLaunch& a, const Item& it, const
 // infinite or NaN.  The matrix products above give a hidden key the probability
 // 0, which times such a value would still be NaN.  A wave per row: 64 keys at a
 // time, a lane each for the logits, then each lane D / 64 entries of the output.
-template <typename T, int D>
+template <typename T, int D, bool PAGED>
 __device__ __forceinline__ void odd_item(const PrefixLaunch& a, const Item& it) {
   constexpr int kPer = D / 64;
   const int lane = threadIdx.x & 63;
   const int64_t* ks = it.prefix ? a.pks : a.ks;
   const int64_t* vs = it.prefix ? a.pvs : a.vs;
-  const T* kh = reinterpret_cast<const T*>(it.prefix ? a.pk : a.k) + (int64_t)it.owner * ks[0] + (int64_t)it.h * ks[1];
-  const T* vh = reinterpret_cast<const T*>(it.prefix ? a.pv : a.v) + (int64_t)it.owner * vs[0] + (int64_t)it.h * vs[1];
+  const int64_t owner = PAGED ? 0 : it.owner;
+  const T* kh = reinterpret_cast<const T*>(it.prefix ? a.pk : a.k) + owner * ks[0] + (int64_t)it.h * ks[1];
+  const T* vh = reinterpret_cast<const T*>(it.prefix ? a.pv : a.v) + owner * vs[0] + (int64_t)it.h * vs[1];
+  // Key j's place; whether it is there.
+  auto place = [&](int j, const int64_t* st, int64_t& at) {
+    at = (int64_t)j * st[2];
+    if constexpr (PAGED) {
+      const int e = PageTile<64>::entry_of(a, j), page = a.table[(int64_t)it.owner * a.table_stride + e];
+      if ((uint32_t)page >= (uint32_t)a.n_pages) return false;
+      at = (int64_t)page * st[0] + (int64_t)(j - e * a.page) * st[2];
+    }
+    return true;
+  };
   for (int row = it.row0 + (threadIdx.x >> 6); row < it.row1; row += blockDim.x >> 6) {
     const RowAt x = row_at(a, it.prefix, it.owner, it.h, row);
     const T* q = query_of<T>(a, x);
@@ -352,9 +455,11 @@ __device__ __forceinline__ void odd_item(const PrefixLaunch& a, const Item& it) 
     for (int i = 0; i < kPer; ++i) o[i] = 0.f;
     for (int key0 = it.key_lo; key0 < end; key0 += 64) {
       float s = -INFINITY;
-      if (key0 + lane < end) {
+      int64_t at;
+      const bool there = key0 + lane < end && place(key0 + lane, ks, at);
+      if (there) {
         s = 0.f;
-        const T* k = kh + (int64_t)(key0 + lane) * ks[2];
+        const T* k = kh + at;
         for (int d = 0; d < D; ++d) s = __builtin_fmaf((float)k[d], (float)q[d], s);
       }
       float mn = s;
@@ -364,14 +469,15 @@ __device__ __forceinline__ void odd_item(const PrefixLaunch& a, const Item& it) 
       const float ref = mn == -INFINITY ? 0.f : mn;
       const float alpha = __builtin_amdgcn_exp2f(m - ref);
       m = mn;
-      const float p = key0 + lane < end ? __builtin_amdgcn_exp2f(__builtin_fmaf(s, a.c2, -ref)) : 0.f;
+      const float p = there ? __builtin_amdgcn_exp2f(__builtin_fmaf(s, a.c2, -ref)) : 0.f;
       l = l * alpha + p;
 #pragma unroll
       for (int i = 0; i < kPer; ++i) o[i] *= alpha;
       for (int j = 0; j < min(64, end - key0); ++j) {
         const float pj = __shfl(p, j);
+        if (!place(key0 + j, vs, at)) continue;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) o[i] = __builtin_fmaf(pj, (float)vh[(int64_t)(key0 + j) * vs[2] + kPer * lane + i], o[i]);
+        for (int i = 0; i < kPer; ++i) o[i] = __builtin_fmaf(pj, (float)vh[at + kPer * lane + i], o[i]);
       }
     }
 #pragma unroll
@@ -397,7 +503,7 @@ struct StreamShared {
   float m[kWaves][16 * R], l[kWaves][16 * R];
 };
 
-template <typename T, int D, int R>
+template <typename T, int D, int R, bool PAGED>
 __device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& it, StreamShared<D, R>& sh) {
   using F = Frag<T, D>;
   constexpr int kE = F::kKeys / 16, kDt = F::kDt;
@@ -422,10 +528,22 @@ __device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& i
   }
   plain = __all(plain);
 
-  const __amdgpu_buffer_rsrc_t kr = it.prefix ? rows_of<T>(a.pk, a.pks, it, key_hi) : rows_of<T>(a.k, a.ks, it, key_hi);
-  const __amdgpu_buffer_rsrc_t vr = it.prefix ? rows_of<T>(a.pv, a.pvs, it, key_hi) : rows_of<T>(a.v, a.vs, it, key_hi);
-  const uint32_t krow = (uint32_t)(it.prefix ? a.pks[2] : a.ks[2]) * sizeof(T);
-  const uint32_t vrow = (uint32_t)(it.prefix ? a.pvs[2] : a.vs[2]) * sizeof(T);
+  // Tiles of K and V: one head's rows, or its rows in the pages.
+  __amdgpu_buffer_rsrc_t kr, vr;
+  uint32_t krow, vrow;
+  const T *kh, *vh;
+  const int32_t* table;
+  PageTile<F::kKeys> pages;
+  if constexpr (PAGED) {
+    kh = reinterpret_cast<const T*>(a.k) + (int64_t)it.h * a.ks[1];
+    vh = reinterpret_cast<const T*>(a.v) + (int64_t)it.h * a.vs[1];
+    table = a.table + (int64_t)it.owner * a.table_stride;
+  } else {
+    kr = it.prefix ? rows_of<T>(a.pk, a.pks, it, key_hi) : rows_of<T>(a.k, a.ks, it, key_hi);
+    vr = it.prefix ? rows_of<T>(a.pv, a.pvs, it, key_hi) : rows_of<T>(a.v, a.vs, it, key_hi);
+    krow = (uint32_t)(it.prefix ? a.pks[2] : a.ks[2]) * sizeof(T);
+    vrow = (uint32_t)(it.prefix ? a.pvs[2] : a.vs[2]) * sizeof(T);
+  }
 
   f32x4 acc[R][kDt];
   float m[R], l[R];
@@ -438,27 +556,43 @@ __device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& i
   }
 
   F f;
+  auto load_k = [&](int key) {
+    if constexpr (PAGED) {
+      pages.resolve(a);
+      f.load_k(kh, pages.k, g, r);
+      pages.lookup(a, table, key + kWaves * F::kKeys, key_hi, lane);
+    } else {
+      f.load_k(kr, krow, key, g, r);
+    }
+  };
+  auto load_v = [&](int key) {
+    if constexpr (PAGED) f.load_v(vh, pages.v, g, r);
+    else f.load_v(vr, vrow, key, g, r);
+  };
   bool odd = false;  // an infinite or NaN value in a chunk that some rows see a part of
   int key0 = key_lo + wave * F::kKeys;
   if (key0 < key_hi) {
-    f.load_k(kr, krow, key0, g, r);
-    f.load_v(vr, vrow, key0, g, r);
+    if constexpr (PAGED) pages.lookup(a, table, key0, key_hi, lane);
+    load_k(key0);
+    load_v(key0);
   }
   for (; key0 < key_hi; key0 += kWaves * F::kKeys) {
     f32x4 s[R][kE];
 #pragma unroll
     for (int q = 0; q < R; ++q) f.logits(qf[q], s[q]);
     const int next = key0 + kWaves * F::kKeys;
-    if (next < key_hi) f.load_k(kr, krow, next, g, r);
+    const uint32_t ok = (uint32_t)pages.ok;  // of this tile
+    const bool whole = PAGED ? ok == (uint32_t)pages.kAll : key0 + F::kKeys <= key_hi;
+    if (next < key_hi) load_k(next);
 #pragma unroll
     for (int q = 0; q < R; ++q) {
-      if (!plain || key0 + F::kKeys > key_hi) {
+      if (!plain || !whole) {
         const int lim = limit[q] - key0 - 4 * g;
 #pragma unroll
         for (int e = 0; e < kE; ++e)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (16 * e + i >= lim) s[q][e][i] = -INFINITY;
+            if (16 * e + i >= lim || (PAGED && !(ok >> (16 * e + 4 * g + i) & 1))) s[q][e][i] = -INFINITY;
       }
       float mx = -INFINITY;
 #pragma unroll
@@ -484,6 +618,13 @@ __device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& i
         for (int dt = 0; dt < kDt; ++dt) acc[q][dt] *= alpha;
       }
     }
+    if (PAGED && !whole) {
+#pragma unroll
+      for (int e = 0; e < kE; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!(ok >> (16 * e + 4 * g + i) & 1)) f.zero_v(e, i);
+    }
     if (!plain) {
 #pragma unroll
       for (int e = 0; e < kE; ++e)
@@ -491,11 +632,11 @@ __device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& i
         for (int i = 0; i < 4; ++i) odd = odd || f.odd(e, i);
     }
     f.template value<R>(s, acc);
-    if (next < key_hi) f.load_v(vr, vrow, next, g, r);
+    if (next < key_hi) load_v(next);
   }
 
   if (!plain && __syncthreads_or(odd)) {
-    odd_item<T, D>(a, it);
+    odd_item<T, D, PAGED>(a, it);
     return;
   }
 
@@ -564,7 +705,7 @@ struct TileShared {
   unsigned char k[2][kTileKeys * D * 2], v[2][kTileKeys * D * 2];
 };
 
-template <int D, int ROWS>
+template <int D, int ROWS, bool PAGED>
 __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it, TileShared<D>& sh) {
   constexpr int kRowBytes = D * 2, kChunks = kRowBytes / 16;
   constexpr int kC = D / 16, kDt = D / 32;
@@ -590,9 +731,21 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
   const bool plain = __all(limit >= key_hi);
   const bool idle = it.row0 + 32 * wave >= it.row1;  // no row in this wave
 
-  const __amdgpu_buffer_rsrc_t kr = it.prefix ? rows_of<__bf16>(a.pk, a.pks, it, key_hi) : rows_of<__bf16>(a.k, a.ks, it, key_hi);
-  const __amdgpu_buffer_rsrc_t vr = it.prefix ? rows_of<__bf16>(a.pv, a.pvs, it, key_hi) : rows_of<__bf16>(a.v, a.vs, it, key_hi);
-  const uint32_t krow = (uint32_t)(it.prefix ? a.pks[2] : a.ks[2]) * 2, vrow = (uint32_t)(it.prefix ? a.pvs[2] : a.vs[2]) * 2;
+  __amdgpu_buffer_rsrc_t kr, vr;
+  uint32_t krow, vrow;
+  const __bf16 *kh, *vh;
+  const int32_t* table;
+  PageTile<kTileKeys> pages;
+  if constexpr (PAGED) {
+    kh = reinterpret_cast<const __bf16*>(a.k) + (int64_t)it.h * a.ks[1];
+    vh = reinterpret_cast<const __bf16*>(a.v) + (int64_t)it.h * a.vs[1];
+    table = a.table + (int64_t)it.owner * a.table_stride;
+  } else {
+    kr = it.prefix ? rows_of<__bf16>(a.pk, a.pks, it, key_hi) : rows_of<__bf16>(a.k, a.ks, it, key_hi);
+    vr = it.prefix ? rows_of<__bf16>(a.pv, a.pvs, it, key_hi) : rows_of<__bf16>(a.v, a.vs, it, key_hi);
+    krow = (uint32_t)(it.prefix ? a.pks[2] : a.ks[2]) * 2;
+    vrow = (uint32_t)(it.prefix ? a.pvs[2] : a.vs[2]) * 2;
+  }
 
   // Pieces of 16 bytes are permuted by row: the 16 rows of a K fragment's half and
   // the four rows by four pieces of a V fragment's fall on all 64 banks (two rows of
@@ -604,6 +757,22 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
   bool odd = false;  // as for few rows
   u32x4 kreg[kUnits], vreg[kUnits];
   auto load = [&](int key0) {
+    if constexpr (PAGED) {
+      pages.resolve(a);
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u) {
+        const int p = tid + kThreads * u, key = p / kChunks;
+        kreg[u] = *reinterpret_cast<const u32x4*>(kh + from_lane(pages.k, key) + p % kChunks * 8);
+        vreg[u] = *reinterpret_cast<const u32x4*>(vh + from_lane(pages.v, key) + p % kChunks * 8);
+      }
+      if (pages.ok != pages.kAll) {
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u)
+          if (!(pages.ok >> ((tid + kThreads * u) / kChunks) & 1)) vreg[u] = u32x4{0, 0, 0, 0};
+      }
+      pages.lookup(a, table, key0 + kTileKeys, key_hi, lane);
+      return;
+    }
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
       const int p = tid + kThreads * u;
@@ -659,6 +828,7 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
   float m = -INFINITY, l = 0.f;
 
   if (key_lo < key_hi) {
+    if constexpr (PAGED) pages.lookup(a, table, key_lo, key_hi, lane);
     load(key_lo);
     store(0);
   }
@@ -666,6 +836,8 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
     constexpr int buf = decltype(buf_c)::value;
     __syncthreads();
     const int next = key0 + kTileKeys;
+    const uint64_t ok = pages.ok;  // of this tile
+    const bool whole = PAGED ? ok == pages.kAll : next <= key_hi;
     if (next < key_hi) load(next);
     if (!idle) {
       f32x16 s[2];
@@ -689,14 +861,15 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
             s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[(c - kAhead) % (kAhead + 1)][kt], qf[c - kAhead], s[kt], 0, 0, 0);
         }
       }
-      if (!plain || next > key_hi) {
+      if (!plain || !whole) {
         asm volatile("");  // a branch: the comparisons cost as much as the exponentials' FMAs
         const int lim = limit - key0 - 4 * hl;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (32 * kt + 8 * (i / 4) + i % 4 >= lim) s[kt][i] = -INFINITY;
+            if (32 * kt + 8 * (i / 4) + i % 4 >= lim || (PAGED && !(ok >> (32 * kt + 8 * (i / 4) + i % 4 + 4 * hl) & 1)))
+              s[kt][i] = -INFINITY;
       }
       float mx = -INFINITY;
 #pragma unroll
@@ -744,7 +917,7 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
   }
 
   if (causal && __syncthreads_or(odd)) {
-    odd_item<__bf16, D>(a, it);
+    odd_item<__bf16, D, PAGED>(a, it);
     return;
   }
   auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
@@ -762,30 +935,34 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
 
 // What takes the prefix's items and the own caches' (rows per work-group: 16,
 // 32, 128 or 256).  The prefix's come first: they are the longer ones.
-template <typename T, int D, int ROWS>
+template <typename T, int D, int ROWS, bool PAGED>
 struct Part {
   using Shared = StreamShared<D, ROWS / 16>;
   static __device__ __forceinline__ void run(const PrefixLaunch& a, const Item& it, Shared& sh) {
-    stream_item<T, D, ROWS / 16>(a, it, sh);
+    stream_item<T, D, ROWS / 16, PAGED>(a, it, sh);
+  }
+};
+template <int D, bool PAGED>
+struct Part<__bf16, D, kTileRows, PAGED> {
+  using Shared = TileShared<D>;
+  static __device__ __forceinline__ void run(const PrefixLaunch& a, const Item& it, Shared& sh) {
+    tile_item<D, kTileRows, PAGED>(a, it, sh);
   }
 };
 template <int D>
-struct Part<__bf16, D, kTileRows> {
+struct Part<__bf16, D, kWideRows, false> {
   using Shared = TileShared<D>;
-  static __device__ __forceinline__ void run(const PrefixLaunch& a, const Item& it, Shared& sh) { tile_item<D, kTileRows>(a, it, sh); }
-};
-template <int D>
-struct Part<__bf16, D, kWideRows> {
-  using Shared = TileShared<D>;
-  static __device__ __forceinline__ void run(const PrefixLaunch& a, const Item& it, Shared& sh) { tile_item<D, kWideRows>(a, it, sh); }
+  static __device__ __forceinline__ void run(const PrefixLaunch& a, const Item& it, Shared& sh) {
+    tile_item<D, kWideRows, false>(a, it, sh);
+  }
 };
 constexpr int threads_of(int rows) { return rows >= kTileRows ? 2 * rows : kThreads; }
 
 // (0: none of them in this launch, so that the code of the other alone is there.)
-template <typename T, int D, int PREFIX, int OWN>
+template <typename T, int D, int PREFIX, int OWN, bool PAGED = false>
 __global__ __launch_bounds__(threads_of(PREFIX > OWN ? PREFIX : OWN), 2) void prefix_kernel(PrefixLaunch a) {
-  using P = Part<T, D, PREFIX ? PREFIX : OWN>;
-  using O = Part<T, D, OWN ? OWN : PREFIX>;
+  using P = Part<T, D, PREFIX ? PREFIX : OWN, PAGED>;
+  using O = Part<T, D, OWN ? OWN : PREFIX, PAGED>;
   union Shared {
     typename P::Shared p;
     typename O::Shared o;
@@ -914,6 +1091,27 @@ __global__ __launch_bounds__(kThreads) void prefix_merge_kernel(PrefixLaunch a) 
 }
 
 template <typename T, int D>
+hipError_t launch_merge(const PrefixLaunch& a, hipStream_t stream) {
+  if (a.direct) return hipSuccess;
+  const int64_t rows = (int64_t)a.B * a.H * a.G * a.T;
+  if (rows > 2048 || a.prefix_split + a.own_split <= kMergeBatch * (256 / D))
+    prefix_merge_kernel<T, D, 1><<<(unsigned)((rows + kWaves - 1) / kWaves), kThreads, 0, stream>>>(a);
+  else
+    prefix_merge_kernel<T, D, kWaves><<<(unsigned)rows, kThreads, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t launch_paged_t(const PrefixLaunch& a, hipStream_t stream) {
+  const unsigned groups = 8u * (unsigned)a.own_slots;
+  if (a.own_rows == 16) prefix_kernel<T, D, 0, 16, true><<<groups, kThreads, 0, stream>>>(a);
+  else if (a.own_rows == 32) prefix_kernel<T, D, 0, 32, true><<<groups, kThreads, 0, stream>>>(a);
+  else if constexpr (std::is_same_v<T, __bf16>) prefix_kernel<T, D, 0, kTileRows, true><<<groups, kThreads, 0, stream>>>(a);
+  if (hipError_t e = hipGetLastError()) return e;
+  return launch_merge<T, D>(a, stream);
+}
+
+template <typename T, int D>
 hipError_t launch_t(const PrefixLaunch& a, hipStream_t stream) {
   PrefixLaunch own = a;
   auto run = [&](auto kernel, const PrefixLaunch& x, int threads = kThreads) {
@@ -938,13 +1136,7 @@ hipError_t launch_t(const PrefixLaunch& a, hipStream_t stream) {
   else if (a.own_rows == 16 && own.prefix_slots && a.prefix_rows == 32) run(prefix_kernel<T, D, 32, 16>, own);
   else if (a.own_rows == 16) run(prefix_kernel<T, D, 16, 16>, own);
   if (hipError_t e = hipGetLastError()) return e;
-  if (a.direct) return hipSuccess;
-  const int64_t rows = (int64_t)a.B * a.H * a.G * a.T;
-  if (rows > 2048 || a.prefix_split + a.own_split <= kMergeBatch * (256 / D))
-    prefix_merge_kernel<T, D, 1><<<(unsigned)((rows + kWaves - 1) / kWaves), kThreads, 0, stream>>>(a);
-  else
-    prefix_merge_kernel<T, D, kWaves><<<(unsigned)rows, kThreads, 0, stream>>>(a);
-  return hipGetLastError();
+  return launch_merge<T, D>(a, stream);
 }
 
 }  // namespace
@@ -952,6 +1144,11 @@ hipError_t launch_t(const PrefixLaunch& a, hipStream_t stream) {
 hipError_t launch_prefix(const PrefixLaunch& a, int dtype, int D, hipStream_t stream) {
   if (dtype == NACL_F32) return D == 64 ? launch_t<float, 64>(a, stream) : launch_t<float, 128>(a, stream);
   return D == 64 ? launch_t<__bf16, 64>(a, stream) : launch_t<__bf16, 128>(a, stream);
+}
+
+hipError_t launch_paged(const PrefixLaunch& a, int dtype, int D, hipStream_t stream) {
+  if (dtype == NACL_F32) return D == 64 ? launch_paged_t<float, 64>(a, stream) : launch_paged_t<float, 128>(a, stream);
+  return D == 64 ? launch_paged_t<__bf16, 64>(a, stream) : launch_paged_t<__bf16, 128>(a, stream);
 }
 
 }  // namespace nacl

@@ -1,5 +1,5 @@
 // Queries and keys of new tokens, normalised per head and rotated by position,
-// into the cache (nacl_rotate_append).
+// into the cache (nacl_rotate_append) or its pages (nacl_paged_append).
 
 #include "device_common.h"
 #include "internal.h"
@@ -93,8 +93,18 @@ __global__ __launch_bounds__(kRotThreads) void rotate_append_kernel(RotateLaunch
   if (tok >= (int64_t)a.B * a.T) return;  // whole groups of kLanes lanes leave together
   const int b = (int)(tok / a.T), t = (int)(tok - (int64_t)b * a.T);
   if (a.n_new && t >= a.n_new[b]) return;
-  const int64_t row = (int64_t)a.row0 + (a.lens ? a.lens[b] : 0) + t;
-  const bool in_cache = row >= 0 && row < a.L;
+  // The token's place: a row of its sequence's cache, or of the page that its slot lies in.
+  int64_t row, owner = b;
+  bool in_cache;
+  if (a.slots) {
+    const int slot = a.slots[tok];
+    in_cache = slot >= 0 && slot < a.n_pages * a.page;
+    owner = slot / a.page;
+    row = slot - owner * a.page;
+  } else {
+    row = (int64_t)a.row0 + (a.lens ? a.lens[b] : 0) + t;
+    in_cache = row >= 0 && row < a.L;
+  }
 
   const bool rotated = 16 * j < a.rot;
   const bool halves = rotated && !a.interleaved;
@@ -125,8 +135,8 @@ __global__ __launch_bounds__(kRotThreads) void rotate_append_kernel(RotateLaunch
   const T* kn = reinterpret_cast<const T*>(a.k_new) + (int64_t)b * a.kns[0] + (int64_t)t * a.kns[2];
   const T* vn = reinterpret_cast<const T*>(a.v_new) + (int64_t)b * a.vns[0] + (int64_t)t * a.vns[2];
   T* qo = reinterpret_cast<T*>(a.q_out) + (int64_t)b * a.qos[0] + (int64_t)t * a.qos[2];
-  T* kc = reinterpret_cast<T*>(a.k) + (int64_t)b * a.ks[0] + row * a.ks[2];
-  T* vc = reinterpret_cast<T*>(a.v) + (int64_t)b * a.vs[0] + row * a.vs[2];
+  T* kc = reinterpret_cast<T*>(a.k) + owner * a.ks[0] + row * a.ks[2];
+  T* vc = reinterpret_cast<T*>(a.v) + owner * a.vs[0] + row * a.vs[2];
 
   for (int hb = h0; hb < h1; hb += kRotHeads) {
     Rot16<T> x[kRotHeads];

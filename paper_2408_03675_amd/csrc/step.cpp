@@ -1,5 +1,5 @@
-// C ABI of the decoding step between two evictions: argument validation,
-// the attention's plan and workspace, and the launches.
+// C ABI of the decoding step between two evictions: argument validation and the
+// launches.
 
 #include <hip/hip_runtime.h>
 
@@ -8,53 +8,11 @@
 
 #include "../../include/nacl.h"
 #include "internal.h"
+#include "step_common.h"
 
 namespace {
 
-using nacl::fail_status;
-
-constexpr int kPlanCus = 256;  // compute units the launches are planned for
-constexpr size_t kAlign = 256;
-size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
-int elt_bytes(int dtype) { return dtype == NACL_F32 ? 4 : 2; }
-int q_group_of(const nacl_problem* p) { return p->q_group > 1 ? p->q_group : 1; }
-
-// Bytes [lo, hi) that a strided tensor of n[0] x n[1] x n[2] rows of D spans.
-struct Extent {
-  uintptr_t lo = 0, hi = 0;
-  Extent(const void* base, const int64_t st[3], int64_t n0, int64_t n1, int64_t n2, int64_t D, int eb) {
-    lo = (uintptr_t)base;
-    hi = lo + (uintptr_t)((n0 - 1) * st[0] + (n1 - 1) * st[1] + (n2 - 1) * st[2] + D) * eb;
-  }
-  Extent(const void* base, uintptr_t bytes) : lo((uintptr_t)base), hi((uintptr_t)base + bytes) {}
-  bool meets(const Extent& o) const { return lo < o.hi && o.lo < hi; }
-};
-
-int check_strides(const char* name, const int64_t st[3], int eb) {
-  for (int i = 0; i < 3; ++i) {
-    if (st[i] < 0) return fail_status(NACL_ERR_INVALID_ARG, "%s[%d] < 0", name, i);
-    if (st[i] > ((int64_t)1 << 40)) return fail_status(NACL_ERR_UNSUPPORTED, "%s[%d] exceeds 2^40", name, i);
-    if ((st[i] * eb) % 16)
-      return fail_status(NACL_ERR_INVALID_ARG, "%s[%d] * element size must be a multiple of 16 bytes", name, i);
-  }
-  return NACL_OK;
-}
-
-// The problem and the parts of a step that both calls read.
-int check_step(const nacl_problem* p, const nacl_step* s) {
-  int st = nacl::validate_problem(p);
-  if (st) return st;
-  if (!s) return fail_status(NACL_ERR_INVALID_ARG, "step is NULL");
-  if (s->T < 1) return fail_status(NACL_ERR_INVALID_ARG, "T must be >= 1 (got %d)", s->T);
-  if (s->T > NACL_MAX_L) return fail_status(NACL_ERR_UNSUPPORTED, "T = %d exceeds %d", s->T, NACL_MAX_L);
-  if (s->row0 < 0) return fail_status(NACL_ERR_INVALID_ARG, "row0 must be >= 0 (got %d)", s->row0);
-  if ((int64_t)p->B * s->T >= (int64_t)1 << 28)
-    return fail_status(NACL_ERR_UNSUPPORTED, "B * T reaches 2^28");
-  if (!aligned(s->lens, 4) || !aligned(s->n_new, 4))
-    return fail_status(NACL_ERR_INVALID_ARG, "lens and n_new must be 4-byte aligned");
-  return check_strides("the step's q_stride", s->q_stride, elt_bytes(p->dtype));
-}
+using namespace nacl;
 
 int check_prefix(const nacl_problem* p, const nacl_prefix* x) {
   if (!x) return NACL_OK;
@@ -65,80 +23,6 @@ int check_prefix(const nacl_problem* p, const nacl_prefix* x) {
   const int eb = elt_bytes(p->dtype);
   if (int st = check_strides("the prefix's k_stride", x->k_stride, eb)) return st;
   return check_strides("the prefix's v_stride", x->v_stride, eb);
-}
-
-// How the attention's rows and keys are shared out.  It depends on sizes only:
-// the lengths are on the device, where each row block's keys are dealt to at
-// most n_split chunks.
-struct Plan {
-  int per_group = 1, Lp = 0;
-  int prefix_rows = 16, own_rows = 16;
-  int prefix_blocks = 0, prefix_split = 0, own_blocks = 0, own_split = 0;
-  int64_t prefix_units = 0, prefix_slots = 0, own_units = 0, own_slots = 0, rows = 0;
-  bool direct = false;
-  size_t ml = 0, total = 0;  // byte offset of part_ml, workspace bytes
-};
-
-Plan plan_of(const nacl_problem* p, const nacl_step* s, const nacl_prefix* x) {
-  Plan a;
-  const int G = q_group_of(p);
-  const int groups = x ? x->G : 1;
-  a.per_group = p->B / groups;
-  a.Lp = x ? x->L : 0;
-  a.rows = (int64_t)p->B * p->H * G * s->T;
-  const int64_t own_rows = (int64_t)G * s->T, prefix_rows = own_rows * a.per_group;
-  auto block = [&](int64_t rows) {
-    return rows <= 16 ? 16 : rows <= 32 || p->dtype == NACL_F32 ? 32 : nacl::kPrefixTileRows;
-  };
-  a.own_rows = block(own_rows);
-  a.prefix_rows = x ? block(prefix_rows) : a.own_rows;
-  // Of a prefix 256 rows share a tile where there are as many: half the reads per
-  // row (8 heads, 26214 keys: 512 rows 89 us, by tiles of 128 97, 2048 rows 246 and
-  // 271, 256 rows 54 and 58, 160 rows 43 and 48).  Not of the own caches, whose work-groups are fewer (4 caches of
-  // 4096 rows, 8 heads, 256 rows: 54 us, by 256 rows 83).
-  if (x && a.prefix_rows == nacl::kPrefixTileRows && prefix_rows > nacl::kPrefixTileRows) a.prefix_rows = nacl::kPrefixWideRows;
-  auto up = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
-  a.own_blocks = (int)up(own_rows, a.own_rows);
-  a.prefix_blocks = x ? (int)up(prefix_rows, a.prefix_rows) : 0;
-  const int64_t own_blocks = (int64_t)p->B * p->H * a.own_blocks, prefix_blocks = (int64_t)groups * p->H * a.prefix_blocks;
-  // Chunks of about the same number of keys in both, as many as run together: three
-  // work-groups per CU of 16 rows (32 caches of 8256 rows: 188 us, two 207, four 197), two of
-  // 32 (3 caches of 5000 rows, 8 heads: 21.5 us, one 25; fp32, 32 rows of 8 heads to 8000 keys
-  // beside 32 caches of 2000: 135 and 158) and of 16 beside a prefix read by tiles (whole
-  // calls with 40 caches of 300 rows: 35.8 us, three 37.0, one 36.6; 16 of 4000: 80.1, 81.3,
-  // 79.7; 48 of 1500: 63.0, 62.3, 70.0; 64 of 2000 and 128 of 1000 within 0.3 %), four
-  // of 128, as causal blocks differ in length (512 tokens, 64 query heads over 8192 rows: 207
-  // us, three 227).  Where most keys are a bf16 prefix's, one: fewer partial outputs to write
-  // and join (32 rows of 8 heads to 26214 keys: 26 us, two 30, three 35; 8 sequences, 32
-  // heads, a prefix of 6553 rows and 576 of their own: 33 us, three 35.5; but 32 caches of
-  // 4000 rows beside 8 prefixes of 2000: 123 us, three 115).  A prefix read by tiles has
-  // chunks of its own, one per CU (128 rows of 8 heads to 26214 keys: 40 us, two per CU 45; 64
-  // rows 34.5 and 37) of at least 256 keys (128 rows of one head to 26214: 23 us, with 128
-  // keys 26, with 512 26).
-  const bool tiles = x && a.prefix_rows >= nacl::kPrefixTileRows;
-  const int64_t own_keys = own_blocks * p->L, prefix_keys = prefix_blocks * a.Lp;
-  const int64_t keys = own_keys + (tiles ? 0 : prefix_keys);
-  const bool mostly_prefix = !tiles && p->dtype == NACL_BF16 && prefix_keys >= own_keys;
-  const int per_cu = a.own_rows == nacl::kPrefixTileRows ? 4 : mostly_prefix ? 1 : tiles || a.own_rows == 32 || a.prefix_rows == 32 ? 2 : 3;
-  const int64_t chunk = std::max<int64_t>(nacl::kPrefixMinChunk, up(keys, per_cu * kPlanCus));
-  a.own_split = (int)up(p->L, chunk);
-  a.prefix_split = (int)up(a.Lp, tiles ? std::max<int64_t>(256, up(prefix_keys, kPlanCus)) : chunk);
-  a.own_units = (int64_t)p->B * p->H * a.own_split;
-  a.prefix_units = x ? (int64_t)groups * p->H * a.prefix_split : 0;
-  a.own_slots = up(a.own_units, 8) * a.own_blocks;
-  a.prefix_slots = up(a.prefix_units, 8) * a.prefix_blocks;
-  a.direct = !x && a.own_split == 1;
-  const size_t slots = a.direct ? 0 : (size_t)a.rows * (a.own_split + a.prefix_split);
-  a.ml = align_up(slots * p->D * sizeof(float));
-  a.total = a.ml + align_up(std::max<size_t>(slots * sizeof(float2), 1));
-  return a;
-}
-
-int check_planned(const Plan& a) {
-  if (a.rows >= (int64_t)1 << 26) return fail_status(NACL_ERR_UNSUPPORTED, "B * H * q_group * T reaches 2^26");
-  if (8 * (a.own_slots + a.prefix_slots) >= (int64_t)1 << 24)
-    return fail_status(NACL_ERR_UNSUPPORTED, "%lld work-groups, at most 2^24", (long long)(8 * (a.own_slots + a.prefix_slots)));
-  return NACL_OK;
 }
 
 int check_draw(const nacl_draw* d) {
@@ -154,28 +38,12 @@ int check_draw(const nacl_draw* d) {
   return NACL_OK;
 }
 
-int check_workspace(const void* ws, size_t ws_bytes, size_t need) {
-  if (ws_bytes < need) return fail_status(NACL_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", ws_bytes, need);
-  if (!ws) return fail_status(NACL_ERR_WORKSPACE, "workspace is NULL");
-  if (!aligned(ws, kAlign)) return fail_status(NACL_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-  return NACL_OK;
-}
-
-int launched(hipError_t e, const char* what) {
-  return e == hipSuccess ? (int)NACL_OK : fail_status(NACL_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-}
-
-}  // namespace
-
-extern "C" {
-
-int nacl_rotate_append(const nacl_problem* p, const nacl_step* s, const nacl_rotation* r, const int32_t* positions,
-                       const void* q_new, const void* k_new, const void* v_new, void* q_out, void* k, void* v,
-                       void* stream) {
-  nacl::clear_detail();
+// What the two forms of the rotation into a cache have in common.
+int check_rotate(const nacl_problem* p, const nacl_step* s, const nacl_rotation* r, const int32_t* positions,
+                 const void* q_new, const void* k_new, const void* v_new, const void* q_out, const void* k, const void* v) {
   int st = check_step(p, s);
   if (st) return st;
-  const int eb = elt_bytes(p->dtype), G = q_group_of(p);
+  const int eb = elt_bytes(p->dtype);
   if ((st = check_strides("the step's k_stride", s->k_stride, eb))) return st;
   if ((st = check_strides("the step's v_stride", s->v_stride, eb))) return st;
   if ((st = check_strides("the step's q_out_stride", s->q_out_stride, eb))) return st;
@@ -191,15 +59,19 @@ int nacl_rotate_append(const nacl_problem* p, const nacl_step* s, const nacl_rot
     return fail_status(NACL_ERR_INVALID_ARG, "inv_freq and positions must be 4-byte aligned");
   if (!q_new || !k_new || !v_new || !q_out || !k || !v)
     return fail_status(NACL_ERR_INVALID_ARG, "q_new, k_new, v_new, q_out, k and v must be non-NULL");
-  for (const void* t : {q_new, k_new, v_new, (const void*)q_out, (const void*)k, (const void*)v, r->q_weight, r->k_weight})
+  for (const void* t : {q_new, k_new, v_new, q_out, k, v, r->q_weight, r->k_weight})
     if (!aligned(t, 16)) return fail_status(NACL_ERR_INVALID_ARG, "tensors must be 16-byte aligned");
-  // What is written: q_out (or q_new itself), K and V.
-  const int Hq = p->H * G;
-  const Extent kc(k, p->k_stride, p->B, p->H, p->L, p->D, eb), vc(v, p->v_stride, p->B, p->H, p->L, p->D, eb);
+  return NACL_OK;
+}
+
+// That what is written (q_out, or q_new itself, and the cache's kc and vc) lies apart
+// from what is read, and q_out's rows from each other.
+int check_rotate_apart(const nacl_problem* p, const nacl_step* s, const void* q_new, const void* k_new,
+                       const void* v_new, const void* q_out, const Extent& kc, const Extent& vc) {
+  const int eb = elt_bytes(p->dtype), Hq = p->H * q_group_of(p);
   const Extent qn(q_new, s->q_stride, p->B, Hq, s->T, p->D, eb), kn(k_new, s->k_stride, p->B, p->H, s->T, p->D, eb);
   const Extent vn(v_new, s->v_stride, p->B, p->H, s->T, p->D, eb);
   const Extent qo(q_out, s->q_out_stride, p->B, Hq, s->T, p->D, eb);
-  if (kc.meets(vc)) return fail_status(NACL_ERR_INVALID_ARG, "K and V overlap");
   for (const Extent* t : {&qn, &kn, &vn, &qo})
     if (t->meets(kc) || t->meets(vc)) return fail_status(NACL_ERR_INVALID_ARG, "the new tokens or q_out overlap the cache");
   const bool in_place = q_out == q_new;
@@ -212,19 +84,19 @@ int nacl_rotate_append(const nacl_problem* p, const nacl_step* s, const nacl_rot
   } else if (qo.meets(qn) || qo.meets(kn) || qo.meets(vn)) {
     return fail_status(NACL_ERR_INVALID_ARG, "q_out overlaps the new tokens");
   }
-  // Rows of what is written lie apart.
   const int64_t dims[3] = {p->B, Hq, s->T};
   for (int i = 0; i < 3; ++i)
     if (dims[i] > 1 && s->q_out_stride[i] < p->D)
       return fail_status(NACL_ERR_INVALID_ARG, "q_out_stride[%d] must be at least D", i);
-  const int64_t cache_dims[3] = {p->B, p->H, p->L};
-  for (int i = 0; i < 3; ++i)
-    if (cache_dims[i] > 1 && (p->k_stride[i] < p->D || p->v_stride[i] < p->D))
-      return fail_status(NACL_ERR_INVALID_ARG, "K and V need strides of at least D (k_stride, v_stride [%d])", i);
+  return NACL_OK;
+}
+
+nacl::RotateLaunch rotate_launch(const nacl_problem* p, const nacl_step* s, const nacl_rotation* r, const int32_t* positions,
+                                 const void* q_new, const void* k_new, const void* v_new, void* q_out) {
   nacl::RotateLaunch a{};
   a.B = p->B;
   a.H = p->H;
-  a.G = G;
+  a.G = q_group_of(p);
   a.T = s->T;
   a.L = p->L;
   a.row0 = s->row0;
@@ -236,8 +108,6 @@ int nacl_rotate_append(const nacl_problem* p, const nacl_step* s, const nacl_rot
     a.kns[i] = s->k_stride[i];
     a.vns[i] = s->v_stride[i];
     a.qos[i] = s->q_out_stride[i];
-    a.ks[i] = p->k_stride[i];
-    a.vs[i] = p->v_stride[i];
   }
   a.pos_stride = r->pos_stride;
   a.lens = s->lens;
@@ -250,8 +120,58 @@ int nacl_rotate_append(const nacl_problem* p, const nacl_step* s, const nacl_rot
   a.k_new = k_new;
   a.v_new = v_new;
   a.q_out = q_out;
+  return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+int nacl_rotate_append(const nacl_problem* p, const nacl_step* s, const nacl_rotation* r, const int32_t* positions,
+                       const void* q_new, const void* k_new, const void* v_new, void* q_out, void* k, void* v,
+                       void* stream) {
+  nacl::clear_detail();
+  int st = check_rotate(p, s, r, positions, q_new, k_new, v_new, q_out, k, v);
+  if (st) return st;
+  const int eb = elt_bytes(p->dtype);
+  const Extent kc(k, p->k_stride, p->B, p->H, p->L, p->D, eb), vc(v, p->v_stride, p->B, p->H, p->L, p->D, eb);
+  if (kc.meets(vc)) return fail_status(NACL_ERR_INVALID_ARG, "K and V overlap");
+  if ((st = check_rotate_apart(p, s, q_new, k_new, v_new, q_out, kc, vc))) return st;
+  const int64_t cache_dims[3] = {p->B, p->H, p->L};
+  for (int i = 0; i < 3; ++i)
+    if (cache_dims[i] > 1 && (p->k_stride[i] < p->D || p->v_stride[i] < p->D))
+      return fail_status(NACL_ERR_INVALID_ARG, "K and V need strides of at least D (k_stride, v_stride [%d])", i);
+  nacl::RotateLaunch a = rotate_launch(p, s, r, positions, q_new, k_new, v_new, q_out);
+  for (int i = 0; i < 3; ++i) {
+    a.ks[i] = p->k_stride[i];
+    a.vs[i] = p->v_stride[i];
+  }
   a.k = k;
   a.v = v;
+  return launched(nacl::launch_rotate_append(a, p->dtype, p->D, kPlanCus, static_cast<hipStream_t>(stream)), "rotate kernel");
+}
+
+int nacl_paged_append(const nacl_problem* p, const nacl_step* s, const nacl_rotation* r, const int32_t* positions,
+                      const void* q_new, const void* k_new, const void* v_new, const nacl_pages* x,
+                      const int32_t* slots, void* q_out, void* stream) {
+  nacl::clear_detail();
+  if (!x) return fail_status(NACL_ERR_INVALID_ARG, "pages are NULL");
+  int st = check_rotate(p, s, r, positions, q_new, k_new, v_new, q_out, x->k, x->v);
+  if (st) return st;
+  if ((st = check_pages(p, x)) || (st = check_pool(p, x)) || (st = check_pool_apart(p, x))) return st;
+  if (!slots || !aligned(slots, 4)) return fail_status(NACL_ERR_INVALID_ARG, "slots must be non-NULL and 4-byte aligned");
+  const Extent kc = pool_extent(p, x, x->k, x->k_stride), vc = pool_extent(p, x, x->v, x->v_stride);
+  if ((st = check_rotate_apart(p, s, q_new, k_new, v_new, q_out, kc, vc))) return st;
+  nacl::RotateLaunch a = rotate_launch(p, s, r, positions, q_new, k_new, v_new, q_out);
+  for (int i = 0; i < 3; ++i) {
+    a.ks[i] = x->k_stride[i];
+    a.vs[i] = x->v_stride[i];
+  }
+  a.k = x->k;
+  a.v = x->v;
+  a.slots = slots;
+  a.page = x->page;
+  a.n_pages = x->n_pages;
   return launched(nacl::launch_rotate_append(a, p->dtype, p->D, kPlanCus, static_cast<hipStream_t>(stream)), "rotate kernel");
 }
 

@@ -30,7 +30,9 @@ SAMPLE_UNIFORM = 2
 EXPORTED = ("nacl_workspace_bytes", "nacl_score", "nacl_select", "nacl_compact", "nacl_compact_slots",
             "nacl_append", "nacl_evict", "nacl_evict_slots", "nacl_evict_noalloc", "nacl_attention",
             "nacl_rotate_append", "nacl_prefix_workspace_bytes", "nacl_prefix_attention",
-            "nacl_sample_workspace_bytes", "nacl_sample", "nacl_status_string",
+            "nacl_sample_workspace_bytes", "nacl_sample", "nacl_pages_assign", "nacl_paged_append",
+            "nacl_paged_workspace_bytes", "nacl_paged_attention", "nacl_beam_workspace_bytes", "nacl_beam_select",
+            "nacl_beam_reorder", "nacl_status_string",
             "nacl_last_error_detail", "nacl_version")
 
 
@@ -85,6 +87,21 @@ class _Draw(ctypes.Structure):
     ]
 
 
+class _Pages(ctypes.Structure):
+    _fields_ = [
+        ("n_pages", ctypes.c_int32), ("page", ctypes.c_int32), ("entries", ctypes.c_int32),
+        ("table_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3),
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("table", ctypes.c_void_p),
+    ]
+
+
+class _Beams(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("W", ctypes.c_int32), ("V", ctypes.c_int32), ("K", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("stride", ctypes.c_int64), ("end_token", ctypes.c_int32), ("ended", ctypes.c_void_p),
+    ]
+
+
 _lib = None
 
 
@@ -129,6 +146,21 @@ def load_library(path=LIB_PATH):
     lib.nacl_sample_workspace_bytes.restype = sz
     lib.nacl_sample.argtypes = [W, vp, vp, vp, vp, vp, sz, vp]
     lib.nacl_sample.restype = ctypes.c_int
+    G, M = ctypes.POINTER(_Pages), ctypes.POINTER(_Beams)
+    lib.nacl_pages_assign.argtypes = [P, S, G] + [vp] * 9
+    lib.nacl_pages_assign.restype = ctypes.c_int
+    lib.nacl_paged_append.argtypes = [P, S, R, vp, vp, vp, vp, G, vp, vp, vp]
+    lib.nacl_paged_append.restype = ctypes.c_int
+    lib.nacl_paged_workspace_bytes.argtypes = [P, S, G]
+    lib.nacl_paged_workspace_bytes.restype = sz
+    lib.nacl_paged_attention.argtypes = [P, S, G, vp, vp, vp, vp, sz, vp]
+    lib.nacl_paged_attention.restype = ctypes.c_int
+    lib.nacl_beam_workspace_bytes.argtypes = [M]
+    lib.nacl_beam_workspace_bytes.restype = sz
+    lib.nacl_beam_select.argtypes = [M, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.nacl_beam_select.restype = ctypes.c_int
+    lib.nacl_beam_reorder.argtypes = [P, G, i32, vp, vp, vp, vp, ctypes.c_int64, vp, vp, vp]
+    lib.nacl_beam_reorder.restype = ctypes.c_int
     lib.nacl_status_string.argtypes = [ctypes.c_int]
     lib.nacl_status_string.restype = ctypes.c_char_p
     lib.nacl_last_error_detail.argtypes = []
@@ -694,6 +726,20 @@ class Prefix(_Keeper):
         self._keep(k, v, lens)
 
 
+def _rotation(prob, step, rotation, positions, dev):
+    """The call's nacl_rotation and its positions' address."""
+    if rotation.fits != step.fits[1:]:
+        raise ValueError("the rotation was made for another head size or dtype")
+    rotation.current()
+    if rotation.dev is not None and rotation.dev != dev:
+        raise ValueError(f"the rotation's tensors are on {rotation.dev}, the call runs on {dev}")
+    if positions is None:
+        return rotation.with_stride(0), None
+    per_row = positions.dim() == 2
+    _like(positions, "positions", dev, (prob.B, step.T) if per_row else (step.T,), torch.int32)
+    return rotation.with_stride(step.T if per_row else 0), positions.data_ptr()
+
+
 def rotate_append(prob, step, rotation, positions, q_new, k_new, v_new, k, v, q_out=None):
     """The new tokens' queries and keys normalised and rotated, keys and values
     written into the cache k, v (include/nacl.h: nacl_rotate_append).  q_new
@@ -705,22 +751,12 @@ def rotate_append(prob, step, rotation, positions, q_new, k_new, v_new, k, v, q_
     _cache(k, "k", dev, step, step.k_stride)
     _cache(v, "v", dev, step, step.v_stride)
     step.on(prob, dev)
-    if rotation.fits != step.fits[1:]:
-        raise ValueError("the rotation was made for another head size or dtype")
-    rotation.current()
-    if rotation.dev is not None and rotation.dev != dev:
-        raise ValueError(f"the rotation's tensors are on {rotation.dev}, the call runs on {dev}")
+    r, pos = _rotation(prob, step, rotation, positions, dev)
     dt = step.dtype
     if q_out is None:
         q_out = torch.empty(step.q_shape, dtype=dt, device=dev)
     s = step.strided(_rows4(q_new, "q_new", dev, step.q_shape, dt), _rows4(k_new, "k_new", dev, step.new_shape, dt),
                      _rows4(v_new, "v_new", dev, step.new_shape, dt), _rows4(q_out, "q_out", dev, step.q_shape, dt))
-    pos = None
-    if positions is not None:
-        per_row = positions.dim() == 2
-        _like(positions, "positions", dev, (prob.B, step.T) if per_row else (step.T,), torch.int32)
-        pos = positions.data_ptr()
-    r = rotation.with_stride(step.T if pos is not None and per_row else 0)
     _launch(dev, lib.nacl_rotate_append, prob.ref(), s, r, pos, q_new.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
             q_out.data_ptr(), k.data_ptr(), v.data_ptr())
     return q_out
@@ -841,3 +877,245 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, toke
     _launch(dev, lib.nacl_sample, d, logits.data_ptr(), u.data_ptr(), tokens.data_ptr(),
             None if logprobs is None else logprobs.data_ptr(), ws.data_ptr(), n)
     return tokens, logprobs
+
+
+# Decoding over a paged cache, and beam search.
+
+def _table(t, name, dev, rows, entries=None):
+    """A [B, entries] int32 table, rows of any stride; its row stride."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise ValueError(f"{name} must be [B, entries]")
+    _gpu(t, name, dev, (rows, t.shape[1] if entries is None else entries), torch.int32)
+    stride, one = t.stride()
+    if t.shape[1] > 1 and one != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return stride if rows > 1 else max(stride, t.shape[1])
+
+
+class Pages(_Keeper):
+    """nacl_pages: the pools k, v [n_pages, H, page, D] of any strides, whose pages
+    the table, int32 [B, entries], deals to the problem's sequences."""
+
+    def __init__(self, prob, k, v, table):
+        self.prob, self.k, self.v, self.table = prob, k, v, table
+        self._take()
+
+    def _take(self):
+        prob, k, v, table = self.prob, self.k, self.v, self.table
+        if not isinstance(k, torch.Tensor) or k.dim() != 4:
+            raise ValueError("the pages' k must be [n_pages, H, page, D]")
+        n, _, page, _ = k.shape
+        if max(n, page) >= 2 ** 31:
+            raise ValueError("pages and their rows must fit 32 bits")
+        x = _Pages()
+        x.n_pages, x.page = n, page
+        dev = _gpu(k, "the pages' k", k.device).device
+        shape = (n, prob.H, page, prob.D)
+        x.k_stride[:] = _rows4(k, "the pages' k", dev, shape, prob.torch_dtype)[:3]
+        x.v_stride[:] = _rows4(v, "the pages' v", dev, shape, prob.torch_dtype)[:3]
+        x.table_stride = _table(table, "the table", dev, prob.B)
+        if table.shape[1] >= 2 ** 31:
+            raise ValueError("the table's entries must fit 32 bits")
+        x.entries = table.shape[1]
+        x.k, x.v, x.table = k.data_ptr(), v.data_ptr(), table.data_ptr()
+        self.c, self.dev = x, dev
+        self._keep(k, v, table)
+
+    def on(self, prob):
+        if prob is not self.prob:
+            raise ValueError("the pages were made for another problem")
+        self.current()
+        return self.dev
+
+
+def pages_assign(step, page, table, held, free, n_free, shared=None, held_out=None, n_free_out=None, slots=None,
+                 missing=None):
+    """Pages of `page` rows for the step's new tokens, and their slots (include/nacl.h:
+    nacl_pages_assign).  table int32 [B, entries] and the stack free int32
+    [n_pages] are updated in place; held, shared int32 [B], n_free int32 [1].
+    Returns (held_out [B], n_free_out [1], slots [B, T], missing [1]), new tensors
+    or the given ones; held_out may be held and n_free_out n_free."""
+    lib = _lib or load_library()
+    prob = step.prob
+    dev = getattr(table, "device", None)
+    x = _Pages()
+    x.table_stride = _table(table, "table", dev, prob.B)
+    step.on(prob, dev)
+    if not isinstance(free, torch.Tensor) or free.dim() != 1:
+        raise ValueError("free must be [n_pages]")
+    if not 0 <= max(int(page), free.shape[0], table.shape[1]) < 2 ** 31 or int(page) < 0:
+        raise ValueError("pages, their rows and the table's entries must fit 32 bits")
+    x.n_pages, x.page, x.entries, x.table = free.shape[0], int(page), table.shape[1], table.data_ptr()
+    rows, one = (prob.B,), (1,)
+    _like(free, "free", dev, free.shape, torch.int32)
+    _like(held, "held", dev, rows, torch.int32)
+    _like(n_free, "n_free", dev, one, torch.int32)
+    if shared is not None:
+        _like(shared, "shared", dev, rows, torch.int32)
+    outs = []
+    for t, name, shape in ((held_out, "held_out", rows), (n_free_out, "n_free_out", one), (slots, "slots", (prob.B, step.T)),
+                           (missing, "missing", one)):
+        if t is None:
+            t = torch.empty(shape, dtype=torch.int32, device=dev)
+        else:
+            _like(t, name, dev, shape, torch.int32)
+        outs.append(t)
+    held_out, n_free_out, slots, missing = outs
+    _launch(dev, lib.nacl_pages_assign, prob.ref(), step.c, x, held.data_ptr(), None if shared is None else shared.data_ptr(),
+            free.data_ptr(), n_free.data_ptr(), held_out.data_ptr(), n_free_out.data_ptr(), slots.data_ptr(),
+            missing.data_ptr())
+    return held_out, n_free_out, slots, missing
+
+
+def paged_append(prob, step, rotation, positions, q_new, k_new, v_new, pages, slots, q_out=None):
+    """rotate_append into pages: the token (b, t) goes to slots[b, t], int32 [B, T]
+    (include/nacl.h: nacl_paged_append).  Returns q_out."""
+    lib = _lib or load_library()
+    dev = pages.on(prob)
+    step.on(prob, dev)
+    r, pos = _rotation(prob, step, rotation, positions, dev)
+    dt = step.dtype
+    _like(slots, "slots", dev, (prob.B, step.T), torch.int32)
+    if q_out is None:
+        q_out = torch.empty(step.q_shape, dtype=dt, device=dev)
+    s = step.strided(_rows4(q_new, "q_new", dev, step.q_shape, dt), _rows4(k_new, "k_new", dev, step.new_shape, dt),
+                     _rows4(v_new, "v_new", dev, step.new_shape, dt), _rows4(q_out, "q_out", dev, step.q_shape, dt))
+    _launch(dev, lib.nacl_paged_append, prob.ref(), s, r, pos, q_new.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), pages.c,
+            slots.data_ptr(), q_out.data_ptr())
+    return q_out
+
+
+def paged_workspace(prob, step, pages, device=None):
+    """A workspace for paged_attention calls of these sizes."""
+    lib = load_library()
+    dev = pages.on(prob)
+    n = int(lib.nacl_paged_workspace_bytes(prob.ref(), ctypes.byref(step.c), ctypes.byref(pages.c)))
+    if n == 0:
+        raise NaclError(NACL_ERR_INVALID_ARG, lib.nacl_last_error_detail().decode())
+    return torch.empty(n, dtype=torch.uint8, device=dev if device is None else device)
+
+
+def paged_attention(prob, step, q, pages, out=None, lse=None, ws=None):
+    """Attention of the step's queries q [B, H*q_group, T, D] to their sequences'
+    pages, which hold the step's own tokens already (include/nacl.h:
+    nacl_paged_attention).  Returns (out [B, H*q_group, T, D], lse [B, H*q_group, T]
+    fp32); lse=False: no lse."""
+    lib = _lib or load_library()
+    dev = pages.on(prob)
+    step.on(prob, dev)
+    s = step.strided(_rows4(q, "q", dev, step.q_shape, step.dtype))
+    if out is None:
+        out = torch.empty(step.q_shape, dtype=step.dtype, device=dev)
+    else:
+        _like(out, "out", dev, step.q_shape, step.dtype)
+    if lse is None:
+        lse = torch.empty(step.q_shape[:3], dtype=torch.float32, device=dev)
+    elif lse is False:
+        lse = None
+    else:
+        _like(lse, "lse", dev, step.q_shape[:3], torch.float32)
+    if ws is None:
+        ws = paged_workspace(prob, step, pages, dev)
+    n = ws.numel()
+    _like(ws, "ws", dev, (n,), torch.uint8)
+    _launch(dev, lib.nacl_paged_attention, prob.ref(), s, pages.c, q.data_ptr(), out.data_ptr(),
+            None if lse is None else lse.data_ptr(), ws.data_ptr(), n)
+    return out, lse
+
+
+def _beams(B, W, V, K):
+    if not -2 ** 31 <= min(B, W, V, K) <= max(B, W, V, K) < 2 ** 31:
+        raise ValueError("B, W, V and K must fit 32 bits")
+    return _Beams(int(B), int(W), int(V), int(K), NACL_F32, int(V))
+
+
+def beam_workspace(B, W, V, K, device="cuda"):
+    """A workspace for beam_select calls of B groups of W beams over a vocabulary of
+    V with K continuations each, of either dtype."""
+    lib = load_library()
+    n = int(lib.nacl_beam_workspace_bytes(ctypes.byref(_beams(B, W, V, K))))
+    if n == 0:
+        raise NaclError(NACL_ERR_INVALID_ARG, lib.nacl_last_error_detail().decode())
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def beam_select(logits, scores, K, ended=None, end_token=0, parents=None, tokens=None, out=None, ws=None):
+    """The K best continuations of every group's beams: logits [B * W, V] (fp32 or
+    bf16, any row stride), scores fp32 [B, W], ended (optional) int32 [B, W]
+    (include/nacl.h: nacl_beam_select).  Returns (parents int32 [B, K], tokens int32
+    [B, K], out fp32 [B, K])."""
+    lib = _lib or load_library()
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("logits must be [B * W, V] of fp32 or bf16")
+    N, V = logits.shape
+    dev = logits.device
+    if not logits.is_cuda:
+        _gpu(logits, "logits", dev)
+    if not isinstance(scores, torch.Tensor) or scores.dim() != 2 or scores.numel() != N:
+        raise ValueError("scores must be [B, W] for logits of [B * W, V]")
+    B, W = scores.shape
+    stride, one = logits.stride()
+    if V > 1 and one != 1:
+        raise ValueError("logits must have a contiguous last dimension")
+    if N > 1 and stride < V:
+        raise ValueError("rows of logits must not overlap")
+    _like(scores, "scores", dev, scores.shape, torch.float32)
+    d = _beams(B, W, V, int(K))
+    d.dtype = NACL_F32 if logits.dtype == torch.float32 else NACL_BF16
+    if N > 1:
+        d.stride = stride
+    if ended is not None:
+        _like(ended, "ended", dev, scores.shape, torch.int32)
+        if not 0 <= int(end_token) < V:
+            raise ValueError(f"end_token must lie in [0, {V})")
+        d.ended, d.end_token = ended.data_ptr(), int(end_token)
+    shape = (B, int(K))
+    if ws is None:
+        ws = beam_workspace(B, W, V, int(K), dev)
+    outs = []
+    for t, name, dtype in ((parents, "parents", torch.int32), (tokens, "tokens", torch.int32), (out, "out", torch.float32)):
+        if t is None:
+            t = torch.empty(shape, dtype=dtype, device=dev)
+        else:
+            _like(t, name, dev, shape, dtype)
+        outs.append(t)
+    parents, tokens, out = outs
+    n = ws.numel()
+    _like(ws, "ws", dev, (n,), torch.uint8)
+    _launch(dev, lib.nacl_beam_select, d, logits.data_ptr(), scores.data_ptr(), parents.data_ptr(), tokens.data_ptr(),
+            out.data_ptr(), ws.data_ptr(), n)
+    return parents, tokens, out
+
+
+def beam_reorder(prob, pages, parents, lens, held=None, table_out=None, lens_out=None, held_out=None):
+    """Every beam takes over what its parent holds, parents int32 [B / W, W], lens and
+    held (optional) int32 [B] (include/nacl.h: nacl_beam_reorder).  Returns
+    (table_out [B, entries], lens_out [B], held_out [B] or None): the tables of the
+    next step, new tensors or the given ones, which are not the old ones."""
+    lib = _lib or load_library()
+    dev = pages.on(prob)
+    if not isinstance(parents, torch.Tensor) or parents.dim() != 2 or parents.numel() != prob.B:
+        raise ValueError("parents must be [B / W, W]")
+    _like(parents, "parents", dev, parents.shape, torch.int32)
+    rows = (prob.B,)
+    _like(lens, "lens", dev, rows, torch.int32)
+    if held is None:
+        if held_out is not None:
+            raise ValueError("held_out needs held")
+    else:
+        _like(held, "held", dev, rows, torch.int32)
+        if held_out is None:
+            held_out = torch.empty_like(held)
+        else:
+            _like(held_out, "held_out", dev, rows, torch.int32)
+    if table_out is None:
+        table_out = torch.empty((prob.B, pages.c.entries), dtype=torch.int32, device=dev)
+    stride = _table(table_out, "table_out", dev, prob.B, pages.c.entries)
+    if lens_out is None:
+        lens_out = torch.empty_like(lens)
+    else:
+        _like(lens_out, "lens_out", dev, rows, torch.int32)
+    _launch(dev, lib.nacl_beam_reorder, prob.ref(), pages.c, parents.shape[1], parents.data_ptr(), lens.data_ptr(),
+            None if held is None else held.data_ptr(), table_out.data_ptr(), stride, lens_out.data_ptr(),
+            None if held_out is None else held_out.data_ptr())
+    return table_out, lens_out, held_out

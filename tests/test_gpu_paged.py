@@ -1,0 +1,317 @@
+"""Decoding over a paged cache: nacl_pages_assign against its reference,
+nacl_paged_append against the rotation into a contiguous cache, bit for bit, and
+nacl_paged_attention against the float64 attention of each row."""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+nacl = pytest.importorskip("paper_2408_03675_amd.nacl")
+from oracle.paged import assign_pages
+from oracle.step import attend_row
+from test_gpu_prefix import DEV, DT, _f64, _rows, check_rows
+
+pytestmark = pytest.mark.gpu
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def _pool(g, n, H, page, D, dtype, layout):
+    """Pools of n pages in one of the layouts that programs use."""
+    r = lambda *s: torch.randn(s, generator=g).to(DT[dtype]).to(DEV)
+    if layout == "heads":
+        return r(n, H, page, D), r(n, H, page, D)
+    if layout == "rows":
+        return r(n, page, H, D).transpose(1, 2), r(n, page, H, D).transpose(1, 2)
+    if layout == "one":  # K and V of a page side by side
+        x = r(n, 2, H, page, D)
+        return x[:, 0], x[:, 1]
+    x = r(n, page, H, 2, D).transpose(1, 2)  # K and V of a row side by side
+    return x[..., 0, :], x[..., 1, :]
+
+
+# --------------------------------------------------------------------------
+# Pages
+
+def _assign_case(B, T, page, entries, seed, spare=3, strided=False, short=False):
+    rng = np.random.default_rng(seed)
+    n_pages = B * entries + spare
+    pages = rng.permutation(n_pages)
+    L = entries * page - rng.integers(0, page)
+    held = rng.integers(0, entries + 1, B)
+    lens = rng.integers(0, np.maximum(1, np.minimum(L, held * page + 1)))
+    new = rng.integers(0, T + 1, B)
+    ended = rng.random(B) < 0.2
+    lens[ended], new[ended] = 0, 0
+    table = np.full((B, entries), -1)
+    at = 0
+    for b in range(B):
+        table[b, :held[b]] = pages[at:at + held[b]]
+        at += held[b]
+    n_free = n_pages - at if not short else min(3, n_pages - at)
+    free = np.full(n_pages, -7)
+    free[:n_free] = pages[at:at + n_free]
+    return dict(page=page, n_pages=n_pages, table=table.tolist(), held=held.tolist(), free=free.tolist(), n_free=int(n_free),
+                lens=lens.tolist(), n_new=new.tolist(), T=T, L=int(L))
+
+
+def _assign(c, row0=0, shared=None, in_place=False, stride=0, given=True):
+    B, entries = len(c["table"]), len(c["table"][0])
+    prob = nacl.Problem(B, 1, c["L"], 64, "bf16", [0])
+    lens, n_new = (_i32(c["lens"]), _i32(c["n_new"])) if given else (None, None)
+    step = nacl.Step(prob, c["T"], lens=lens, n_new=n_new, row0=row0)
+    table = torch.full((B, entries + stride), -5, dtype=torch.int32, device=DEV)[:, :entries]
+    table.copy_(_i32(c["table"]))
+    held, free, n_free = _i32(c["held"]), _i32(c["free"]), _i32([c["n_free"]])
+    kw = dict(held_out=held, n_free_out=n_free) if in_place else {}
+    held_out, n_out, slots, missing = nacl.pages_assign(step, c["page"], table, held, free, n_free,
+                                                        shared=None if shared is None else _i32(shared), **kw)
+    torch.cuda.synchronize()
+    if not in_place:
+        assert held.tolist() == c["held"] and n_free.tolist() == [c["n_free"]]
+    return table.tolist(), held_out.tolist(), free.tolist(), int(n_out), slots.tolist(), int(missing)
+
+
+@pytest.mark.parametrize("B,T,page,entries", [(1, 1, 16, 1), (1, 1, 1, 5), (64, 1, 16, 60), (7, 5, 27, 9), (3, 700, 16, 80),
+                                              (300, 60, 13, 12), (1025, 2, 4, 7), (2500, 1, 3, 5), (2, 40000, 128, 400)])
+@pytest.mark.parametrize("short", [False, True])
+def test_assign(B, T, page, entries, short):
+    c = _assign_case(B, T, page, entries, seed=B + T, short=short)
+    want = assign_pages(**c)
+    assert _assign(c) == want
+    assert _assign(c, in_place=True, stride=3) == want
+
+
+def test_assign_shared_row0_and_odd_values():
+    """Pages that belong to others, lengths and counts outside their ranges, a
+    stack that claims too much or less than nothing, entries outside the pool."""
+    c = _assign_case(40, 4, 8, 10, seed=5)
+    shared = [(7 * b) % 11 for b in range(40)]
+    assert _assign(c, shared=shared) == assign_pages(**c, shared=shared)
+    assert _assign(c, row0=13) == assign_pages(**c, row0=13)
+    c["lens"][3], c["lens"][4], c["n_new"][5], c["n_new"][6] = -9, 1 << 30, 99, -4
+    c["held"][7], c["held"][8], c["table"][9][0], c["table"][10][0] = -3, 99, 1 << 30, -2
+    assert _assign(c) == assign_pages(**c)
+    for n in (-5, 1 << 30):
+        assert _assign(dict(c, n_free=n)) == assign_pages(**dict(c, n_free=n))
+
+
+def test_assign_without_lengths():
+    c = _assign_case(5, 20, 8, 4, seed=8)
+    got = _assign(c, given=False)
+    assert got == assign_pages(**dict(c, lens=[0] * 5, n_new=[20] * 5))
+
+
+# --------------------------------------------------------------------------
+# Append
+
+@pytest.mark.parametrize("layout", ["heads", "rows", "one", "side"])
+@pytest.mark.parametrize("B,H,G,T,D,rot,page,dtype,norm,inter", [
+    (1, 1, 1, 1, 64, 64, 16, "bf16", False, False), (5, 2, 3, 1, 128, 128, 16, "bf16", True, False),
+    (3, 2, 2, 37, 128, 64, 7, "f32", True, True), (2, 4, 1, 130, 64, 32, 64, "bf16", False, True),
+])
+def test_append_is_the_rotation_into_a_cache(layout, B, H, G, T, D, rot, page, dtype, norm, inter):
+    g = torch.Generator().manual_seed(T)
+    dt, Hq, L = DT[dtype], H * G, 3 * page + T
+    entries = -(-L // page)
+    n = B * entries + 2
+    x = torch.randn((B, T, Hq + 2 * H, D), generator=g).to(dt).to(DEV).permute(0, 2, 1, 3)
+    q, kn, vn = x[:, :Hq], x[:, Hq:Hq + H], x[:, Hq + H:]
+    k, v = _pool(g, n, H, page, D, dtype, layout)
+    table = torch.randperm(n, generator=g)[:B * entries].view(B, entries)
+    lens = torch.randint(0, L - T + 1, (B,), generator=g, dtype=torch.int32)
+    new = torch.randint(T // 2, T + 1, (B,), generator=g, dtype=torch.int32)
+    j = lens[:, None].long() + torch.arange(T)
+    slots = (table.gather(1, j // page) * page + j % page).int()
+    slots[torch.arange(T) >= new[:, None]] = -1
+    # Slots that are none: the token joins no cache, its query is turned all the same.
+    slots[0, 0] = n * page
+    pos = torch.randint(0, 1 << 20, (B, T), generator=g, dtype=torch.int32).to(DEV)
+    f = (10000.0 ** (-torch.arange(rot // 2, dtype=torch.float64) / (rot // 2))).float().to(DEV)
+    wq, wk = ((1 + 0.3 * torch.randn((D,), generator=g)).to(dt).to(DEV) if norm else None for _ in range(2))
+    prob = nacl.Problem(B, H, L, D, dtype, [0], q_group=G)
+    rotation = nacl.Rotation(prob, f, wq, wk, eps=1e-5, interleaved=inter)
+    step = nacl.Step(prob, T, lens=lens.to(DEV), n_new=new.to(DEV))
+    kc, vc = (torch.zeros((B, H, L, D), dtype=dt, device=DEV) for _ in range(2))
+    q_ref = torch.full((B, Hq, T, D), 3.0, dtype=dt, device=DEV)
+    nacl.rotate_append(prob, step, rotation, pos, q, kn, vn, kc, vc, q_out=q_ref)
+    want_k, want_v = k.clone(), v.clone()
+    for b in range(B):
+        for t in range(int(new[b])):
+            if (b, t) != (0, 0):
+                s = int(slots[b, t])
+                want_k[s // page, :, s % page] = kc[b, :, int(lens[b]) + t]
+                want_v[s // page, :, s % page] = vc[b, :, int(lens[b]) + t]
+    q_out = torch.full_like(q_ref, 3.0)
+    pages = nacl.Pages(prob, k, v, table.int().to(DEV))
+    nacl.paged_append(prob, step, rotation, pos, q, kn, vn, pages, slots.to(DEV), q_out=q_out)
+    torch.cuda.synchronize()
+    assert torch.equal(q_out, q_ref) and torch.equal(k, want_k) and torch.equal(v, want_v)
+
+
+# --------------------------------------------------------------------------
+# Attention
+
+def _dense(pool, table, L):
+    B, entries = table.shape
+    n, H, page, D = pool.shape
+    x = pool[table.long().clamp(0, n - 1)].permute(0, 2, 1, 3, 4).reshape(B, H, entries * page, D)
+    return x[:, :, :L]
+
+
+def _attend_case(B, H, G, T, L, D, page, dtype, layout="heads", seed=0, spare=3, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    entries = -(-L // page)
+    n = B * entries + spare
+    k, v = _pool(g, n, H, page, D, dtype, layout)
+    table = torch.randperm(n, generator=g)[:B * entries].view(B, entries).int()
+    q = (scale * torch.randn((B, T, H * G, D), generator=g)).to(DT[dtype]).to(DEV).permute(0, 2, 1, 3)
+    lens = torch.randint(0, L - T + 1, (B,), generator=g, dtype=torch.int32)
+    lens[0] = L - T
+    if B > 1:
+        lens[1] = 0
+    return q, k, v, table.to(DEV), lens
+
+
+#        B  H  G  T   L     D   page dtype  layout
+CASES = [
+    (1, 1, 1, 1, 1, 128, 16, "bf16", "heads"),
+    (1, 1, 1, 1, 1, 64, 1, "f32", "heads"),
+    (1, 8, 4, 1, 2112, 128, 16, "bf16", "heads"),
+    (5, 2, 7, 1, 333, 128, 16, "bf16", "rows"),
+    (3, 2, 1, 1, 129, 64, 1, "bf16", "one"),
+    (6, 4, 2, 5, 333, 64, 27, "f32", "side"),
+    (2, 1, 8, 3, 100, 128, 33, "f32", "rows"),
+    (4, 2, 2, 1, 700, 128, 64, "bf16", "side"),
+    (3, 2, 4, 5, 500, 64, 5, "bf16", "heads"),
+    (2, 2, 4, 65, 200, 128, 16, "bf16", "heads"),
+    (1, 3, 1, 130, 131, 64, 11, "bf16", "one"),
+    (2, 1, 2, 40, 3000, 128, 100, "bf16", "rows"),
+    (40, 1, 2, 1, 50, 64, 128, "bf16", "heads"),
+    (1, 2, 64, 1, 300, 128, 32, "bf16", "rows"),
+    (1, 1, 2, 1, 70000, 64, 7, "bf16", "heads"),
+    (1, 1, 1, 2, 40000, 128, 20000, "f32", "heads"),
+    (2, 2, 1, 33, 90, 64, 16, "f32", "heads"),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_attention_rows(case):
+    B, H, G, T, L, D, page, dtype, layout = case
+    q, k, v, table, lens = _attend_case(*case)
+    prob = nacl.Problem(B, H, L, D, dtype, [L - 1], q_group=G)
+    step = nacl.Step(prob, T, lens=lens.to(DEV))
+    out, lse = nacl.paged_attention(prob, step, q, nacl.Pages(prob, k, v, table))
+    torch.cuda.synchronize()
+    check_rows(q, _dense(k, table, L), _dense(v, table, L), None, None, lens, None, out, lse, prob.c.sm_scale,
+               _rows(B, H * G, T))
+
+
+@pytest.mark.parametrize("dtype,G,T", [("bf16", 3, 4), ("f32", 3, 4), ("bf16", 8, 3), ("bf16", 3, 50)])
+@pytest.mark.parametrize("page", [8, 16, 27])
+def test_hidden_rows_may_hold_anything(dtype, G, T, page):
+    """Rows past the lengths, pages of nobody, later tokens, padding with NaN and
+    infinities; lengths below 0 and past the table; a page that two sequences
+    share; a table with strided rows."""
+    B, H, L, D = 5, 2, 160, 128
+    q, k, v, table, _ = _attend_case(B, H, G, T, L, D, page, dtype, seed=page)
+    room = table.shape[1] * page
+    lens = torch.tensor([40, -400, 1000, 7, 90], dtype=torch.int32)
+    n_new = torch.tensor([T, T, T, 2, T], dtype=torch.int32)
+    row0, shared = 5, 16 // page
+    table[4, :shared] = table[0, :shared]
+    used = torch.zeros((k.shape[0], page), dtype=torch.bool)
+    for b in range(B):
+        for j in range(min(room, L, max(0, row0 + int(lens[b]) + int(n_new[b])))):
+            used[int(table[b, j // page]), j % page] = True
+    for pool, bad in ((k, math.nan), (v, math.inf)):
+        pool.transpose(1, 2)[~used.to(DEV)] = bad
+    odd_at = row0 + 40 + 2  # tokens 2 and later of sequence 0 see it, the others not
+    k[int(table[0, odd_at // page]), :, odd_at % page] = math.nan
+    v[int(table[0, (odd_at + 1) // page]), :, (odd_at + 1) % page] = math.inf
+    wide = torch.full((B, table.shape[1] + 3), -1, dtype=torch.int32, device=DEV)
+    wide[:, :table.shape[1]] = table
+    prob = nacl.Problem(B, H, L, D, dtype, [L - 1], q_group=G, sm_scale=0.2)
+    step = nacl.Step(prob, T, lens=lens.to(DEV), row0=row0, n_new=n_new.to(DEV))
+    out, lse = nacl.paged_attention(prob, step, q, nacl.Pages(prob, k, v, wide[:, :table.shape[1]]))
+    torch.cuda.synchronize()
+    kd, vd = _dense(k, table, L), _dense(v, table, L)
+    odd = {(0, hq, t) for hq in range(H * G) for t in range(2, T)}
+    check_rows(q, kd, vd, None, None, lens, None, out, lse, 0.2, [x for x in _rows(B, H * G, T) if x not in odd], row0=row0,
+               n_new=n_new.tolist())
+    for b, hq, t in odd:
+        assert torch.isnan(out[b, hq, t]).any()
+
+
+@pytest.mark.parametrize("dtype,G,T,page", [("bf16", 2, 1, 16), ("f32", 2, 3, 5), ("bf16", 4, 40, 16), ("bf16", 2, 1, 64)])
+def test_pages_outside_the_pool_are_not_seen(dtype, G, T, page):
+    B, H, L, D = 3, 2, 400, 64
+    q, k, v, table, lens = _attend_case(B, H, G, T, L, D, page, dtype, seed=3)
+    lens[:] = torch.tensor([L - T, 200, 60])
+    bad = table.clone()
+    bad[0, 1], bad[0, 3], bad[1, :], bad[2, 0] = -1, k.shape[0], -9, 1 << 30
+    bad[0, table.shape[1] - 1] = -1 << 31
+    k[0, :, 0], v[0, :, 0] = math.nan, math.inf  # where nothing is to be read
+    k0 = k.clone()
+    prob = nacl.Problem(B, H, L, D, dtype, [L - 1], q_group=G)
+    step = nacl.Step(prob, T, lens=lens.to(DEV))
+    there = (bad.cpu() >= 0) & (bad.cpu() < k.shape[0])
+    # Page 0 is out of the way, so its NaN is nobody's.
+    there &= bad.cpu() != 0
+    bad[bad == 0] = -1
+    out, lse = nacl.paged_attention(prob, step, q, nacl.Pages(prob, k, v, bad))
+    torch.cuda.synchronize()
+    kd, vd = _f64(_dense(k0, bad, L)), _f64(_dense(v, bad, L))
+    seen = there.repeat_interleave(page, dim=1)[:, :L].numpy()
+    u = 2.0 ** -8 if dtype == "bf16" else 0.0
+    for b, hq, t in _rows(B, H * G, T):
+        n = int(lens[b]) + t + 1
+        at = np.flatnonzero(seen[b, :n])
+        ref, ref_l, size, S = attend_row(_f64(q[b, hq, t]), kd[b, hq // G, at], vd[b, hq // G, at], prob.c.sm_scale)
+        o, l = _f64(out[b, hq, t]), float(lse[b, hq, t])
+        if len(at) == 0:
+            assert l == -math.inf and (o == 0).all()
+            continue
+        gamma = (D + 8) * 2.0 ** -24 * S + (len(at) + 64) * 2.0 ** -24  # as for check_rows
+        tol = torch.finfo(q.dtype).eps / 2 * np.abs(ref) + (u + 2 * gamma) * 1.01 * size
+        assert (np.abs(o - ref) <= tol).all() and abs(l - ref_l) <= gamma + 2.0 ** -23 * abs(ref_l) + 2.0 ** -22
+
+
+def test_no_logit_has_weight():
+    """Infinite negative logits: zeros and -infinity, in one chunk and in many."""
+    for L in (100, 5000):
+        q, k, v, table, lens = _attend_case(1, 1, 1, 1, L, 64, 16, "bf16")
+        q[..., 0], k[..., 0] = 1.0, -math.inf
+        prob = nacl.Problem(1, 1, L, 64, "bf16", [L - 1])
+        out, lse = nacl.paged_attention(prob, nacl.Step(prob, 1, lens=lens.to(DEV)), q, nacl.Pages(prob, k, v, table))
+        assert (out == 0).all() and (lse == -math.inf).all()
+
+
+def test_far_pages():
+    """Pages whose places pass 32 bits of elements."""
+    H, page, D, n = 1, 16, 128, (1 << 32) // (16 * 128) + 64
+    k = torch.zeros((n, H, page, D), dtype=torch.bfloat16, device=DEV)
+    prob = nacl.Problem(1, H, 64, D, "bf16", [0])
+    g = torch.Generator().manual_seed(0)
+    table = _i32([[n - 1, 3, n - 5, n - 2]])
+    rows = torch.randn((64, D), generator=g).bfloat16().to(DEV)
+    k[table[0].long(), 0] = rows.view(4, page, D)
+    q = torch.randn((1, 1, 1, D), generator=g).bfloat16().to(DEV)
+    step = nacl.Step(prob, 1, lens=_i32([62]))
+    out, lse = nacl.paged_attention(prob, step, q, nacl.Pages(prob, k, k, table))
+    check_rows(q, rows[None, None], rows[None, None], None, None, [62], None, out, lse, prob.c.sm_scale, [(0, 0, 0)])
+    # And the append's, and the reordering's.
+    v = torch.zeros((n, H, page, D), dtype=torch.bfloat16, device=DEV)
+    kn, vn = (torch.randn((1, 1, 1, D), generator=g).bfloat16().to(DEV) for _ in range(2))
+    slots = _i32([[(n - 1) * page + 5]])
+    nacl.paged_append(prob, step, nacl.Rotation(prob), None, q, kn, vn, nacl.Pages(prob, k, v, table), slots)
+    assert torch.equal(k[n - 1, 0, 5], kn[0, 0, 0]) and torch.equal(v[n - 1, 0, 5], vn[0, 0, 0])
+    two = nacl.Problem(2, H, 64, D, "bf16", [0])
+    table = _i32([[n - 1, 3], [n - 7, n - 9]])
+    want = k[[n - 1, 3]].clone()
+    nacl.beam_reorder(two, nacl.Pages(two, k, v, table), _i32([[0, 0]]), _i32([32, 32]))
+    assert torch.equal(k[[n - 7, n - 9]], want)
