@@ -36,31 +36,37 @@ __device__ __forceinline__ double of_order_key(uint64_t k) {
   return __builtin_bit_cast(double, (k >> 63) ? k & ~(1ull << 63) : ~k);
 }
 
-// A bound that at least `want` of the wave's keys (N per lane) reach, at most
-// `most` of them unless more are equal; 1 where fewer than `want` are not 0.
-// Every wave that calls it with the same keys gets the same bound.
+// A bound that at least `want` of the wave's keys (N per lane) reach and at most
+// `most` of them, unless more are equal to it; 1 where fewer than `want` are not 0.
+// It is looked for downwards from the largest key, top, in steps that grow from
+// `step`, then between the last two: a handful of rounds where the step is of the
+// size of the keys' distances, twice the key's bits at most.  `reach`: how many keys
+// reach it.  Every wave with the same keys gets the same bound.
 template <int N, typename K>
-__device__ __forceinline__ K bound_of(const K (&key)[N], int want, int most) {
-  K bound = 0;
-  for (int bit = 8 * (int)sizeof(K) - 1; bit >= 0; --bit) {
-    const K trial = bound | (K)1 << bit;
-    int n = 0;
+__device__ __forceinline__ K bound_of(const K (&key)[N], K top, K step, int want, int most, int& reach) {
+  if (top == 0) {
+    reach = 0;
+    return 1;
+  }
+  K lo = 0, hi = 0, d = min(step, (K)(top - 1));  // distances: too few keys are nearer than lo
+  for (;;) {
+    reach = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) n += (int)__popcll(__ballot(key[i] >= trial));
-    if (n >= want) {
-      bound = trial;
-      if (n <= most) break;
+    for (int i = 0; i < N; ++i) reach += (int)__popcll(__ballot(key[i] >= top - d));
+    if (reach >= want) {
+      if (reach <= most || d == lo) break;
+      hi = d;
+      d = lo + (d - lo) / 2;
+    } else {
+      if (d == top - 1) break;
+      lo = d + 1;
+      d = hi ? lo + (hi - lo) / 2 : d > (top - 1) / 4 ? top - 1 : 4 * d + 3;
     }
   }
-  return bound ? bound : 1;
+  return top - d;
 }
-template <int N, typename K>
-__device__ __forceinline__ int count_of(const K (&key)[N], K bound) {
-  int n = 0;
-#pragma unroll
-  for (int i = 0; i < N; ++i) n += (int)__popcll(__ballot(key[i] >= bound));
-  return n;
-}
+
+constexpr int kRankPad = 3;  // zeros behind a list that is read by fours
 
 // ---------------------------------------------------------------------------
 // Slices.  A thread takes kPer tokens as 16-byte pieces; the piece's place is its
@@ -92,13 +98,14 @@ struct Piece<float> {
 };
 
 constexpr uint32_t kLeast = 0x00800000u;  // key of the lowest finite number
+constexpr float kLog2e = 1.44269504f;
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void beam_slices_kernel(BeamLaunch a) {
   using P = Piece<T>;
   constexpr int kPieces = kPer / P::kN;
-  // Logits that reach the bound: at most K threads hold them.
-  __shared__ uint64_t list[kMaxK * kPer];
+  // Logits that reach the bound, of kMaxK threads at most.
+  __shared__ uint64_t list[kMaxK * kPer + kRankPad];
   __shared__ uint32_t maxima[kThreads];
   __shared__ float wave_max[kThreads / 64];
   __shared__ double wave_sum[kThreads / 64];
@@ -109,40 +116,51 @@ __global__ __launch_bounds__(kThreads) void beam_slices_kernel(BeamLaunch a) {
   const T* x0 = reinterpret_cast<const T*>(a.logits) + (int64_t)row * a.stride;
   const int head = (int)(((uintptr_t)x0 & 15) / sizeof(T));  // tokens by which the pieces start before the row
   const int first = slice * kBeamSlice - head;
+  auto token = [&](int u, int i) { return first + (u * kThreads + tid) * P::kN + i; };
 
-  // NaN and what lies outside the row are -infinity, -0 is 0.
   float x[kPieces][P::kN];
+  if (first >= 0 && first + kBeamSlice <= a.V) {
 #pragma unroll
-  for (int u = 0; u < kPieces; ++u) {
-    const int at = first + (u * kThreads + tid) * P::kN;
-    if (at >= 0 && at + P::kN <= a.V) {
-      P::load(x0 + at, x[u]);
-    } else {
+    for (int u = 0; u < kPieces; ++u) P::load(x0 + token(u, 0), x[u]);
+  } else {
 #pragma unroll
-      for (int i = 0; i < P::kN; ++i) x[u][i] = (uint32_t)(at + i) < (uint32_t)a.V ? (float)x0[at + i] : -INFINITY;
+    for (int u = 0; u < kPieces; ++u) {
+      const int at = token(u, 0);
+      if (at >= 0 && at + P::kN <= a.V) {
+        P::load(x0 + at, x[u]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < P::kN; ++i) x[u][i] = (uint32_t)(at + i) < (uint32_t)a.V ? (float)x0[at + i] : -INFINITY;
+      }
     }
   }
-  float m = -INFINITY;
-#pragma unroll
-  for (int u = 0; u < kPieces; ++u)
-#pragma unroll
-    for (int i = 0; i < P::kN; ++i) {
-      x[u][i] = x[u][i] == x[u][i] ? x[u][i] + 0.f : -INFINITY;
-      m = fmaxf(m, x[u][i]);
-    }
   if (tid == 0) found = 0;
-  maxima[tid] = m == -INFINITY ? 0 : float_order_key(m);
 
-  // The slice's maximum and its exponentials' sum against it, each thread's sum
-  // of kPer in fp32 against its own maximum, those in fp64.  Infinite logits share
-  // a row, so they count as one each and the others as nothing.
-  float sum = 0.f;
+  // The thread's maximum and its exponentials' sum against it, of kPer terms in
+  // fp32.  A NaN among the logits, or nothing but infinities, makes the sum a NaN.
+  float m = -INFINITY, sum = 0.f;
 #pragma unroll
   for (int u = 0; u < kPieces; ++u)
 #pragma unroll
-    for (int i = 0; i < P::kN; ++i)
-      sum += m == INFINITY ? (x[u][i] == INFINITY ? 1.f : 0.f)
-                           : __builtin_amdgcn_exp2f((x[u][i] - (m == -INFINITY ? 0.f : m)) * 1.44269504f);
+    for (int i = 0; i < P::kN; ++i) m = x[u][i] > m ? x[u][i] : m;
+#pragma unroll
+  for (int u = 0; u < kPieces; ++u)
+#pragma unroll
+    for (int i = 0; i < P::kN; ++i) sum += __builtin_amdgcn_exp2f((x[u][i] - m) * kLog2e);
+  if (!(sum == sum)) {
+    // A NaN counts as -infinity; infinite logits share a row, one each, and the
+    // others are nothing beside them.
+    sum = 0.f;
+#pragma unroll
+    for (int u = 0; u < kPieces; ++u)
+#pragma unroll
+      for (int i = 0; i < P::kN; ++i) {
+        const float e = x[u][i] == m ? 1.f : __builtin_amdgcn_exp2f((x[u][i] - m) * kLog2e);
+        sum += m > -INFINITY && x[u][i] == x[u][i] ? e : 0.f;
+      }
+  }
+  const uint32_t mine = m == -INFINITY ? 0 : float_order_key(m + 0.f);  // (-0 is 0)
+  maxima[tid] = mine;
   float wm = m;
 #pragma unroll
   for (int i = 1; i < 64; i *= 2) wm = fmaxf(wm, __shfl_xor(wm, i));
@@ -151,20 +169,22 @@ __global__ __launch_bounds__(kThreads) void beam_slices_kernel(BeamLaunch a) {
   float top = wave_max[0];
 #pragma unroll
   for (int i = 1; i < kThreads / 64; ++i) top = fmaxf(top, wave_max[i]);
-  double s = m == top ? (double)sum : (double)sum * __builtin_amdgcn_exp2f((m - top) * 1.44269504f);
-  if (top == -INFINITY) s = 0.0;
+  // The sums are joined in fp64.
+  double s = (double)(m == top ? sum : sum * __builtin_amdgcn_exp2f((m - top) * kLog2e));
 #pragma unroll
   for (int i = 1; i < 64; i *= 2) s += __shfl_xor(s, i);
   if (lane == 0) wave_sum[wave] = s;
 
-  // The bound: the K-th largest of the threads' maxima or a little less.  Where
-  // more threads reach it, equal maxima do, and those with the first tokens count.
+  // The bound of the threads' maxima; logits of a language model are a few units
+  // apart there, 2^20 steps each.
   uint32_t key[kThreads / 64];
 #pragma unroll
   for (int i = 0; i < kThreads / 64; ++i) key[i] = maxima[lane + 64 * i];
-  const uint32_t bound = bound_of(key, a.K, a.K);
+  int reach;
+  const uint32_t top_key = top == -INFINITY ? 0 : float_order_key(top + 0.f);
+  const int most = min(2 * a.K, kMaxK);
+  const uint32_t bound = bound_of(key, top_key, 1u << 20, a.K, most, reach);
   uint32_t tie = 0;  // of the logits equal to the bound, those whose ~token reaches it
-  const int reach = count_of(key, bound);
   __syncthreads();  // the maxima are read
   const int64_t slot = (int64_t)row * a.S + slice;
   if (tid == 0) {
@@ -174,38 +194,43 @@ __global__ __launch_bounds__(kThreads) void beam_slices_kernel(BeamLaunch a) {
     a.sums[2 * slot] = (double)top;
     a.sums[2 * slot + 1] = t;
   }
-  const uint32_t mine = m == -INFINITY ? 0 : float_order_key(m);
-  if (reach > a.K) {
+  if (reach > most) {
+    // Equal maxima: the threads with the first tokens among them count.
     uint32_t k = mine > bound ? ~0u : 0;
     if (mine == bound) {
 #pragma unroll
       for (int u = kPieces - 1; u >= 0; --u)
 #pragma unroll
         for (int i = P::kN - 1; i >= 0; --i)
-          if (x[u][i] == m) k = ~(uint32_t)(first + (u * kThreads + tid) * P::kN + i);
+          if (x[u][i] == m) k = ~(uint32_t)token(u, i);
     }
     maxima[tid] = k;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kThreads / 64; ++i) key[i] = maxima[lane + 64 * i];
-    tie = bound_of(key, a.K, a.K);
+    tie = bound_of(key, ~0u, 1u << 12, a.K, a.K, reach);
   }
   if (mine >= bound) {
+    const float least = of_order_key(max(bound, kLeast));
 #pragma unroll
     for (int u = 0; u < kPieces; ++u)
 #pragma unroll
-      for (int i = 0; i < P::kN; ++i) {
-        const uint32_t k = float_order_key(x[u][i]), t = ~(uint32_t)(first + (u * kThreads + tid) * P::kN + i);
-        if (k >= kLeast && (k > bound || (k == bound && t >= tie))) list[atomicAdd(&found, 1)] = (uint64_t)k << 32 | t;
-      }
+      for (int i = 0; i < P::kN; ++i)
+        if (x[u][i] >= least) {
+          const uint32_t t = ~(uint32_t)token(u, i);
+          if (x[u][i] > least || t >= tie) list[atomicAdd(&found, 1)] = (uint64_t)float_order_key(x[u][i] + 0.f) << 32 | t;
+        }
   }
   __syncthreads();
   const int n = found;
+  if (tid < kRankPad) list[n + tid] = 0;
+  __syncthreads();
   uint64_t* out = a.keys + slot * a.K;
   for (int i = tid; i < n; i += kThreads) {
     const uint64_t k = list[i];
     int rank = 0;
-    for (int j = 0; j < n; ++j) rank += list[j] > k;
+    for (int j = 0; j < n; j += 4)
+      rank += (list[j] > k) + (list[j + 1] > k) + (list[j + 2] > k) + (list[j + 3] > k);
     if (rank < a.K) out[rank] = k;
   }
   for (int i = n + tid; i < a.K; i += kThreads) out[i] = 0;
@@ -216,6 +241,9 @@ __global__ __launch_bounds__(kThreads) void beam_slices_kernel(BeamLaunch a) {
 
 enum Mode { kNone, kLogits, kInfinite, kEnded };
 
+constexpr int kHeads = kBeamLists / kThreads;  // of a thread, at most
+constexpr int kGroup = 16;                     // lanes per beam
+
 __global__ __launch_bounds__(kThreads) void beam_finish_kernel(BeamLaunch a) {
   // A logit's value is (x - tops) + shift (kEnded, kInfinite: shift): a difference
   // that is exact next to a top of any size, then numbers of the values' size.
@@ -223,85 +251,115 @@ __global__ __launch_bounds__(kThreads) void beam_finish_kernel(BeamLaunch a) {
   __shared__ int mode[kMaxK];
   __shared__ uint64_t head[kBeamLists];  // the lists' first values
   __shared__ uint32_t head_at[kBeamLists];
-  __shared__ uint64_t list[kMaxK * kMaxK];
-  __shared__ uint32_t list_at[kMaxK * kMaxK];
+  __shared__ uint64_t list[kMaxK * kMaxK + kRankPad];
+  __shared__ uint32_t list_at[kMaxK * kMaxK + kRankPad];
+  __shared__ uint64_t wave_max[kThreads / 64];
   __shared__ int found;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int group = blockIdx.x;
+  const int lists = a.W * a.S;
+  const uint64_t* keys = a.keys + (int64_t)group * lists * a.K;
 
-  // The beams' normalisers, a wave per beam.
-  for (int w = wave; w < a.W; w += kThreads / 64) {
+  // The lists' first R entries are on their way while the normalisers are made: about
+  // four times as many as are looked for, so that their bound is near K's.
+  const int R = min(min(a.K, kBeamLists / lists), max(1, (4 * a.K + lists - 1) / lists));
+  const int heads = lists * R;
+  uint64_t raw[kHeads];
+#pragma unroll
+  for (int c = 0; c < kHeads; ++c) {
+    const int i = tid + c * kThreads;
+    raw[c] = i < heads ? keys[(int64_t)(i / R) * a.K + i % R] : 0;
+  }
+
+  // The beams' normalisers, kGroup lanes per beam.
+  for (int w0 = 0; w0 < a.W; w0 += kThreads / kGroup) {
+    const int w = w0 + tid / kGroup, sub = tid % kGroup;
     const int64_t row = (int64_t)group * a.W + w;
-    const double score = (double)a.scores[row];
-    const bool ended = a.ended && a.ended[row];
+    const bool there = w < a.W, ended = there && a.ended && a.ended[row];
+    const double score = there ? (double)a.scores[row] : 0.0;
     double top = -INFINITY, sum = 0.0;
-    if (!ended) {
-      const double* sums = a.sums + 2 * row * a.S;
-      for (int s = lane; s < a.S; s += 64) top = fmax(top, sums[2 * s]);
-#pragma unroll
-      for (int i = 1; i < 64; i *= 2) top = fmax(top, __shfl_xor(top, i));
-      for (int s = lane; s < a.S; s += 64) {
-        const double m = sums[2 * s];
-        if (m == top) sum += sums[2 * s + 1];
-        else if (m != -INFINITY && top != INFINITY) sum += sums[2 * s + 1] * exp(m - top);
+    if (there && !ended) {
+      const double2* sums = reinterpret_cast<const double2*>(a.sums) + row * a.S;
+      for (int s = sub; s < a.S; s += kGroup) {
+        const double2 x = sums[s];  // maximum, sum
+        if (x.x == top) {
+          sum += x.x == -INFINITY ? 0.0 : x.y;
+        } else if (x.x > top) {
+          sum = x.y + (x.x == INFINITY ? 0.0 : sum * exp(top - x.x));
+          top = x.x;
+        } else if (top != INFINITY) {
+          sum += x.y * exp(x.x - top);
+        }
       }
-#pragma unroll
-      for (int i = 1; i < 64; i *= 2) sum += __shfl_xor(sum, i);
     }
-    if (lane == 0) {
+    double all = top;
+#pragma unroll
+    for (int i = 1; i < kGroup; i *= 2) all = fmax(all, __shfl_xor(all, i));
+    if (top != all) sum = all == INFINITY ? 0.0 : sum * exp(top - all);
+#pragma unroll
+    for (int i = 1; i < kGroup; i *= 2) sum += __shfl_xor(sum, i);
+    if (there && sub == 0) {
       const bool finite = fabs(score) < INFINITY;
-      mode[w] = !finite || (!ended && top == -INFINITY) ? kNone : ended ? kEnded : top == INFINITY ? kInfinite : kLogits;
-      tops[w] = top;
+      mode[w] = !finite || (!ended && all == -INFINITY) ? kNone : ended ? kEnded : all == INFINITY ? kInfinite : kLogits;
+      tops[w] = all;
       shift[w] = ended ? score : score - log(sum);
     }
   }
   if (tid == 0) found = 0;
   __syncthreads();
 
-  const int lists = a.W * a.S;
-  const uint64_t* keys = a.keys + (int64_t)group * lists * a.K;
-  // Entry r of list l: its value and its place, beam and token.
-  auto entry = [&](int l, int r, uint32_t& at) -> uint64_t {
+  // Entry r of list l, whose key is k: its value and its place, beam and token.
+  auto entry = [&](int l, int r, uint64_t k, uint32_t& at) -> uint64_t {
     const int w = l / a.S, kind = mode[w];
     if (kind == kNone) return 0;
     at = (uint32_t)w << 20 | (uint32_t)a.end_token;
     if (kind == kEnded) return l == w * a.S && r == 0 ? order_key(shift[w]) : 0;
-    const uint64_t k = keys[(int64_t)l * a.K + r];
     if (!k) return 0;
     at = (uint32_t)w << 20 | ~(uint32_t)k;
     const float x = of_order_key((uint32_t)(k >> 32));
     if (kind == kInfinite) return x == INFINITY ? order_key(shift[w]) : 0;
     return order_key(((double)x - tops[w]) + shift[w]);
   };
-  // The lists' first R entries, and the bound that K of them reach (of equal
-  // values the first places).
-  const int R = min(a.K, kBeamLists / lists), heads = lists * R;
-  for (int i = tid; i < kBeamLists; i += kThreads) {
+  uint64_t top = 0;
+#pragma unroll
+  for (int c = 0; c < kHeads; ++c) {
+    const int i = tid + c * kThreads;
+    if (c * kThreads >= heads) break;
     uint32_t at = 0;
-    head[i] = i < heads ? entry(i / R, i % R, at) : 0;
+    head[i] = i < heads ? entry(i / R, i % R, raw[c], at) : 0;
     head_at[i] = at;
+    top = max(top, head[i]);
   }
+#pragma unroll
+  for (int i = 1; i < 64; i *= 2) top = max(top, (uint64_t)__shfl_xor((unsigned long long)top, i));
+  if (lane == 0) wave_max[wave] = top;
   __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kThreads / 64; ++i) top = max(top, wave_max[i]);
+
+  // The bound of the heads (of equal values the first places).  Values are a few
+  // units apart, 2^48 steps each.  (The list holds what follows `most` heads.)
   uint64_t bound = 1;
   uint32_t tie = 0;
+  const int most = R > 1 || 2 * a.K * a.K <= kMaxK * kMaxK ? 2 * a.K : a.K;
   auto search = [&](auto n_c) {
     constexpr int N = decltype(n_c)::value;
     uint64_t k[N];
+    int reach;
 #pragma unroll
     for (int i = 0; i < N; ++i) k[i] = head[64 * i + lane];
-    bound = bound_of(k, a.K, a.K);
-    if (count_of(k, bound) > a.K) {
+    bound = bound_of(k, top, (uint64_t)1 << 48, a.K, most, reach);
+    if (reach > most) {
       uint32_t t[N];
 #pragma unroll
       for (int i = 0; i < N; ++i) t[i] = k[i] > bound ? ~0u : k[i] == bound ? ~head_at[64 * i + lane] : 0;
-      tie = bound_of(t, a.K, a.K);
+      tie = bound_of(t, ~0u, 1u << 20, a.K, a.K, reach);
     }
   };
-  if (heads <= 64) search(std::integral_constant<int, 1>{});
-  else if (heads <= 256) search(std::integral_constant<int, 4>{});
-  else search(std::integral_constant<int, 16>{});
+  if (heads <= kThreads) search(std::integral_constant<int, kThreads / 64>{});
+  else search(std::integral_constant<int, kBeamLists / 64>{});
 
-  // What reaches it: K of the heads at most, and of their lists what follows.
+  // What reaches it, and of the lists whose heads all do, what follows.
   auto reaches = [&](uint64_t v, uint32_t at) { return v > bound || (v == bound && ~at >= tie); };
   auto add = [&](uint64_t v, uint32_t at) {
     const int i = atomicAdd(&found, 1);
@@ -314,18 +372,22 @@ __global__ __launch_bounds__(kThreads) void beam_finish_kernel(BeamLaunch a) {
     if (i % R != R - 1) continue;
     for (int r = R; r < a.K; ++r) {
       uint32_t at = 0;
-      const uint64_t v = entry(i / R, r, at);
+      const uint64_t v = entry(i / R, r, keys[(int64_t)(i / R) * a.K + r], at);
       if (!reaches(v, at)) break;
       add(v, at);
     }
   }
   __syncthreads();
   const int n = found;
+  if (tid < kRankPad) list[n + tid] = 0;
+  __syncthreads();
   for (int i = tid; i < n; i += kThreads) {
     const uint64_t v = list[i];
     const uint32_t at = list_at[i];
     int rank = 0;
-    for (int j = 0; j < n; ++j) rank += list[j] > v || (list[j] == v && list_at[j] < at);
+    for (int j = 0; j < n; j += 4)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) rank += list[j + e] > v || (list[j + e] == v && list_at[j + e] < at);
     if (rank < a.K) {
       const int64_t to = (int64_t)group * a.K + rank;
       a.parents[to] = (int)(at >> 20);
