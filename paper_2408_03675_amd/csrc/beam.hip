@@ -36,6 +36,15 @@ __device__ __forceinline__ double of_order_key(uint64_t k) {
   return __builtin_bit_cast(double, (k >> 63) ? k & ~(1ull << 63) : ~k);
 }
 
+// x of the lane N further in its row of 16, cyclically.
+template <int N>
+__device__ __forceinline__ double row_turn(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)u, 0x120 + N, 0xF, 0xF, true);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)(u >> 32), 0x120 + N, 0xF, 0xF, true);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
 // A bound that at least `want` of the wave's keys (N per lane) reach and at most
 // `most` of them, unless more are equal to it; 1 where fewer than `want` are not 0.
 // It is looked for downwards from the largest key, top, in steps that grow from
@@ -249,39 +258,50 @@ __global__ __launch_bounds__(kThreads) void beam_finish_kernel(BeamLaunch a) {
   // that is exact next to a top of any size, then numbers of the values' size.
   __shared__ double tops[kMaxK], shift[kMaxK];
   __shared__ int mode[kMaxK];
-  __shared__ uint64_t head[kBeamLists];  // the lists' first values
+  __shared__ uint64_t head[kBeamLists];  // the lists' first values, and their places
   __shared__ uint32_t head_at[kBeamLists];
   __shared__ uint64_t list[kMaxK * kMaxK + kRankPad];
   __shared__ uint32_t list_at[kMaxK * kMaxK + kRankPad];
-  __shared__ uint64_t wave_max[kThreads / 64];
+  __shared__ uint64_t best;
   __shared__ int found;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63;
   const int group = blockIdx.x;
+  if (tid == 0) {
+    best = 0;
+    found = 0;
+  }
+  __syncthreads();
   const int lists = a.W * a.S;
   const uint64_t* keys = a.keys + (int64_t)group * lists * a.K;
 
-  // The lists' first R entries are on their way while the normalisers are made: about
-  // four times as many as are looked for, so that their bound is near K's.
-  const int R = min(min(a.K, kBeamLists / lists), max(1, (4 * a.K + lists - 1) / lists));
-  const int heads = lists * R;
+  // The lists' first `kept` entries, on their way while the normalisers are made.
+  // The bound is looked for among the first R of a list, about four times as many as
+  // are wanted, so that it is near theirs.
+  const int kept = min(a.K, kBeamLists / lists), n_kept = lists * kept;
+  const int R = min(kept, max(1, (4 * a.K + lists - 1) / lists)), heads = lists * R;
   uint64_t raw[kHeads];
 #pragma unroll
   for (int c = 0; c < kHeads; ++c) {
     const int i = tid + c * kThreads;
-    raw[c] = i < heads ? keys[(int64_t)(i / R) * a.K + i % R] : 0;
+    raw[c] = i < n_kept ? keys[(int64_t)(i / kept) * a.K + i % kept] : 0;
   }
 
   // The beams' normalisers, kGroup lanes per beam.
   for (int w0 = 0; w0 < a.W; w0 += kThreads / kGroup) {
     const int w = w0 + tid / kGroup, sub = tid % kGroup;
     const int64_t row = (int64_t)group * a.W + w;
-    const bool there = w < a.W, ended = there && a.ended && a.ended[row];
-    const double score = there ? (double)a.scores[row] : 0.0;
-    double top = -INFINITY, sum = 0.0;
-    if (there && !ended) {
+    const bool there = w < a.W;
+    double top = -INFINITY, sum = 0.0, score = 0.0;
+    bool ended = false;
+    if (there) {
+      // (Of a beam that has ended, whatever the sums hold is not used.)
       const double2* sums = reinterpret_cast<const double2*>(a.sums) + row * a.S;
+      double2 next = sub < a.S ? sums[sub] : double2{-INFINITY, 0.0};
+      score = (double)a.scores[row];
+      ended = a.ended && a.ended[row];
       for (int s = sub; s < a.S; s += kGroup) {
-        const double2 x = sums[s];  // maximum, sum
+        const double2 x = next;  // maximum, sum
+        if (s + kGroup < a.S) next = sums[s + kGroup];
         if (x.x == top) {
           sum += x.x == -INFINITY ? 0.0 : x.y;
         } else if (x.x > top) {
@@ -293,19 +313,24 @@ __global__ __launch_bounds__(kThreads) void beam_finish_kernel(BeamLaunch a) {
       }
     }
     double all = top;
-#pragma unroll
-    for (int i = 1; i < kGroup; i *= 2) all = fmax(all, __shfl_xor(all, i));
+    all = fmax(all, row_turn<8>(all));
+    all = fmax(all, row_turn<4>(all));
+    all = fmax(all, row_turn<2>(all));
+    all = fmax(all, row_turn<1>(all));
     if (top != all) sum = all == INFINITY ? 0.0 : sum * exp(top - all);
-#pragma unroll
-    for (int i = 1; i < kGroup; i *= 2) sum += __shfl_xor(sum, i);
+    sum += row_turn<8>(sum);
+    sum += row_turn<4>(sum);
+    sum += row_turn<2>(sum);
+    sum += row_turn<1>(sum);
     if (there && sub == 0) {
       const bool finite = fabs(score) < INFINITY;
       mode[w] = !finite || (!ended && all == -INFINITY) ? kNone : ended ? kEnded : all == INFINITY ? kInfinite : kLogits;
       tops[w] = all;
       shift[w] = ended ? score : score - log(sum);
+      // The beam's best value: that of its largest logit.
+      if (mode[w] != kNone) atomicMax((unsigned long long*)&best, (unsigned long long)order_key(shift[w]));
     }
   }
-  if (tid == 0) found = 0;
   __syncthreads();
 
   // Entry r of list l, whose key is k: its value and its place, beam and token.
@@ -320,22 +345,16 @@ __global__ __launch_bounds__(kThreads) void beam_finish_kernel(BeamLaunch a) {
     if (kind == kInfinite) return x == INFINITY ? order_key(shift[w]) : 0;
     return order_key(((double)x - tops[w]) + shift[w]);
   };
-  uint64_t top = 0;
 #pragma unroll
   for (int c = 0; c < kHeads; ++c) {
     const int i = tid + c * kThreads;
-    if (c * kThreads >= heads) break;
+    if (i >= n_kept) break;
     uint32_t at = 0;
-    head[i] = i < heads ? entry(i / R, i % R, raw[c], at) : 0;
+    head[i] = entry(i / kept, i % kept, raw[c], at);
     head_at[i] = at;
-    top = max(top, head[i]);
   }
-#pragma unroll
-  for (int i = 1; i < 64; i *= 2) top = max(top, (uint64_t)__shfl_xor((unsigned long long)top, i));
-  if (lane == 0) wave_max[wave] = top;
   __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kThreads / 64; ++i) top = max(top, wave_max[i]);
+  const uint64_t top = best;
 
   // The bound of the heads (of equal values the first places).  Values are a few
   // units apart, 2^48 steps each.  (The list holds what follows `most` heads.)
@@ -345,34 +364,40 @@ __global__ __launch_bounds__(kThreads) void beam_finish_kernel(BeamLaunch a) {
   auto search = [&](auto n_c) {
     constexpr int N = decltype(n_c)::value;
     uint64_t k[N];
+    uint32_t at[N];
     int reach;
 #pragma unroll
-    for (int i = 0; i < N; ++i) k[i] = head[64 * i + lane];
+    for (int i = 0; i < N; ++i) {
+      const int x = 64 * i + lane, from = x / R * kept + x % R;
+      k[i] = x < heads ? head[from] : 0;
+      at[i] = x < heads ? head_at[from] : 0;
+    }
     bound = bound_of(k, top, (uint64_t)1 << 48, a.K, most, reach);
     if (reach > most) {
       uint32_t t[N];
 #pragma unroll
-      for (int i = 0; i < N; ++i) t[i] = k[i] > bound ? ~0u : k[i] == bound ? ~head_at[64 * i + lane] : 0;
+      for (int i = 0; i < N; ++i) t[i] = k[i] > bound ? ~0u : k[i] == bound ? ~at[i] : 0;
       tie = bound_of(t, ~0u, 1u << 20, a.K, a.K, reach);
     }
   };
-  if (heads <= kThreads) search(std::integral_constant<int, kThreads / 64>{});
+  if (heads <= 64) search(std::integral_constant<int, 1>{});
+  else if (heads <= kThreads) search(std::integral_constant<int, kThreads / 64>{});
   else search(std::integral_constant<int, kBeamLists / 64>{});
 
-  // What reaches it, and of the lists whose heads all do, what follows.
+  // What reaches it, and of the lists whose entries here all do, what follows.
   auto reaches = [&](uint64_t v, uint32_t at) { return v > bound || (v == bound && ~at >= tie); };
   auto add = [&](uint64_t v, uint32_t at) {
     const int i = atomicAdd(&found, 1);
     list[i] = v;
     list_at[i] = at;
   };
-  for (int i = tid; i < heads; i += kThreads) {
+  for (int i = tid; i < n_kept; i += kThreads) {
     if (!reaches(head[i], head_at[i])) continue;
     add(head[i], head_at[i]);
-    if (i % R != R - 1) continue;
-    for (int r = R; r < a.K; ++r) {
+    if (i % kept != kept - 1) continue;
+    for (int r = kept; r < a.K; ++r) {
       uint32_t at = 0;
-      const uint64_t v = entry(i / R, r, keys[(int64_t)(i / R) * a.K + r], at);
+      const uint64_t v = entry(i / kept, r, keys[(int64_t)(i / kept) * a.K + r], at);
       if (!reaches(v, at)) break;
       add(v, at);
     }

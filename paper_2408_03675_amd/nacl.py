@@ -550,13 +550,13 @@ def _launch(dev, call, *args):
 def _like(t, name, dev, shape, dtype):
     """_gpu's checks of a contiguous tensor in one expression, for calls where
     the host's time counts; what does not pass is reported by _gpu."""
-    if not (isinstance(t, torch.Tensor) and t.device == dev and t.shape == shape and t.dtype == dtype and t.is_contiguous()):
+    if not (isinstance(t, torch.Tensor) and t.device == dev and t.shape == shape and t.dtype is dtype and t.is_contiguous()):
         _gpu(t, name, dev, shape, dtype, contiguous=True)
 
 
 def _rows4(t, name, dev, shape, dtype):
     """A [., ., ., D] tensor with a contiguous last dimension; its strides."""
-    if not (isinstance(t, torch.Tensor) and t.device == dev and t.shape == shape and t.dtype == dtype):
+    if not (isinstance(t, torch.Tensor) and t.device == dev and t.shape == shape and t.dtype is dtype):
         _gpu(t, name, dev, shape, dtype)
     st = t.stride()
     if st[3] != 1:
@@ -609,6 +609,7 @@ class Step(_Keeper):
         self.q_shape, self.new_shape = (B, Hq, self.T, D), (B, H, self.T, D)
         self.cache_shape = (B, H, L, D)
         self.fits = (H, D, self.dtype)
+        self.rows, self.token_shape = torch.Size((B,)), torch.Size((B, self.T))
         self.k_stride, self.v_stride = tuple(prob.c.k_stride) + (1,), tuple(prob.c.v_stride) + (1,)
         s = _Step()
         s.T, s.row0 = self.T, int(row0)
@@ -736,7 +737,7 @@ def _rotation(prob, step, rotation, positions, dev):
     if positions is None:
         return rotation.with_stride(0), None
     per_row = positions.dim() == 2
-    _like(positions, "positions", dev, (prob.B, step.T) if per_row else (step.T,), torch.int32)
+    _like(positions, "positions", dev, step.token_shape if per_row else step.token_shape[1:], torch.int32)
     return rotation.with_stride(step.T if per_row else 0), positions.data_ptr()
 
 
@@ -881,15 +882,20 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, toke
 
 # Decoding over a paged cache, and beam search.
 
+_ONE = torch.Size((1,))
+
+
 def _table(t, name, dev, rows, entries=None):
     """A [B, entries] int32 table, rows of any stride; its row stride."""
     if not isinstance(t, torch.Tensor) or t.dim() != 2:
         raise ValueError(f"{name} must be [B, entries]")
-    _gpu(t, name, dev, (rows, t.shape[1] if entries is None else entries), torch.int32)
+    n, m = t.shape
     stride, one = t.stride()
-    if t.shape[1] > 1 and one != 1:
+    if not (t.dtype is torch.int32 and t.is_cuda and t.device == dev and n == rows and (entries is None or m == entries) and m):
+        _gpu(t, name, dev, (rows, m if entries is None else entries), torch.int32)
+    if m > 1 and one != 1:
         raise ValueError(f"{name} must have contiguous rows")
-    return stride if rows > 1 else max(stride, t.shape[1])
+    return stride if rows > 1 or stride > m else m
 
 
 class Pages(_Keeper):
@@ -938,29 +944,41 @@ def pages_assign(step, page, table, held, free, n_free, shared=None, held_out=No
     lib = _lib or load_library()
     prob = step.prob
     dev = getattr(table, "device", None)
-    x = _Pages()
-    x.table_stride = _table(table, "table", dev, prob.B)
+    stride = _table(table, "table", dev, prob.B)
     step.on(prob, dev)
-    if not isinstance(free, torch.Tensor) or free.dim() != 1:
-        raise ValueError("free must be [n_pages]")
-    if not 0 <= max(int(page), free.shape[0], table.shape[1]) < 2 ** 31 or int(page) < 0:
-        raise ValueError("pages, their rows and the table's entries must fit 32 bits")
-    x.n_pages, x.page, x.entries, x.table = free.shape[0], int(page), table.shape[1], table.data_ptr()
-    rows, one = (prob.B,), (1,)
-    _like(free, "free", dev, free.shape, torch.int32)
-    _like(held, "held", dev, rows, torch.int32)
-    _like(n_free, "n_free", dev, one, torch.int32)
+    rows, tokens, i32, page = step.rows, step.token_shape, torch.int32, int(page)
+    if held_out is None:
+        held_out = torch.empty(rows, dtype=i32, device=dev)
+    if n_free_out is None:
+        n_free_out = torch.empty(_ONE, dtype=i32, device=dev)
+    if slots is None:
+        slots = torch.empty(tokens, dtype=i32, device=dev)
+    if missing is None:
+        missing = torch.empty(_ONE, dtype=i32, device=dev)
+    try:
+        good = (free.dtype is i32 and free.device == dev and free.is_contiguous() and free.dim() == 1 and
+                held.dtype is i32 and held.device == dev and held.shape == rows and held.is_contiguous() and
+                n_free.dtype is i32 and n_free.device == dev and n_free.shape == _ONE and
+                held_out.dtype is i32 and held_out.device == dev and held_out.shape == rows and held_out.is_contiguous() and
+                n_free_out.dtype is i32 and n_free_out.device == dev and n_free_out.shape == _ONE and
+                slots.dtype is i32 and slots.device == dev and slots.shape == tokens and slots.is_contiguous() and
+                missing.dtype is i32 and missing.device == dev and missing.shape == _ONE)
+    except AttributeError:
+        good = False
+    if not good:
+        if not isinstance(free, torch.Tensor) or free.dim() != 1:
+            raise ValueError("free must be [n_pages]")
+        for x, name, shape in ((free, "free", free.shape), (held, "held", rows), (n_free, "n_free", _ONE),
+                               (held_out, "held_out", rows), (n_free_out, "n_free_out", _ONE), (slots, "slots", tokens),
+                               (missing, "missing", _ONE)):
+            _gpu(x, name, dev, shape, i32, contiguous=True)
     if shared is not None:
-        _like(shared, "shared", dev, rows, torch.int32)
-    outs = []
-    for t, name, shape in ((held_out, "held_out", rows), (n_free_out, "n_free_out", one), (slots, "slots", (prob.B, step.T)),
-                           (missing, "missing", one)):
-        if t is None:
-            t = torch.empty(shape, dtype=torch.int32, device=dev)
-        else:
-            _like(t, name, dev, shape, torch.int32)
-        outs.append(t)
-    held_out, n_free_out, slots, missing = outs
+        _like(shared, "shared", dev, rows, i32)
+    n_pages, entries = free.shape[0], table.shape[1]
+    if not 0 <= page < 2 ** 31 or n_pages >= 2 ** 31 or entries >= 2 ** 31:
+        raise ValueError("pages, their rows and the table's entries must fit 32 bits")
+    x = _Pages(n_pages, page, entries, stride)
+    x.table = table.data_ptr()
     _launch(dev, lib.nacl_pages_assign, prob.ref(), step.c, x, held.data_ptr(), None if shared is None else shared.data_ptr(),
             free.data_ptr(), n_free.data_ptr(), held_out.data_ptr(), n_free_out.data_ptr(), slots.data_ptr(),
             missing.data_ptr())
@@ -974,12 +992,12 @@ def paged_append(prob, step, rotation, positions, q_new, k_new, v_new, pages, sl
     dev = pages.on(prob)
     step.on(prob, dev)
     r, pos = _rotation(prob, step, rotation, positions, dev)
-    dt = step.dtype
-    _like(slots, "slots", dev, (prob.B, step.T), torch.int32)
+    dt, q_shape, new_shape = step.dtype, step.q_shape, step.new_shape
+    _like(slots, "slots", dev, step.token_shape, torch.int32)
     if q_out is None:
-        q_out = torch.empty(step.q_shape, dtype=dt, device=dev)
-    s = step.strided(_rows4(q_new, "q_new", dev, step.q_shape, dt), _rows4(k_new, "k_new", dev, step.new_shape, dt),
-                     _rows4(v_new, "v_new", dev, step.new_shape, dt), _rows4(q_out, "q_out", dev, step.q_shape, dt))
+        q_out = torch.empty(q_shape, dtype=dt, device=dev)
+    s = step.strided(_rows4(q_new, "q_new", dev, q_shape, dt), _rows4(k_new, "k_new", dev, new_shape, dt),
+                     _rows4(v_new, "v_new", dev, new_shape, dt), _rows4(q_out, "q_out", dev, q_shape, dt))
     _launch(dev, lib.nacl_paged_append, prob.ref(), s, r, pos, q_new.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), pages.c,
             slots.data_ptr(), q_out.data_ptr())
     return q_out
@@ -1053,33 +1071,35 @@ def beam_select(logits, scores, K, ended=None, end_token=0, parents=None, tokens
         _gpu(logits, "logits", dev)
     if not isinstance(scores, torch.Tensor) or scores.dim() != 2 or scores.numel() != N:
         raise ValueError("scores must be [B, W] for logits of [B * W, V]")
-    B, W = scores.shape
+    group = scores.shape
+    B, W = group
+    K, end_token = int(K), int(end_token)
+    if N >= 2 ** 31 or V >= 2 ** 31 or not 0 <= K < 2 ** 31:
+        raise ValueError("B, W, V and K must fit 32 bits")
     stride, one = logits.stride()
     if V > 1 and one != 1:
         raise ValueError("logits must have a contiguous last dimension")
     if N > 1 and stride < V:
         raise ValueError("rows of logits must not overlap")
-    _like(scores, "scores", dev, scores.shape, torch.float32)
-    d = _beams(B, W, V, int(K))
-    d.dtype = NACL_F32 if logits.dtype == torch.float32 else NACL_BF16
-    if N > 1:
-        d.stride = stride
+    _like(scores, "scores", dev, group, torch.float32)
+    d = _Beams(B, W, V, K, NACL_F32 if logits.dtype is torch.float32 else NACL_BF16, stride if N > 1 else V)
     if ended is not None:
-        _like(ended, "ended", dev, scores.shape, torch.int32)
-        if not 0 <= int(end_token) < V:
+        _like(ended, "ended", dev, group, torch.int32)
+        if not 0 <= end_token < V:
             raise ValueError(f"end_token must lie in [0, {V})")
-        d.ended, d.end_token = ended.data_ptr(), int(end_token)
-    shape = (B, int(K))
+        d.ended, d.end_token = ended.data_ptr(), end_token
+    shape, i32, f32 = torch.Size((B, K)), torch.int32, torch.float32
+    if parents is None:
+        parents = torch.empty(shape, dtype=i32, device=dev)
+    if tokens is None:
+        tokens = torch.empty(shape, dtype=i32, device=dev)
+    if out is None:
+        out = torch.empty(shape, dtype=f32, device=dev)
     if ws is None:
-        ws = beam_workspace(B, W, V, int(K), dev)
-    outs = []
-    for t, name, dtype in ((parents, "parents", torch.int32), (tokens, "tokens", torch.int32), (out, "out", torch.float32)):
-        if t is None:
-            t = torch.empty(shape, dtype=dtype, device=dev)
-        else:
-            _like(t, name, dev, shape, dtype)
-        outs.append(t)
-    parents, tokens, out = outs
+        ws = beam_workspace(B, W, V, K, dev)
+    _like(parents, "parents", dev, shape, i32)
+    _like(tokens, "tokens", dev, shape, i32)
+    _like(out, "out", dev, shape, f32)
     n = ws.numel()
     _like(ws, "ws", dev, (n,), torch.uint8)
     _launch(dev, lib.nacl_beam_select, d, logits.data_ptr(), scores.data_ptr(), parents.data_ptr(), tokens.data_ptr(),
@@ -1096,25 +1116,26 @@ def beam_reorder(prob, pages, parents, lens, held=None, table_out=None, lens_out
     dev = pages.on(prob)
     if not isinstance(parents, torch.Tensor) or parents.dim() != 2 or parents.numel() != prob.B:
         raise ValueError("parents must be [B / W, W]")
-    _like(parents, "parents", dev, parents.shape, torch.int32)
-    rows = (prob.B,)
-    _like(lens, "lens", dev, rows, torch.int32)
+    i32, rows = torch.int32, torch.Size((prob.B,))
+    _like(parents, "parents", dev, parents.shape, i32)
+    _like(lens, "lens", dev, rows, i32)
     if held is None:
         if held_out is not None:
             raise ValueError("held_out needs held")
     else:
-        _like(held, "held", dev, rows, torch.int32)
+        _like(held, "held", dev, rows, i32)
         if held_out is None:
             held_out = torch.empty_like(held)
         else:
-            _like(held_out, "held_out", dev, rows, torch.int32)
+            _like(held_out, "held_out", dev, rows, i32)
+    entries = pages.c.entries
     if table_out is None:
-        table_out = torch.empty((prob.B, pages.c.entries), dtype=torch.int32, device=dev)
-    stride = _table(table_out, "table_out", dev, prob.B, pages.c.entries)
+        table_out = torch.empty((prob.B, entries), dtype=i32, device=dev)
+    stride = _table(table_out, "table_out", dev, prob.B, entries)
     if lens_out is None:
         lens_out = torch.empty_like(lens)
     else:
-        _like(lens_out, "lens_out", dev, rows, torch.int32)
+        _like(lens_out, "lens_out", dev, rows, i32)
     _launch(dev, lib.nacl_beam_reorder, prob.ref(), pages.c, parents.shape[1], parents.data_ptr(), lens.data_ptr(),
             None if held is None else held.data_ptr(), table_out.data_ptr(), stride, lens_out.data_ptr(),
             None if held_out is None else held_out.data_ptr())
