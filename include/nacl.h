@@ -482,8 +482,8 @@ size_t nacl_beam_workspace_bytes(const nacl_beams* d);
  * values (-infinity past fp32's range); where there are fewer than K, -1, -1 and
  * -infinity follow.
  * logits: device [B * W, V], element alignment; scores: device fp32 [B, W].
- * Exponentials are fp32, their sums and the values fp64 in an order that V and the
- * row's alignment fix.  V at most NACL_MAX_V, and W times the row's slices
+ * Exponentials are fp32, sums of 32 of them too, further sums and the values fp64, in
+ * an order that B, W and V fix: equal rows have equal values.  V at most NACL_MAX_V, and W times the row's slices
  * of 8192 tokens at most 1024 (about 2^23 tokens in a group). */
 int nacl_beam_select(const nacl_beams* d, const void* logits, const float* scores, int32_t* parents,
                      int32_t* tokens, float* out, void* ws, size_t ws_bytes, void* stream);

@@ -22,8 +22,10 @@ namespace nacl {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPer = kBeamSlice / kThreads;  // tokens per thread of a slice
 constexpr int kMaxK = 64;
+// Keys that may reach a bound before it is looked for more closely: each costs a
+// place in a list, each round of the search some 100 cycles.
+__host__ __device__ constexpr int most_of(int K) { return K + K / 4 + 2; }
 
 __device__ __forceinline__ float of_order_key(uint32_t k) {
   return __uint_as_float((k & 0x80000000u) ? k & 0x7FFFFFFFu : ~k);
@@ -75,12 +77,9 @@ __device__ __forceinline__ K bound_of(const K (&key)[N], K top, K step, int want
   return top - d;
 }
 
-constexpr int kRankPad = 3;  // zeros behind a list that is read by fours
-
 // ---------------------------------------------------------------------------
-// Slices.  A thread takes kPer tokens as 16-byte pieces; the piece's place is its
-// address's, so that rows of any alignment are read by aligned loads (the row's
-// first and last pieces by elements).
+// Slices.  A thread takes kPer tokens as pieces of 16 bytes, at any alignment of the
+// row, so that a row's result depends on its logits alone (equal beams tie).
 
 template <typename T>
 struct Piece;
@@ -88,7 +87,8 @@ template <>
 struct Piece<__bf16> {
   static constexpr int kN = 8;
   static __device__ __forceinline__ void load(const __bf16* p, float (&x)[8]) {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+    typedef uint32_t words __attribute__((ext_vector_type(4), aligned(2)));
+    const words w = *reinterpret_cast<const words*>(p);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       x[2 * i] = __uint_as_float(w[i] << 16);
@@ -100,7 +100,8 @@ template <>
 struct Piece<float> {
   static constexpr int kN = 4;
   static __device__ __forceinline__ void load(const float* p, float (&x)[4]) {
-    const f32x4 w = *reinterpret_cast<const f32x4*>(p);
+    typedef float words __attribute__((ext_vector_type(4), aligned(4)));
+    const words w = *reinterpret_cast<const words*>(p);
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = w[i];
   }
@@ -109,12 +110,12 @@ struct Piece<float> {
 constexpr uint32_t kLeast = 0x00800000u;  // key of the lowest finite number
 constexpr float kLog2e = 1.44269504f;
 
-template <typename T>
+// kPer tokens per thread.
+template <typename T, int kPer>
 __global__ __launch_bounds__(kThreads) void beam_slices_kernel(BeamLaunch a) {
   using P = Piece<T>;
-  constexpr int kPieces = kPer / P::kN;
-  // Logits that reach the bound, of kMaxK threads at most.
-  __shared__ uint64_t list[kMaxK * kPer + kRankPad];
+  constexpr int kPieces = kPer / P::kN, kSlice = kPer * kThreads;
+  __shared__ uint64_t list[most_of(kMaxK) * kPer];  // logits that reach the bound
   __shared__ uint32_t maxima[kThreads];
   __shared__ float wave_max[kThreads / 64];
   __shared__ double wave_sum[kThreads / 64];
@@ -123,43 +124,57 @@ __global__ __launch_bounds__(kThreads) void beam_slices_kernel(BeamLaunch a) {
   const int row = blockIdx.y, slice = blockIdx.x;
   if (a.ended && a.ended[row]) return;  // its one continuation needs no logits
   const T* x0 = reinterpret_cast<const T*>(a.logits) + (int64_t)row * a.stride;
-  const int head = (int)(((uintptr_t)x0 & 15) / sizeof(T));  // tokens by which the pieces start before the row
-  const int first = slice * kBeamSlice - head;
+  const int first = slice * kSlice;
   auto token = [&](int u, int i) { return first + (u * kThreads + tid) * P::kN + i; };
 
   float x[kPieces][P::kN];
-  if (first >= 0 && first + kBeamSlice <= a.V) {
+  if (first + kSlice <= a.V) {
 #pragma unroll
     for (int u = 0; u < kPieces; ++u) P::load(x0 + token(u, 0), x[u]);
   } else {
+    // What lies past the row's end is -infinity.  A piece of which that is a part is
+    // loaded by elements, after the whole ones are under way together (in the place
+    // of the others, the row's first).
+#pragma unroll
+    for (int u = 0; u < kPieces; ++u)
+      if (a.V >= P::kN) P::load(x0 + (token(u, 0) + P::kN <= a.V ? token(u, 0) : 0), x[u]);
 #pragma unroll
     for (int u = 0; u < kPieces; ++u) {
-      const int at = token(u, 0);
-      if (at >= 0 && at + P::kN <= a.V) {
-        P::load(x0 + at, x[u]);
-      } else {
+      if (token(u, 0) + P::kN <= a.V) continue;
 #pragma unroll
-        for (int i = 0; i < P::kN; ++i) x[u][i] = (uint32_t)(at + i) < (uint32_t)a.V ? (float)x0[at + i] : -INFINITY;
-      }
+      for (int i = 0; i < P::kN; ++i) x[u][i] = -INFINITY;
+      if (token(u, 0) >= a.V) continue;
+#pragma unroll
+      for (int i = 0; i < P::kN; ++i)
+        if (token(u, i) < a.V) x[u][i] = (float)x0[token(u, i)];
     }
   }
   if (tid == 0) found = 0;
 
   // The thread's maximum and its exponentials' sum against it, of kPer terms in
-  // fp32.  A NaN among the logits, or nothing but infinities, makes the sum a NaN.
+  // fp32, as powers of two of x log2(e) - c with c = m log2(e) rounded, from which the
+  // sum is freed afterwards (c's own rounding, in front of all terms alike).
   float m = -INFINITY, sum = 0.f;
 #pragma unroll
   for (int u = 0; u < kPieces; ++u)
 #pragma unroll
-    for (int i = 0; i < P::kN; ++i) m = x[u][i] > m ? x[u][i] : m;
+    for (int i = 0; i < P::kN; i += 2) asm("v_max3_f32 %0, %0, %1, %2" : "+v"(m) : "v"(x[u][i]), "v"(x[u][i + 1]));
+  const float c = m * kLog2e;
 #pragma unroll
   for (int u = 0; u < kPieces; ++u)
 #pragma unroll
-    for (int i = 0; i < P::kN; ++i) sum += __builtin_amdgcn_exp2f((x[u][i] - m) * kLog2e);
-  if (!(sum == sum)) {
-    // A NaN counts as -infinity; infinite logits share a row, one each, and the
-    // others are nothing beside them.
+    for (int i = 0; i < P::kN; ++i) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(x[u][i], kLog2e, -c));
+  sum *= __builtin_amdgcn_exp2f(-__builtin_fmaf(m, kLog2e, -c));
+  if (!(sum == sum && __builtin_fabsf(m) < 0x1p20f)) {
+    // A NaN among the logits, no finite maximum, or one next to which c's rounding
+    // is not small.  A NaN counts as -infinity; infinite logits share a row, one
+    // each, and the others are nothing beside them.
+    m = -INFINITY;
     sum = 0.f;
+#pragma unroll
+    for (int u = 0; u < kPieces; ++u)
+#pragma unroll
+      for (int i = 0; i < P::kN; ++i) m = x[u][i] > m ? x[u][i] : m;
 #pragma unroll
     for (int u = 0; u < kPieces; ++u)
 #pragma unroll
@@ -191,7 +206,7 @@ __global__ __launch_bounds__(kThreads) void beam_slices_kernel(BeamLaunch a) {
   for (int i = 0; i < kThreads / 64; ++i) key[i] = maxima[lane + 64 * i];
   int reach;
   const uint32_t top_key = top == -INFINITY ? 0 : float_order_key(top + 0.f);
-  const int most = min(2 * a.K, kMaxK);
+  const int most = most_of(a.K);
   const uint32_t bound = bound_of(key, top_key, 1u << 20, a.K, most, reach);
   uint32_t tie = 0;  // of the logits equal to the bound, those whose ~token reaches it
   __syncthreads();  // the maxima are read
@@ -232,14 +247,12 @@ __global__ __launch_bounds__(kThreads) void beam_slices_kernel(BeamLaunch a) {
   }
   __syncthreads();
   const int n = found;
-  if (tid < kRankPad) list[n + tid] = 0;
-  __syncthreads();
   uint64_t* out = a.keys + slot * a.K;
   for (int i = tid; i < n; i += kThreads) {
     const uint64_t k = list[i];
     int rank = 0;
-    for (int j = 0; j < n; j += 4)
-      rank += (list[j] > k) + (list[j + 1] > k) + (list[j + 2] > k) + (list[j + 3] > k);
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) rank += list[j] > k;
     if (rank < a.K) out[rank] = k;
   }
   for (int i = n + tid; i < a.K; i += kThreads) out[i] = 0;
@@ -260,8 +273,8 @@ __global__ __launch_bounds__(kThreads) void beam_finish_kernel(BeamLaunch a) {
   __shared__ int mode[kMaxK];
   __shared__ uint64_t head[kBeamLists];  // the lists' first values, and their places
   __shared__ uint32_t head_at[kBeamLists];
-  __shared__ uint64_t list[kMaxK * kMaxK + kRankPad];
-  __shared__ uint32_t list_at[kMaxK * kMaxK + kRankPad];
+  __shared__ uint64_t list[kMaxK * kMaxK];
+  __shared__ uint32_t list_at[kMaxK * kMaxK];
   __shared__ uint64_t best;
   __shared__ int found;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -277,8 +290,9 @@ __global__ __launch_bounds__(kThreads) void beam_finish_kernel(BeamLaunch a) {
   // The lists' first `kept` entries, on their way while the normalisers are made.
   // The bound is looked for among the first R of a list, about four times as many as
   // are wanted, so that it is near theirs.
-  const int kept = min(a.K, kBeamLists / lists), n_kept = lists * kept;
-  const int R = min(kept, max(1, (4 * a.K + lists - 1) / lists)), heads = lists * R;
+  const int enough = max(1, (4 * a.K + lists - 1) / lists);
+  const int kept = min(min(a.K, kBeamLists / lists), max(4, 4 * enough)), n_kept = lists * kept;
+  const int R = min(kept, enough), heads = lists * R;
   uint64_t raw[kHeads];
 #pragma unroll
   for (int c = 0; c < kHeads; ++c) {
@@ -360,7 +374,7 @@ __global__ __launch_bounds__(kThreads) void beam_finish_kernel(BeamLaunch a) {
   // units apart, 2^48 steps each.  (The list holds what follows `most` heads.)
   uint64_t bound = 1;
   uint32_t tie = 0;
-  const int most = R > 1 || 2 * a.K * a.K <= kMaxK * kMaxK ? 2 * a.K : a.K;
+  const int most = R > 1 || most_of(a.K) * a.K <= kMaxK * kMaxK ? most_of(a.K) : a.K;
   auto search = [&](auto n_c) {
     constexpr int N = decltype(n_c)::value;
     uint64_t k[N];
@@ -403,17 +417,21 @@ __global__ __launch_bounds__(kThreads) void beam_finish_kernel(BeamLaunch a) {
     }
   }
   __syncthreads();
+  // Eight lanes rank one of them.
   const int n = found;
-  if (tid < kRankPad) list[n + tid] = 0;
-  __syncthreads();
-  for (int i = tid; i < n; i += kThreads) {
+  for (int i = tid / 8; i < n; i += kThreads / 8) {
     const uint64_t v = list[i];
     const uint32_t at = list_at[i];
     int rank = 0;
-    for (int j = 0; j < n; j += 4)
+#pragma unroll 4
+    for (int j = tid % 8; j < n; j += 8) {
+      const uint64_t v2 = list[j];
+      const uint32_t at2 = list_at[j];
+      rank += (int)((v2 > v) | ((v2 == v) & (at2 < at)));
+    }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) rank += list[j + e] > v || (list[j + e] == v && list_at[j + e] < at);
-    if (rank < a.K) {
+    for (int x = 1; x < 8; x *= 2) rank += __shfl_xor(rank, x);
+    if (rank < a.K && tid % 8 == 0) {
       const int64_t to = (int64_t)group * a.K + rank;
       a.parents[to] = (int)(at >> 20);
       a.tokens[to] = (int)(at & 0xFFFFFu);
@@ -431,8 +449,14 @@ __global__ __launch_bounds__(kThreads) void beam_finish_kernel(BeamLaunch a) {
 
 hipError_t launch_beam(const BeamLaunch& a, int dtype, hipStream_t stream) {
   const dim3 grid((unsigned)a.S, (unsigned)(a.B * a.W));
-  if (dtype == NACL_F32) beam_slices_kernel<float><<<grid, kThreads, 0, stream>>>(a);
-  else beam_slices_kernel<__bf16><<<grid, kThreads, 0, stream>>>(a);
+  auto run = [&](auto kernel) { kernel<<<grid, kThreads, 0, stream>>>(a); };
+  if (a.slice == kBeamSmallSlice) {
+    if (dtype == NACL_F32) run(beam_slices_kernel<float, kBeamSmallSlice / kThreads>);
+    else run(beam_slices_kernel<__bf16, kBeamSmallSlice / kThreads>);
+  } else {
+    if (dtype == NACL_F32) run(beam_slices_kernel<float, kBeamSlice / kThreads>);
+    else run(beam_slices_kernel<__bf16, kBeamSlice / kThreads>);
+  }
   if (hipError_t e = hipGetLastError()) return e;
   beam_finish_kernel<<<a.B, kThreads, 0, stream>>>(a);
   return hipGetLastError();

@@ -322,10 +322,11 @@ struct ReorderLaunch {
 hipError_t launch_reorder(ReorderLaunch a, int dtype, int D, int cus, hipStream_t stream);
 
 // The best continuations of every group's beams (beam.hip).
-constexpr int kBeamSlice = 8192;   // tokens per work-group
+constexpr int kBeamSlice = 8192, kBeamSmallSlice = 2048;  // tokens per work-group
 constexpr int kBeamLists = 1024;   // slices of a group's beams at most
 struct BeamLaunch {
-  int B, W, V, K, S;
+  int B, W, V, K;
+  int slice, S;                  // tokens per work-group, slices per row
   int64_t stride;
   const void* logits;
   const float* scores;

@@ -39,9 +39,15 @@ Extent table_extent(const void* base, int64_t stride, int64_t B, int64_t entries
   return words(base, (B - 1) * stride + entries);
 }
 
-// Slices of a row's logits: pieces of 16 bytes, the first of which starts up to 7
-// tokens before the row.
-int beam_slices(const nacl_beams* d) { return (int)(((int64_t)d->V + 7 + kBeamSlice - 1) / kBeamSlice); }
+// Small slices where large ones leave compute units without one and the small ones'
+// lists are still a few (4 beams of 32000 tokens: the kernels 4.7 + 4.6 us, by large ones
+// 6.2 + 4.2; 8 of 131072, whose small slices are 512: 5.7 + 9.4 and 6.8 + 6.7).
+int beam_slice(const nacl_beams* d) {
+  auto slices = [&](int n) { return ((int64_t)d->V + n - 1) / n; };
+  const bool small = d->B * d->W * slices(kBeamSlice) < kPlanCus && d->W * slices(kBeamSmallSlice) <= kBeamLists / 4;
+  return small ? kBeamSmallSlice : kBeamSlice;
+}
+int beam_slices(const nacl_beams* d) { return (d->V + beam_slice(d) - 1) / beam_slice(d); }
 
 int check_beams(const nacl_beams* d) {
   if (!d) return fail_status(NACL_ERR_INVALID_ARG, "beams are NULL");
@@ -50,7 +56,7 @@ int check_beams(const nacl_beams* d) {
   if (d->W > NACL_MAX_W || d->K > NACL_MAX_W) return fail_status(NACL_ERR_UNSUPPORTED, "W or K exceeds %d", NACL_MAX_W);
   if ((int64_t)d->B * d->W > 65535) return fail_status(NACL_ERR_UNSUPPORTED, "B * W exceeds 65535");
   if (d->V > NACL_MAX_V) return fail_status(NACL_ERR_UNSUPPORTED, "V = %d exceeds %d", d->V, NACL_MAX_V);
-  if (d->W * beam_slices(d) > kBeamLists)
+  if ((int64_t)d->W * beam_slices(d) > kBeamLists)
     return fail_status(NACL_ERR_UNSUPPORTED, "a group of %d beams of %d slices, at most %d in all", d->W, beam_slices(d), kBeamLists);
   if (d->dtype != NACL_F32 && d->dtype != NACL_BF16) return fail_status(NACL_ERR_INVALID_ARG, "unknown dtype %d", d->dtype);
   if (d->stride < d->V) return fail_status(NACL_ERR_INVALID_ARG, "the row stride must be at least V");
@@ -198,9 +204,8 @@ int nacl_beam_select(const nacl_beams* d, const void* logits, const float* score
   a.W = d->W;
   a.V = d->V;
   a.K = d->K;
-  // (Where every row starts at 16 bytes, its pieces start with it.)
-  const bool straight = aligned(logits, 16) && (rows == 1 || d->stride * eb % 16 == 0);
-  a.S = straight ? (d->V + kBeamSlice - 1) / kBeamSlice : beam_slices(d);
+  a.slice = beam_slice(d);
+  a.S = beam_slices(d);
   a.stride = d->stride;
   a.logits = logits;
   a.scores = scores;

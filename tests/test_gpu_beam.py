@@ -137,19 +137,18 @@ def test_select_from_strided_rows(dtype):
         wide = torch.full((B * W * (V + gap) + lead + 16,), 1e4, dtype=DT[dtype], device=DEV)
         rows = wide[lead:lead + B * W * (V + gap)].view(B * W, V + gap)[:, :V]
         rows.copy_(logits)
-        got = nacl.beam_select(rows, scores, K)
-        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
-        _check(rows, scores, K, got)
+        for x, y in zip(nacl.beam_select(rows, scores, K), want):
+            assert torch.equal(x, y)
 
 
 def test_select_again_and_in_halves():
     """The same call gives the same bits, and a group's result does not depend on the
     others."""
-    logits, scores = _make(6, 5, 70001, "f32")
+    logits, scores = _make(40, 5, 70001, "f32")
     a, b = nacl.beam_select(logits, scores, 10), nacl.beam_select(logits, scores, 10)
-    half = nacl.beam_select(logits[15:].clone(), scores[3:].contiguous(), 10)
+    half = nacl.beam_select(logits[75:].clone(), scores[15:].contiguous(), 10)
     for x, y, z in zip(a, b, half):
-        assert torch.equal(x, y) and (torch.equal(x[3:], z) or x.dtype == torch.float32)
+        assert torch.equal(x, y) and torch.equal(x[15:], z)
 
 
 # --------------------------------------------------------------------------
