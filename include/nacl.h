@@ -400,7 +400,7 @@ int nacl_sample(const nacl_draw* d, const void* logits, const float* u, int32_t*
 
 typedef struct nacl_pages {
   int32_t n_pages, page;   /* pages of the pool and rows per page; n_pages * page below 2^31 */
-  int32_t entries;         /* pages per sequence that the table has room for */
+  int32_t entries;         /* pages per sequence that the table has room for, at most 2^20 */
   int64_t table_stride;    /* elements between two sequences' entries, at least entries */
   int64_t k_stride[3];     /* element strides of the pools for page, h, row; multiples of 16 bytes */
   int64_t v_stride[3];

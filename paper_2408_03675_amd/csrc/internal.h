@@ -300,7 +300,7 @@ struct AssignLaunch {
   int32_t* slots;
   int32_t* missing;              // or nullptr
 };
-hipError_t launch_assign(const AssignLaunch& a, hipStream_t stream);
+hipError_t launch_assign(const AssignLaunch& a, int cus, hipStream_t stream);
 
 // What beams hold, taken over from their parents (pages.hip).
 struct ReorderLaunch {

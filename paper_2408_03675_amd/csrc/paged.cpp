@@ -112,7 +112,7 @@ int nacl_pages_assign(const nacl_problem* p, const nacl_step* s, const nacl_page
   a.n_free_out = n_free_out;
   a.slots = slots;
   a.missing = missing;
-  return launched(nacl::launch_assign(a, static_cast<hipStream_t>(stream)), "page kernels");
+  return launched(nacl::launch_assign(a, kPlanCus, static_cast<hipStream_t>(stream)), "page kernels");
 }
 
 size_t nacl_paged_workspace_bytes(const nacl_problem* p, const nacl_step* s, const nacl_pages* x) {

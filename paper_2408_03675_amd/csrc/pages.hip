@@ -10,141 +10,230 @@ namespace nacl {
 namespace {
 
 // ---------------------------------------------------------------------------
-// nacl_pages_assign.  One work-group takes the sequences 1024 at a time: the
-// pages to give back and to take are counted per sequence, a scan over the
-// sequences gives each its run of the stack, and the pages themselves are moved
-// by all threads together, a thread finding its page's sequence in the scanned
-// counts (a sequence that ended gives hundreds back, most take none).
+// nacl_pages_assign.  A thread per sequence counts the pages that it gives back or
+// takes; a scan over the sequences gives each its run of the stack.  The pages are
+// moved by all threads together, a thread finding its page's sequence in the
+// scanned counts (a sequence that ended gives hundreds back, most take none).
 
-constexpr int kAssignThreads = 1024;
-constexpr int kAssignSlots = 16384;  // slots that the same launch writes
+constexpr int kAssignSeqs = 1024;     // sequences of a work-group
 
-// The rows that sequence b holds before and after the step.
-__device__ __forceinline__ int64_t rows_before(const AssignLaunch& a, int b) {
-  return (int64_t)a.row0 + (a.lens ? a.lens[b] : 0);
+// What sequence b holds before the step, what it is to get.
+struct Sequence {
+  int64_t rows;       // before
+  int fresh;          // new tokens
+  int held, wanted;   // pages
+  int keeps;          // entries below do not go back
+};
+__device__ __forceinline__ Sequence sequence(const AssignLaunch& a, int b) {
+  Sequence s;
+  const int shared = a.shared ? a.shared[b] : 0, held = a.held[b];
+  s.rows = (int64_t)a.row0 + (a.lens ? a.lens[b] : 0);
+  s.fresh = a.n_new ? max(0, min(a.T, a.n_new[b])) : a.T;
+  const int64_t after = max((int64_t)0, min(s.rows + s.fresh, (int64_t)a.L));
+  s.wanted = (int)min((int64_t)a.entries, (after + a.page - 1) / a.page);
+  s.held = max(0, min(a.entries, held));
+  s.keeps = max(s.wanted, shared);
+  return s;
 }
-__device__ __forceinline__ int new_of(const AssignLaunch& a, int b) {
-  return a.n_new ? max(0, min(a.T, a.n_new[b])) : a.T;
-}
-__device__ __forceinline__ int pages_wanted(const AssignLaunch& a, int b) {
-  int64_t rows = rows_before(a, b) + new_of(a, b);
-  rows = rows < 0 ? 0 : rows > a.L ? a.L : rows;
-  return (int)min((int64_t)a.entries, (rows + a.page - 1) / a.page);
-}
-__device__ __forceinline__ int pages_held(const AssignLaunch& a, int b) { return max(0, min(a.entries, a.held[b])); }
-
-// The slot of token t of sequence b, whose pages are in place.
-__device__ __forceinline__ int slot_of(const AssignLaunch& a, int b, int t) {
-  const int64_t row = rows_before(a, b) + t;
-  if (t >= new_of(a, b) || row < 0 || row >= a.L) return -1;
-  const int entry = (int)row / a.page;
-  if (entry >= a.held_out[b]) return -1;
-  const int page = a.table[(int64_t)b * a.table_stride + entry];
-  return (uint32_t)page < (uint32_t)a.n_pages ? page * a.page + (int)row % a.page : -1;
+__device__ __forceinline__ int stack_of(const AssignLaunch& a) { return max(0, min(a.n_pages, a.n_free[0])); }
+__device__ __forceinline__ int in_pool(const AssignLaunch& a, int page, int row) {
+  return (uint32_t)page < (uint32_t)a.n_pages ? page * a.page + row % a.page : -1;
 }
 
-// Sums of x over the threads up to and with this one, and over all.
-__device__ __forceinline__ int64_t scan(int64_t x, int64_t* waves, int64_t& all) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int i = 1; i < 64; i *= 2) {
-    const int64_t y = __shfl_up(x, i);
-    if (lane >= i) x += y;
-  }
-  __syncthreads();  // the last call's sums are read
-  if (lane == 63) waves[wave] = x;
-  __syncthreads();
-  int64_t before = 0;
-  all = 0;
-  for (int i = 0; i < (int)(blockDim.x >> 6); ++i) {
-    if (i < wave) before += waves[i];
-    all += waves[i];
-  }
-  return x + before;
+// Sums over the wave's lanes up to and with this one.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);  // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // row_bcast 15, 31
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+  return x;
 }
 
 // The first of n ascending sums that exceeds i.
-__device__ __forceinline__ int owner_of(const int64_t* sums, int n, int64_t i) {
+template <int N>
+__device__ __forceinline__ int owner_of(const int* sums, int n, int i) {
   int lo = 0;
-  for (int step = kAssignThreads / 2; step; step /= 2)
+  for (int step = N / 2; step; step /= 2)
     if (lo + step <= n && sums[lo + step - 1] <= i) lo += step;
   return lo;
 }
 
-__global__ __launch_bounds__(kAssignThreads) void assign_kernel(AssignLaunch a, int with_slots) {
-  __shared__ int64_t sums[kAssignThreads], waves[kAssignThreads / 64];
-  __shared__ int first[kAssignThreads];  // of each sequence's entries that change hands
-  __shared__ int64_t granted_all;
-  const int tid = threadIdx.x;
-  const int64_t in_stack = max(0, min(a.n_pages, a.n_free[0]));
+// The sequences [b0, b0 + n) of a step, n at most N: their counts and scanned sums
+// (of at most 1024 times 2^20 pages).
+template <int N>
+struct Counts {
+  int gives[N], takes[N];  // sums up to and with each
+  int first[N];            // entry of the first page that changes hands
+  int waves[2][N / 64];
+  int granted;             // sum of the takes that the stack has pages for
 
-  // Pages back to the stack: entries [max(wanted, shared), held).
-  int64_t given = 0;
-  for (int b0 = 0; b0 < a.B; b0 += kAssignThreads) {
-    const int b = b0 + tid, n = min(kAssignThreads, a.B - b0);
-    int gives = 0, from = 0;
-    if (tid < n) {
-      from = max(pages_wanted(a, b), a.shared ? a.shared[b] : 0);
-      gives = max(0, pages_held(a, b) - from);
+  // all_gives, all_takes: of all n; the caller has the threads meet before the sums
+  // are read.
+  __device__ __forceinline__ void count(const Sequence& s, int n, int& all_gives, int& all_takes) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int g = tid < n ? max(0, s.held - s.keeps) : 0, t = tid < n ? max(0, s.wanted - s.held) : 0;
+    int gs = wave_scan(g), ts = wave_scan(t);
+    if (lane == 63) {
+      waves[0][wave] = gs;
+      waves[1][wave] = ts;
     }
-    int64_t all;
-    const int64_t upto = scan(gives, waves, all);
-    sums[tid] = upto;
-    first[tid] = from;
+    if (tid == 0) granted = 0;
     __syncthreads();
-    for (int64_t i = tid; i < all; i += kAssignThreads) {
-      const int s = owner_of(sums, n, i);
-      const int entry = first[s] + (int)(i - (s ? sums[s - 1] : 0));
-      const int64_t at = in_stack + given + i;
-      if (at < a.n_pages) a.free[at] = a.table[(int64_t)(b0 + s) * a.table_stride + entry];
+    all_gives = all_takes = 0;
+#pragma unroll
+    for (int i = 0; i < N / 64; ++i) {
+      const int x = waves[0][i], y = waves[1][i];
+      gs += i < wave ? x : 0;
+      ts += i < wave ? y : 0;
+      all_gives += x;
+      all_takes += y;
     }
-    given += all;
+    gives[tid] = gs;
+    takes[tid] = ts;
+    first[tid] = g ? s.keeps : s.held;
+  }
+  __device__ __forceinline__ int before(const int* sums, int i) const { return i ? sums[i - 1] : 0; }
+};
+
+// All sequences by one work-group (N threads, B <= N), or by several that all count
+// and share the pages and the slots out.  What one of them reads, none writes: pages
+// below the stack's top stay where they are in the stack, and those that came back
+// are read where they came from.
+template <int N>
+__global__ __launch_bounds__(N) void assign_kernel(AssignLaunch a, int with_slots) {
+  __shared__ Counts<N> c;
+  __shared__ int64_t rows[N];
+  __shared__ int fresh[N], held[N], held_after[N];
+  const int tid = threadIdx.x;
+  const int in_stack = stack_of(a);
+  const Sequence s = sequence(a, min(tid, a.B - 1));
+  int given, asked;
+  c.count(s, a.B, given, asked);
+  const int stack = (int)min((int64_t)a.n_pages, (int64_t)in_stack + given);
+  const int upto = c.takes[tid];  // (the thread's own)
+  const bool takes = s.wanted > s.held, granted = upto <= stack;
+  const int after = takes && !granted ? s.held : s.wanted;
+  // (The sums rise, so those that get theirs come first.)
+  if (tid < a.B && takes && granted) atomicMax(&c.granted, upto);
+  rows[tid] = s.rows;
+  fresh[tid] = s.fresh;
+  held[tid] = s.held;
+  held_after[tid] = after;
+  __syncthreads();
+  // The stack's page at a place.
+  auto page_at = [&](int place) {
+    if (place < in_stack) return a.free[place];
+    const int i = place - in_stack, b = owner_of<N>(c.gives, a.B, i);
+    return a.table[(int64_t)b * a.table_stride + c.first[b] + i - c.before(c.gives, b)];
+  };
+  // The page of an entry of sequence b below held_after[b].
+  auto page_of = [&](int b, int entry) {
+    return entry < held[b] ? a.table[(int64_t)b * a.table_stride + entry]
+                           : page_at(stack - 1 - (c.before(c.takes, b) + entry - held[b]));
+  };
+  const int wg = blockIdx.x, wgs = gridDim.x;
+  if (wg == 0) {
+    if (tid < a.B) a.held_out[tid] = after;
+    if (tid == 0) {
+      a.n_free_out[0] = stack - c.granted;
+      if (a.missing) a.missing[0] = max(0, asked - stack);
+    }
+  }
+  for (int i = wg * N + tid; i < stack - in_stack; i += wgs * N) a.free[in_stack + i] = page_at(in_stack + i);
+  for (int i = wg * N + tid; i < c.granted; i += wgs * N) {
+    const int b = owner_of<N>(c.takes, a.B, i);
+    a.table[(int64_t)b * a.table_stride + c.first[b] + i - c.before(c.takes, b)] = page_at(stack - 1 - i);
+  }
+  if (!with_slots) return;
+  if (a.T < 64) {
+    const int n = a.B * a.T;
+    for (int i = wg * N + tid; i < n; i += wgs * N) {
+      const int b = i / a.T, t = i - b * a.T;
+      const int64_t row = rows[b] + t;
+      const bool there = t < fresh[b] && row >= 0 && row < a.L && (int)row / a.page < held_after[b];
+      a.slots[i] = there ? in_pool(a, page_of(b, (int)row / a.page), (int)row) : -1;
+    }
+    return;
+  }
+  // A wave takes 64 tokens, whose entries are looked up by a lane each.
+  const int runs = (a.T + 63) / 64, lane = tid & 63;
+  for (int u = wg * (N / 64) + (tid >> 6); u < a.B * runs; u += wgs * (N / 64)) {
+    const int b = u / runs, t = (u - b * runs) * 64 + lane;
+    const int64_t row = rows[b] + t;
+    const bool there = t < fresh[b] && row >= 0 && row < a.L && (int)row / a.page < held_after[b];
+    const uint64_t some = __ballot(there);
+    int slot = -1;
+    if (some) {
+      const int entry = there ? (int)row / a.page : 0;
+      const int e0 = __builtin_amdgcn_readlane(entry, __ffsll((unsigned long long)some) - 1);
+      const int e1 = __builtin_amdgcn_readlane(entry, 63 - __clzll((long long)some));
+      const int page = e0 + lane <= e1 ? page_of(b, e0 + lane) : -1;
+      const int mine = __shfl(page, entry - e0);
+      if (there) slot = in_pool(a, mine, (int)row);
+    }
+    if (t < a.T) a.slots[(int64_t)b * a.T + t] = slot;
+  }
+}
+
+// More sequences, by one work-group, kAssignSeqs at a time: all pages back, then
+// pages off the stack.
+__global__ __launch_bounds__(kAssignSeqs) void assign_many_kernel(AssignLaunch a) {
+  __shared__ Counts<kAssignSeqs> c;
+  const int tid = threadIdx.x;
+  const int64_t in_stack = stack_of(a);
+  int64_t given = 0;
+  for (int b0 = 0; b0 < a.B; b0 += kAssignSeqs) {
+    const int n = min(kAssignSeqs, a.B - b0);
+    int gives, takes;
+    c.count(sequence(a, b0 + min(tid, n - 1)), n, gives, takes);
+    __syncthreads();
+    for (int i = tid; i < gives; i += kAssignSeqs) {
+      const int b = owner_of<kAssignSeqs>(c.gives, n, i);
+      const int64_t place = in_stack + given + i;
+      if (place < a.n_pages)
+        a.free[place] = a.table[(int64_t)(b0 + b) * a.table_stride + c.first[b] + i - c.before(c.gives, b)];
+    }
+    given += gives;
     __syncthreads();
   }
   const int64_t stack = min((int64_t)a.n_pages, in_stack + given);
-
-  // Pages off the stack's top, as long as it lasts: entries [held, wanted).
   int64_t asked = 0, taken = 0;
-  for (int b0 = 0; b0 < a.B; b0 += kAssignThreads) {
-    const int b = b0 + tid, n = min(kAssignThreads, a.B - b0);
-    int takes = 0, held = 0, wanted = 0;
-    if (tid < n) {
-      wanted = pages_wanted(a, b);
-      held = pages_held(a, b);
-      takes = max(0, wanted - held);
-    }
-    int64_t all;
-    const int64_t upto = scan(takes, waves, all);
-    const bool granted = asked + upto <= stack;
-    sums[tid] = upto;
-    first[tid] = held;
-    if (tid == 0) granted_all = 0;
+  for (int b0 = 0; b0 < a.B; b0 += kAssignSeqs) {
+    const int n = min(kAssignSeqs, a.B - b0);
+    const Sequence s = sequence(a, b0 + min(tid, n - 1));
+    int gives, all;
+    c.count(s, n, gives, all);
+    const bool takes = s.wanted > s.held, granted = asked + c.takes[tid] <= stack;
+    if (tid < n && takes && granted) atomicMax(&c.granted, c.takes[tid]);
+    if (tid < n) a.held_out[b0 + tid] = takes && !granted ? s.held : s.wanted;
     __syncthreads();
-    // (Sums rise, so those who get theirs come first: the last of them has all.)
-    const bool next_granted = tid + 1 < n && asked + sums[tid + 1] <= stack;
-    if (tid < n && granted && !next_granted) granted_all = upto;
-    if (tid < n) a.held_out[b] = takes && !granted ? held : wanted;
-    __syncthreads();
-    for (int64_t i = tid; i < granted_all; i += kAssignThreads) {
-      const int s = owner_of(sums, n, i);
-      const int entry = first[s] + (int)(i - (s ? sums[s - 1] : 0));
-      a.table[(int64_t)(b0 + s) * a.table_stride + entry] = a.free[stack - 1 - taken - i];
+    for (int i = tid; i < c.granted; i += kAssignSeqs) {
+      const int b = owner_of<kAssignSeqs>(c.takes, n, i);
+      a.table[(int64_t)(b0 + b) * a.table_stride + c.first[b] + i - c.before(c.takes, b)] = a.free[stack - 1 - taken - i];
     }
     asked += all;
-    taken += granted_all;
+    taken += c.granted;
     __syncthreads();
   }
   if (tid == 0) {
     a.n_free_out[0] = (int)(stack - taken);
     if (a.missing) a.missing[0] = (int)min((int64_t)INT32_MAX, max((int64_t)0, asked - stack));
   }
-  if (with_slots)
-    for (int i = tid; i < a.B * a.T; i += kAssignThreads) a.slots[i] = slot_of(a, i / a.T, i % a.T);
 }
 
+// The slots, of tables and held_out in place.
 __global__ __launch_bounds__(256) void slots_kernel(AssignLaunch a) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i < (int64_t)a.B * a.T) a.slots[i] = slot_of(a, (int)(i / a.T), (int)(i % a.T));
+  if (i >= (int64_t)a.B * a.T) return;
+  const int b = (int)(i / a.T), t = (int)(i - (int64_t)b * a.T);
+  const int64_t row = (int64_t)a.row0 + (a.lens ? a.lens[b] : 0) + t;
+  const int fresh = a.n_new ? min(a.T, a.n_new[b]) : a.T;
+  int slot = -1;
+  if (t < fresh && row >= 0 && row < a.L && (int)row / a.page < a.held_out[b])
+    slot = in_pool(a, a.table[(int64_t)b * a.table_stride + (int)row / a.page], (int)row);
+  a.slots[i] = slot;
 }
 
 // ---------------------------------------------------------------------------
@@ -251,12 +340,26 @@ __global__ __launch_bounds__(kReorderThreads) void reorder_kernel(ReorderLaunch 
 
 }  // namespace
 
-hipError_t launch_assign(const AssignLaunch& a, hipStream_t stream) {
+hipError_t launch_assign(const AssignLaunch& a, int cus, hipStream_t stream) {
   const int64_t slots = (int64_t)a.B * a.T;
-  const bool with_slots = slots <= kAssignSlots;
-  assign_kernel<<<1, kAssignThreads, 0, stream>>>(a, with_slots);
+  // (In place, held and n_free are not there to be read by other work-groups.)
+  const bool in_place = a.held_out == a.held || a.n_free_out == a.n_free;
+  if (a.B <= kAssignSeqs) {
+    const int n = a.B <= 256 ? 256 : kAssignSeqs;
+    // A work-group takes a slot per thread, and up to 32 pages per thread if
+    // every page of the tables changes hands.
+    const bool with_slots = !in_place || slots <= 4 * n;
+    const int64_t by_slots = (slots + n - 1) / n, by_pages = ((int64_t)a.B * a.entries + 32 * n - 1) / (32 * n);
+    const int64_t wgs = in_place ? 1 : by_slots > by_pages ? by_slots : by_pages;
+    const unsigned grid = (unsigned)(wgs > 2 * cus ? 2 * cus : wgs);
+    if (n == 256) assign_kernel<256><<<grid, 256, 0, stream>>>(a, with_slots);
+    else assign_kernel<kAssignSeqs><<<grid, kAssignSeqs, 0, stream>>>(a, with_slots);
+    if (with_slots) return hipGetLastError();
+  } else {
+    assign_many_kernel<<<1, kAssignSeqs, 0, stream>>>(a);
+  }
   if (hipError_t e = hipGetLastError()) return e;
-  if (!with_slots) slots_kernel<<<(unsigned)((slots + 255) / 256), 256, 0, stream>>>(a);
+  slots_kernel<<<(unsigned)((slots + 255) / 256), 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 

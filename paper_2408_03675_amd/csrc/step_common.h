@@ -141,6 +141,7 @@ inline int check_pages(const nacl_problem* p, const nacl_pages* x) {
   if (!x) return fail_status(NACL_ERR_INVALID_ARG, "pages are NULL");
   if (x->n_pages < 1 || x->page < 1 || x->entries < 1)
     return fail_status(NACL_ERR_INVALID_ARG, "n_pages, page and entries must be >= 1 (got %d, %d, %d)", x->n_pages, x->page, x->entries);
+  if (x->entries > 1 << 20) return fail_status(NACL_ERR_UNSUPPORTED, "entries = %d exceeds 2^20", x->entries);
   if ((int64_t)x->n_pages * x->page >= (int64_t)1 << 31)
     return fail_status(NACL_ERR_UNSUPPORTED, "n_pages * page reaches 2^31");
   if (x->table_stride < x->entries) return fail_status(NACL_ERR_INVALID_ARG, "table_stride must be at least entries");

@@ -77,7 +77,8 @@ def _assign(c, row0=0, shared=None, in_place=False, stride=0, given=True):
 
 
 @pytest.mark.parametrize("B,T,page,entries", [(1, 1, 16, 1), (1, 1, 1, 5), (64, 1, 16, 60), (7, 5, 27, 9), (3, 700, 16, 80),
-                                              (300, 60, 13, 12), (1025, 2, 4, 7), (2500, 1, 3, 5), (2, 40000, 128, 400)])
+                                              (300, 60, 13, 12), (1024, 40, 5, 20),
+                                              (1025, 2, 4, 7), (2500, 1, 3, 5), (2, 40000, 128, 400), (256, 1500, 16, 200)])
 @pytest.mark.parametrize("short", [False, True])
 def test_assign(B, T, page, entries, short):
     c = _assign_case(B, T, page, entries, seed=B + T, short=short)

@@ -66,6 +66,7 @@ def _reorder(lib, p=None, x=None, W=2, parents=at(20), lens=at(21), held=at(22),
 
 @pytest.mark.parametrize("kw,code", [
     (dict(n_pages=0), INVALID), (dict(page=0), INVALID), (dict(entries=0), INVALID), (dict(page=-1), INVALID),
+    (dict(entries=(1 << 20) + 1, table_stride=1 << 21), UNSUPPORTED),
     (dict(n_pages=1 << 20, page=1 << 11), UNSUPPORTED), (dict(table_stride=ENTRIES - 1), INVALID),
     (dict(table_stride=1 << 33), UNSUPPORTED), (dict(table=AT + 6 * SIZE + 2), INVALID),
 ])
