@@ -251,6 +251,7 @@ hipError_t launch_rotate_append(RotateLaunch a, int dtype, int D, int cus, hipSt
 constexpr int kPrefixMinChunk = 128;  // keys per chunk at least
 constexpr int kPrefixTileRows = 128;
 constexpr int kPrefixWideRows = 256;
+constexpr int64_t kPagedNearBytes = 0xFFFFE000;
 struct PrefixLaunch {
   int B, H, G, T, L, row0;
   int Lp, per_group;             // rows per head of the prefix (0: none), sequences per group
@@ -279,6 +280,8 @@ struct PrefixLaunch {
   int64_t table_stride;
   int page, n_pages;
   uint32_t page_inv;             // (2^32 - 1) / page
+  int chunk;                     // keys per chunk (not paged: 0)
+  int near;                      // the pools' heads span less than kPagedNearBytes
 };
 hipError_t launch_prefix(const PrefixLaunch& a, int dtype, int D, hipStream_t stream);
 hipError_t launch_paged(const PrefixLaunch& a, int dtype, int D, hipStream_t stream);

@@ -14,12 +14,49 @@ namespace {
 
 using namespace nacl;
 
-// The plan of a step's attention over pages: that of own caches of as many rows
-// as the table has room for.
-Plan paged_plan(const nacl_problem* p, const nacl_step* s, const nacl_pages* x) {
-  nacl_problem q = *p;
-  q.L = (int32_t)std::min<int64_t>(p->L, (int64_t)x->entries * x->page);
-  return plan_of(&q, s, nullptr);
+// How a step's attention over pages is shared out, by sizes alone: blocks of rows
+// as for own caches, and chunks of a fixed number of keys, of which a sequence makes as
+// many as it is long.
+struct PagedPlan {
+  int L = 0, rows = 16, blocks = 0, chunk = 0, split = 0;
+  int64_t units = 0, slots = 0, all_rows = 0;
+  bool direct = false;
+  size_t ml = 0, total = 0;  // byte offset of part_ml, workspace bytes
+};
+PagedPlan paged_plan(const nacl_problem* p, const nacl_step* s, const nacl_pages* x) {
+  PagedPlan a;
+  const int G = q_group_of(p);
+  a.L = (int)std::min<int64_t>(p->L, (int64_t)x->entries * x->page);
+  const int64_t own = (int64_t)G * s->T;
+  a.all_rows = (int64_t)p->B * p->H * own;
+  // Up to 128 rows by 32, whose blocks read the same keys one after the other on one
+  // XCD (64 rows, 8 heads, 16000 keys: 21.4 + 4.6 us, as half a tile of 128 29.0 + 6.8; 128
+  // rows, 8000 keys: 20.6 + 4.9, 21.7 + 7.8).
+  a.rows = own <= 16 ? 16 : own <= kPrefixTileRows || p->dtype == NACL_F32 ? 32 : kPrefixTileRows;
+  auto up = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
+  a.blocks = (int)up(own, a.rows);
+  const int64_t keys = (int64_t)p->B * p->H * a.blocks * a.L;
+  // Five work-groups of 16 rows per CU if every sequence were as long as its table
+  // (three run together; 3 caches of up to 131072 rows 173 us, by three per CU 221; 32 of up
+  // to 8256 129 and 137; 8 of up to 4000 19.9 and 20.4), two of more (4 caches of 8000 rows,
+  // 32 rows: 21.6 us, four 26.3; 64 rows above: four 27.0).
+  const int per_cu = a.rows == 16 ? 5 : 2;
+  const int64_t chunk = std::max<int64_t>(kPrefixMinChunk, up(keys, per_cu * kPlanCus));
+  a.chunk = (int)(up(chunk, 32) * 32);
+  a.split = (int)up(a.L, a.chunk);
+  a.units = (int64_t)p->B * p->H * a.split;
+  a.slots = up(a.units, 8) * a.blocks;
+  a.direct = a.split == 1;
+  const size_t parts = a.direct ? 0 : (size_t)a.all_rows * a.split;
+  a.ml = align_up(parts * p->D * sizeof(float));
+  a.total = a.ml + align_up(std::max<size_t>(parts * sizeof(float2), 1));
+  return a;
+}
+int check_planned(const PagedPlan& a) {
+  if (a.all_rows >= (int64_t)1 << 26) return fail_status(NACL_ERR_UNSUPPORTED, "B * H * q_group * T reaches 2^26");
+  if (8 * a.slots >= (int64_t)1 << 24)
+    return fail_status(NACL_ERR_UNSUPPORTED, "%lld work-groups, at most 2^24", (long long)(8 * a.slots));
+  return NACL_OK;
 }
 
 // Whether one of the written extents meets another or one of those read.
@@ -118,7 +155,7 @@ int nacl_pages_assign(const nacl_problem* p, const nacl_step* s, const nacl_page
 size_t nacl_paged_workspace_bytes(const nacl_problem* p, const nacl_step* s, const nacl_pages* x) {
   nacl::clear_detail();
   if (check_step(p, s) != NACL_OK || check_pages(p, x) != NACL_OK) return 0;
-  const Plan a = paged_plan(p, s, x);
+  const PagedPlan a = paged_plan(p, s, x);
   return check_planned(a) == NACL_OK ? a.total : 0;
 }
 
@@ -132,10 +169,10 @@ int nacl_paged_attention(const nacl_problem* p, const nacl_step* s, const nacl_p
   if (!q || !out || !x->table) return fail_status(NACL_ERR_INVALID_ARG, "q, out and the table must be non-NULL");
   if (!aligned(q, 16) || !aligned(out, 16)) return fail_status(NACL_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
   if (!aligned(lse, 4)) return fail_status(NACL_ERR_INVALID_ARG, "lse must be 4-byte aligned");
-  const Plan plan = paged_plan(p, s, x);
+  const PagedPlan plan = paged_plan(p, s, x);
   if ((st = check_planned(plan))) return st;
   if ((st = check_workspace(ws, ws_bytes, plan.total))) return st;
-  if (overlap({Extent(out, (uintptr_t)plan.rows * p->D * eb), words(lse, plan.rows), Extent(ws, plan.total)},
+  if (overlap({Extent(out, (uintptr_t)plan.all_rows * p->D * eb), words(lse, plan.all_rows), Extent(ws, plan.total)},
               {Extent(q, s->q_stride, p->B, p->H * G, s->T, p->D, eb), pool_extent(p, x, x->k, x->k_stride),
                pool_extent(p, x, x->v, x->v_stride), table_extent(x->table, x->table_stride, p->B, x->entries),
                words(s->lens, p->B), words(s->n_new, p->B)}))
@@ -145,14 +182,14 @@ int nacl_paged_attention(const nacl_problem* p, const nacl_step* s, const nacl_p
   a.H = p->H;
   a.G = G;
   a.T = s->T;
-  a.L = (int)std::min<int64_t>(p->L, (int64_t)x->entries * x->page);
+  a.L = plan.L;
   a.row0 = s->row0;
-  a.per_group = plan.per_group;
-  a.own_rows = plan.own_rows;
-  a.own_blocks = plan.own_blocks;
-  a.own_split = plan.own_split;
-  a.own_units = (int)plan.own_units;
-  a.own_slots = (int)plan.own_slots;
+  a.per_group = p->B;
+  a.own_rows = plan.rows;
+  a.own_blocks = plan.blocks;
+  a.own_split = plan.split;
+  a.own_units = (int)plan.units;
+  a.own_slots = (int)plan.slots;
   a.direct = plan.direct ? 1 : 0;
   a.c2 = (float)((double)p->sm_scale * 1.4426950408889634);
   for (int i = 0; i < 3; ++i) {
@@ -174,6 +211,9 @@ int nacl_paged_attention(const nacl_problem* p, const nacl_step* s, const nacl_p
   a.page = x->page;
   a.n_pages = x->n_pages;
   a.page_inv = ~0u / (uint32_t)x->page;
+  a.chunk = plan.chunk;
+  auto span = [&](const int64_t st[3]) { return ((x->n_pages - 1) * st[0] + (x->page - 1) * st[2] + p->D) * eb; };
+  a.near = std::max(span(x->k_stride), span(x->v_stride)) <= kPagedNearBytes;
   return launched(nacl::launch_paged(a, p->dtype, p->D, static_cast<hipStream_t>(stream)), "paged attention kernels");
 }
 

@@ -77,51 +77,87 @@ __device__ __forceinline__ RowAt row_at(const PrefixLaunch& a, bool prefix, int 
     r.limit = prefix_len(a, owner);
   } else {
     r.b = owner;
-    r.t = row / a.G;
-    r.hq = h * a.G + row % a.G;
+    r.t = a.T == 1 ? 0 : row / a.G;
+    r.hq = h * a.G + row - r.t * a.G;
     r.limit = own_limit(a, owner, r.t);
   }
   return r;
 }
 
+// How a kernel's own caches are laid out: rows of a head behind each other, or pages;
+// pools that span less than 4 GiB (kPagedNear) are addressed as such rows are, by
+// buffer descriptors with 32-bit byte offsets, so that three work-groups of 16 rows fit a
+// CU's registers (32 caches of up to 8256 rows 129 us; by 64-bit addresses, two
+// work-groups, 139).
+enum Layout { kRows, kPagedNear, kPagedFar };
+constexpr uint32_t kNowhere = 0xFFFFF000u;  // a byte offset past every near pool: loads give zeros
+
 // Keys key0 .. key0 + N - 1 of a paged cache: lane i looks key key0 + i mod N up,
 // a tile ahead of the loads that need it, and gives its rows' places to the
 // lanes that load them.
-template <int N>
+template <int N, Layout LAYOUT>
 struct PageTile {
-  int page = 0, row = 0;
-  bool in = false;
-  int64_t k = 0, v = 0;  // the key's row in the pools, in elements
-  uint64_t ok = 0;       // bit i: key key0 + i is there
+  using Place = std::conditional_t<LAYOUT == kPagedFar, int64_t, uint32_t>;  // far: elements; near: bytes
+  int page = 0, row = 0, key = 0;
+  Place k = 0, v = 0;  // the key's row in the pools
+  uint64_t ok = 0;     // bit i: key key0 + i is there
 
   // (A product with 2^32 / page, rounded down, is at most one short of j / page.)
   static __device__ __forceinline__ int entry_of(const PrefixLaunch& a, int j) {
     const int e = (int)__umulhi((uint32_t)j, a.page_inv);
     return j - e * a.page >= a.page ? e + 1 : e;
   }
-  __device__ __forceinline__ void lookup(const PrefixLaunch& a, const int32_t* table, int key0, int key_hi, int lane) {
-    const int j = key0 + (lane & (N - 1));
-    in = j < key_hi;
-    const int e = entry_of(a, in ? j : key_hi - 1);
+  __device__ __forceinline__ void lookup(const PrefixLaunch& a, const int32_t* table, int key0, int lane) {
+    key = key0 + (lane & (N - 1));
+    const int j = min(key, a.L - 1), e = entry_of(a, j);
     row = j - e * a.page;
     page = table[e];
   }
-  // What lies past key_hi or in a page outside the pool is loaded from the pool's
-  // first row, and hidden.
-  __device__ __forceinline__ void resolve(const PrefixLaunch& a) {
-    const bool there = in && (uint32_t)page < (uint32_t)a.n_pages;
+  // What lies past key_hi or in a page outside the pool is hidden, and loaded from
+  // nowhere (far: from the pool's first row).
+  template <typename T>
+  __device__ __forceinline__ void resolve(const PrefixLaunch& a, int key_hi) {
+    const bool there = key < key_hi && (uint32_t)page < (uint32_t)a.n_pages;
     ok = __ballot(there);
     if constexpr (N < 64) ok &= (1ull << N) - 1;
-    k = there ? (int64_t)page * a.ks[0] + (int64_t)row * a.ks[2] : 0;
-    v = there ? (int64_t)page * a.vs[0] + (int64_t)row * a.vs[2] : 0;
+    if constexpr (LAYOUT == kPagedFar) {
+      k = there ? (int64_t)page * a.ks[0] + (int64_t)row * a.ks[2] : 0;
+      v = there ? (int64_t)page * a.vs[0] + (int64_t)row * a.vs[2] : 0;
+    } else {
+      k = there ? ((uint32_t)page * (uint32_t)a.ks[0] + (uint32_t)row * (uint32_t)a.ks[2]) * (uint32_t)sizeof(T) : kNowhere;
+      v = there ? ((uint32_t)page * (uint32_t)a.vs[0] + (uint32_t)row * (uint32_t)a.vs[2]) * (uint32_t)sizeof(T) : kNowhere;
+    }
   }
   static constexpr uint64_t kAll = N < 64 ? (1ull << (N & 63)) - 1 : ~0ull;
 };
-__device__ __forceinline__ int64_t from_lane(int64_t x, int lane) {
-  const uint32_t lo = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * lane, (int)(uint32_t)x);
-  const uint32_t hi = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * lane, (int)(uint32_t)(x >> 32));
-  return (int64_t)((uint64_t)hi << 32 | lo);
+__device__ __forceinline__ uint32_t from_lane(uint32_t x, int lane) {
+  return (uint32_t)__builtin_amdgcn_ds_bpermute(4 * lane, (int)x);
 }
+__device__ __forceinline__ int64_t from_lane(int64_t x, int lane) {
+  return (int64_t)((uint64_t)from_lane((uint32_t)(x >> 32), lane) << 32 | from_lane((uint32_t)x, lane));
+}
+
+// What a head's K or V rows are loaded from: a descriptor and the bytes per row
+// (kRows), a descriptor (kPagedNear), an address (kPagedFar).
+template <typename T, Layout LAYOUT>
+struct Head {
+  __amdgpu_buffer_rsrc_t rsrc;
+  uint32_t row_bytes = 0;
+  const T* at = nullptr;
+  // 16 or 8 bytes, `bytes` from the start of row `key` (kRows) or from a place.
+  template <int BYTES, typename Where>
+  __device__ __forceinline__ auto load(Where where, uint32_t bytes) const {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    using W = std::conditional_t<BYTES == 16, u32x4, u32x2>;
+    if constexpr (LAYOUT == kPagedFar) {
+      return *reinterpret_cast<const W*>(reinterpret_cast<const char*>(at + where) + bytes);
+    } else {
+      const uint32_t off = (LAYOUT == kRows ? (uint32_t)where * row_bytes : (uint32_t)where) + bytes;
+      if constexpr (BYTES == 16) return __builtin_bit_cast(W, __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, 0, 0));
+      else return __builtin_bit_cast(W, __builtin_amdgcn_raw_buffer_load_b64(rsrc, off, 0, 0));
+    }
+  }
+};
 
 // K, V and Q fragments by type.  Lane (g, r) = (lane / 16, lane mod 16).
 //
@@ -155,56 +191,25 @@ struct Frag<__bf16, D> {
     }
   };
 
-  __device__ __forceinline__ void load_k(__amdgpu_buffer_rsrc_t rsrc, uint32_t row_bytes, int key0, int g, int r) {
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-#pragma unroll
-      for (int kb = 0; kb < kKb; ++kb)
-        kf[e][kb] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(
-                                                   rsrc, (uint32_t)(key0 + 16 * e + r) * row_bytes + 64 * kb + 16 * g, 0, 0));
-  }
-  __device__ __forceinline__ void load_v(__amdgpu_buffer_rsrc_t rsrc, uint32_t row_bytes, int key0, int g, int r) {
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t at = (uint32_t)(key0 + 16 * e + 4 * g + i) * row_bytes + (uint32_t)r * (2 * kDt);
-        if constexpr (kDt == 8) {
-          const u32x4 w = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0));
-#pragma unroll
-          for (int c = 0; c < 4; ++c) vw[4 * e + i][c] = w[c];
-        } else {
-          const auto w = __builtin_amdgcn_raw_buffer_load_b64(rsrc, at, 0, 0);
-#pragma unroll
-          for (int c = 0; c < 2; ++c) vw[4 * e + i][c] = w[c];
-        }
-      }
-  }
-  // The same of a paged cache, the rows at k and v of the lanes that looked them up.
-  __device__ __forceinline__ void load_k(const __bf16* head, int64_t k, int g, int r) {
+  // key(i): where key i of the tile lies.
+  template <typename H, typename Key>
+  __device__ __forceinline__ void load_k(const H& head, Key key, int g, int r) {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const __bf16* p = head + from_lane(k, 16 * e + r) + 8 * g;
+      const auto at = key(16 * e + r);
 #pragma unroll
-      for (int kb = 0; kb < kKb; ++kb) kf[e][kb] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(p + 32 * kb));
+      for (int kb = 0; kb < kKb; ++kb) kf[e][kb] = __builtin_bit_cast(bf16x8, head.template load<16>(at, 64 * kb + 16 * g));
     }
   }
-  __device__ __forceinline__ void load_v(const __bf16* head, int64_t v, int g, int r) {
-    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  template <typename H, typename Key>
+  __device__ __forceinline__ void load_v(const H& head, Key key, int g, int r) {
 #pragma unroll
     for (int e = 0; e < 2; ++e)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const __bf16* p = head + from_lane(v, 16 * e + 4 * g + i) + r * kDt;
-        if constexpr (kDt == 8) {
-          const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+        const auto w = head.template load<2 * kDt>(key(16 * e + 4 * g + i), (uint32_t)r * (2 * kDt));
 #pragma unroll
-          for (int c = 0; c < 4; ++c) vw[4 * e + i][c] = w[c];
-        } else {
-          const u32x2 w = *reinterpret_cast<const u32x2*>(p);
-#pragma unroll
-          for (int c = 0; c < 2; ++c) vw[4 * e + i][c] = w[c];
-        }
+        for (int c = 0; c < kDt / 2; ++c) vw[4 * e + i][c] = w[c];
       }
   }
   __device__ __forceinline__ void zero_v(int e, int i) {
@@ -286,36 +291,20 @@ struct Frag<float, D> {
     }
   };
 
-  __device__ __forceinline__ void load_k(__amdgpu_buffer_rsrc_t rsrc, uint32_t row_bytes, int key0, int g, int r) {
+  template <typename H, typename Key>
+  __device__ __forceinline__ void load_k(const H& head, Key key, int g, int r) {
+    const auto at = key(r);
 #pragma unroll
-    for (int c = 0; c < kC; ++c)
-      kf[c] = __builtin_bit_cast(
-          f32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (uint32_t)(key0 + r) * row_bytes + 64 * c + 16 * g, 0, 0));
+    for (int c = 0; c < kC; ++c) kf[c] = __builtin_bit_cast(f32x4, head.template load<16>(at, 64 * c + 16 * g));
   }
-  __device__ __forceinline__ void load_v(__amdgpu_buffer_rsrc_t rsrc, uint32_t row_bytes, int key0, int g, int r) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int c = 0; c < kDt / 4; ++c) {
-        const f32x4 w = __builtin_bit_cast(
-            f32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                       rsrc, (uint32_t)(key0 + 4 * g + i) * row_bytes + (uint32_t)(r * kDt + 4 * c) * 4, 0, 0));
-#pragma unroll
-        for (int x = 0; x < 4; ++x) vw[i][4 * c + x] = w[x];
-      }
-  }
-  __device__ __forceinline__ void load_k(const float* head, int64_t k, int g, int r) {
-    const float* p = head + from_lane(k, r) + 4 * g;
-#pragma unroll
-    for (int c = 0; c < kC; ++c) kf[c] = *reinterpret_cast<const f32x4*>(p + 16 * c);
-  }
-  __device__ __forceinline__ void load_v(const float* head, int64_t v, int g, int r) {
+  template <typename H, typename Key>
+  __device__ __forceinline__ void load_v(const H& head, Key key, int g, int r) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float* p = head + from_lane(v, 4 * g + i) + r * kDt;
+      const auto at = key(4 * g + i);
 #pragma unroll
       for (int c = 0; c < kDt / 4; ++c) {
-        const f32x4 w = *reinterpret_cast<const f32x4*>(p + 4 * c);
+        const f32x4 w = __builtin_bit_cast(f32x4, head.template load<16>(at, (uint32_t)(r * kDt + 4 * c) * 4));
 #pragma unroll
         for (int x = 0; x < 4; ++x) vw[i][4 * c + x] = w[x];
       }
@@ -383,12 +372,52 @@ __device__ __forceinline__ Item item_of(const PrefixLaunch& a, bool prefix, int 
   return it;
 }
 
-// One head's K or V rows below `rows`; what lies past them reads as zeros.
-template <typename T>
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const void* base, const int64_t (&st)[3], const Item& it, int rows) {
-  const T* p = reinterpret_cast<const T*>(base) + (int64_t)it.owner * st[0] + (int64_t)it.h * st[1];
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(p), (short)0, (int)((uint32_t)rows * ((uint32_t)st[2] * sizeof(T))),
-                                           kRsrcWord3);
+// A paged work-group's share.  Its chunk starts at a key that the lengths do not move
+// (chunks of a.chunk keys), so that the first page is looked up while they are loaded.
+__device__ __forceinline__ Item paged_item(const PrefixLaunch& a, int rows, int unit, int block) {
+  Item it;
+  it.prefix = false;
+  if (a.own_blocks == 1) {
+    it.split = blockIdx.x;
+    it.h = blockIdx.y;
+    it.owner = blockIdx.z;
+  } else {
+    it.split = unit % a.own_split;
+    unit /= a.own_split;
+    it.h = unit % a.H;
+    it.owner = unit / a.H;
+  }
+  it.row0 = block * rows;
+  it.row1 = min(a.G * a.T, it.row0 + rows);
+  it.key_lo = it.split * a.chunk;
+  return it;
+}
+__device__ __forceinline__ void paged_limit(const PrefixLaunch& a, Item& it) {
+  int t0 = 0, t1 = 0;
+  if (a.T > 1) {
+    t0 = it.row0 / a.G;
+    t1 = (it.row1 - 1) / a.G;
+  }
+  t1 = last_real(a, it.owner, t0, t1);
+  it.key_hi = min(t1 < t0 ? 0 : own_limit(a, it.owner, t1), it.key_lo + a.chunk);
+}
+
+// One head's K or V rows below the item's last key (what lies past them reads as
+// zeros), or its pool.
+template <typename T, Layout LAYOUT>
+__device__ __forceinline__ Head<T, LAYOUT> head_of(const PrefixLaunch& a, const Item& it, const void* base, const int64_t (&st)[3]) {
+  Head<T, LAYOUT> x;
+  T* p = reinterpret_cast<T*>(const_cast<void*>(base)) + (int64_t)it.h * st[1];
+  if constexpr (LAYOUT == kRows) {
+    p += (int64_t)it.owner * st[0];
+    x.row_bytes = (uint32_t)st[2] * sizeof(T);
+    x.rsrc = __builtin_amdgcn_make_buffer_rsrc(p, (short)0, (int)((uint32_t)it.key_hi * x.row_bytes), kRsrcWord3);
+  } else if constexpr (LAYOUT == kPagedNear) {
+    x.rsrc = __builtin_amdgcn_make_buffer_rsrc(p, (short)0, (int)kNowhere, kRsrcWord3);
+  } else {
+    x.at = p;
+  }
+  return x;
 }
 template <typename T>
 __device__ __forceinline__ const T* query_of(const PrefixLaunch& a, const RowAt& x) {
@@ -427,20 +456,20 @@ __device__ __forceinline__ void put(const PrefixLaunch& a, const Item& it, const
 // infinite or NaN.  The matrix products above give a hidden key the probability
 // 0, which times such a value would still be NaN.  A wave per row: 64 keys at a
 // time, a lane each for the logits, then each lane D / 64 entries of the output.
-template <typename T, int D, bool PAGED>
+template <typename T, int D, Layout LAYOUT>
 __device__ __forceinline__ void odd_item(const PrefixLaunch& a, const Item& it) {
   constexpr int kPer = D / 64;
   const int lane = threadIdx.x & 63;
   const int64_t* ks = it.prefix ? a.pks : a.ks;
   const int64_t* vs = it.prefix ? a.pvs : a.vs;
-  const int64_t owner = PAGED ? 0 : it.owner;
+  const int64_t owner = (LAYOUT != kRows) ? 0 : it.owner;
   const T* kh = reinterpret_cast<const T*>(it.prefix ? a.pk : a.k) + owner * ks[0] + (int64_t)it.h * ks[1];
   const T* vh = reinterpret_cast<const T*>(it.prefix ? a.pv : a.v) + owner * vs[0] + (int64_t)it.h * vs[1];
   // Key j's place; whether it is there.
   auto place = [&](int j, const int64_t* st, int64_t& at) {
     at = (int64_t)j * st[2];
-    if constexpr (PAGED) {
-      const int e = PageTile<64>::entry_of(a, j), page = a.table[(int64_t)it.owner * a.table_stride + e];
+    if constexpr (LAYOUT != kRows) {
+      const int e = PageTile<64, kPagedFar>::entry_of(a, j), page = a.table[(int64_t)it.owner * a.table_stride + e];
       if ((uint32_t)page >= (uint32_t)a.n_pages) return false;
       at = (int64_t)page * st[0] + (int64_t)(j - e * a.page) * st[2];
     }
@@ -503,8 +532,9 @@ struct StreamShared {
   float m[kWaves][16 * R], l[kWaves][16 * R];
 };
 
-template <typename T, int D, int R, bool PAGED>
-__device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& it, StreamShared<D, R>& sh) {
+template <typename T, int D, int R, Layout LAYOUT>
+__device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& it, StreamShared<D, R>& sh,
+                                            PageTile<Frag<T, D>::kKeys, LAYOUT> pages = {}) {
   using F = Frag<T, D>;
   constexpr int kE = F::kKeys / 16, kDt = F::kDt;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -528,22 +558,9 @@ __device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& i
   }
   plain = __all(plain);
 
-  // Tiles of K and V: one head's rows, or its rows in the pages.
-  __amdgpu_buffer_rsrc_t kr, vr;
-  uint32_t krow, vrow;
-  const T *kh, *vh;
-  const int32_t* table;
-  PageTile<F::kKeys> pages;
-  if constexpr (PAGED) {
-    kh = reinterpret_cast<const T*>(a.k) + (int64_t)it.h * a.ks[1];
-    vh = reinterpret_cast<const T*>(a.v) + (int64_t)it.h * a.vs[1];
-    table = a.table + (int64_t)it.owner * a.table_stride;
-  } else {
-    kr = it.prefix ? rows_of<T>(a.pk, a.pks, it, key_hi) : rows_of<T>(a.k, a.ks, it, key_hi);
-    vr = it.prefix ? rows_of<T>(a.pv, a.pvs, it, key_hi) : rows_of<T>(a.v, a.vs, it, key_hi);
-    krow = (uint32_t)(it.prefix ? a.pks[2] : a.ks[2]) * sizeof(T);
-    vrow = (uint32_t)(it.prefix ? a.pvs[2] : a.vs[2]) * sizeof(T);
-  }
+  const Head<T, LAYOUT> kh = head_of<T, LAYOUT>(a, it, it.prefix ? a.pk : a.k, it.prefix ? a.pks : a.ks);
+  const Head<T, LAYOUT> vh = head_of<T, LAYOUT>(a, it, it.prefix ? a.pv : a.v, it.prefix ? a.pvs : a.vs);
+  const int32_t* table = (LAYOUT != kRows) ? a.table + (int64_t)it.owner * a.table_stride : nullptr;
 
   f32x4 acc[R][kDt];
   float m[R], l[R];
@@ -557,22 +574,21 @@ __device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& i
 
   F f;
   auto load_k = [&](int key) {
-    if constexpr (PAGED) {
-      pages.resolve(a);
-      f.load_k(kh, pages.k, g, r);
-      pages.lookup(a, table, key + kWaves * F::kKeys, key_hi, lane);
+    if constexpr (LAYOUT != kRows) {
+      pages.template resolve<T>(a, key_hi);
+      f.load_k(kh, [&](int i) { return from_lane(pages.k, i); }, g, r);
+      pages.lookup(a, table, key + kWaves * F::kKeys, lane);
     } else {
-      f.load_k(kr, krow, key, g, r);
+      f.load_k(kh, [&](int i) { return key + i; }, g, r);
     }
   };
   auto load_v = [&](int key) {
-    if constexpr (PAGED) f.load_v(vh, pages.v, g, r);
-    else f.load_v(vr, vrow, key, g, r);
+    if constexpr (LAYOUT != kRows) f.load_v(vh, [&](int i) { return from_lane(pages.v, i); }, g, r);
+    else f.load_v(vh, [&](int i) { return key + i; }, g, r);
   };
   bool odd = false;  // an infinite or NaN value in a chunk that some rows see a part of
   int key0 = key_lo + wave * F::kKeys;
   if (key0 < key_hi) {
-    if constexpr (PAGED) pages.lookup(a, table, key0, key_hi, lane);
     load_k(key0);
     load_v(key0);
   }
@@ -582,7 +598,7 @@ __device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& i
     for (int q = 0; q < R; ++q) f.logits(qf[q], s[q]);
     const int next = key0 + kWaves * F::kKeys;
     const uint32_t ok = (uint32_t)pages.ok;  // of this tile
-    const bool whole = PAGED ? ok == (uint32_t)pages.kAll : key0 + F::kKeys <= key_hi;
+    const bool whole = (LAYOUT != kRows) ? ok == (uint32_t)pages.kAll : key0 + F::kKeys <= key_hi;
     if (next < key_hi) load_k(next);
 #pragma unroll
     for (int q = 0; q < R; ++q) {
@@ -592,7 +608,7 @@ __device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& i
         for (int e = 0; e < kE; ++e)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (16 * e + i >= lim || (PAGED && !(ok >> (16 * e + 4 * g + i) & 1))) s[q][e][i] = -INFINITY;
+            if (16 * e + i >= lim || ((LAYOUT != kRows) && !(ok >> (16 * e + 4 * g + i) & 1))) s[q][e][i] = -INFINITY;
       }
       float mx = -INFINITY;
 #pragma unroll
@@ -618,7 +634,7 @@ __device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& i
         for (int dt = 0; dt < kDt; ++dt) acc[q][dt] *= alpha;
       }
     }
-    if (PAGED && !whole) {
+    if (LAYOUT == kPagedFar && !whole) {
 #pragma unroll
       for (int e = 0; e < kE; ++e)
 #pragma unroll
@@ -636,7 +652,7 @@ __device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& i
   }
 
   if (!plain && __syncthreads_or(odd)) {
-    odd_item<T, D, PAGED>(a, it);
+    odd_item<T, D, LAYOUT>(a, it);
     return;
   }
 
@@ -705,8 +721,9 @@ struct TileShared {
   unsigned char k[2][kTileKeys * D * 2], v[2][kTileKeys * D * 2];
 };
 
-template <int D, int ROWS, bool PAGED>
-__device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it, TileShared<D>& sh) {
+template <int D, int ROWS, Layout LAYOUT>
+__device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it, TileShared<D>& sh,
+                                          PageTile<kTileKeys, LAYOUT> pages = {}) {
   constexpr int kRowBytes = D * 2, kChunks = kRowBytes / 16;
   constexpr int kC = D / 16, kDt = D / 32;
   constexpr int kThreads = 2 * ROWS;
@@ -731,21 +748,9 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
   const bool plain = __all(limit >= key_hi);
   const bool idle = it.row0 + 32 * wave >= it.row1;  // no row in this wave
 
-  __amdgpu_buffer_rsrc_t kr, vr;
-  uint32_t krow, vrow;
-  const __bf16 *kh, *vh;
-  const int32_t* table;
-  PageTile<kTileKeys> pages;
-  if constexpr (PAGED) {
-    kh = reinterpret_cast<const __bf16*>(a.k) + (int64_t)it.h * a.ks[1];
-    vh = reinterpret_cast<const __bf16*>(a.v) + (int64_t)it.h * a.vs[1];
-    table = a.table + (int64_t)it.owner * a.table_stride;
-  } else {
-    kr = it.prefix ? rows_of<__bf16>(a.pk, a.pks, it, key_hi) : rows_of<__bf16>(a.k, a.ks, it, key_hi);
-    vr = it.prefix ? rows_of<__bf16>(a.pv, a.pvs, it, key_hi) : rows_of<__bf16>(a.v, a.vs, it, key_hi);
-    krow = (uint32_t)(it.prefix ? a.pks[2] : a.ks[2]) * 2;
-    vrow = (uint32_t)(it.prefix ? a.pvs[2] : a.vs[2]) * 2;
-  }
+  const Head<__bf16, LAYOUT> kh = head_of<__bf16, LAYOUT>(a, it, it.prefix ? a.pk : a.k, it.prefix ? a.pks : a.ks);
+  const Head<__bf16, LAYOUT> vh = head_of<__bf16, LAYOUT>(a, it, it.prefix ? a.pv : a.v, it.prefix ? a.pvs : a.vs);
+  const int32_t* table = (LAYOUT != kRows) ? a.table + (int64_t)it.owner * a.table_stride : nullptr;
 
   // Pieces of 16 bytes are permuted by row: the 16 rows of a K fragment's half and
   // the four rows by four pieces of a V fragment's fall on all 64 banks (two rows of
@@ -757,32 +762,25 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
   bool odd = false;  // as for few rows
   u32x4 kreg[kUnits], vreg[kUnits];
   auto load = [&](int key0) {
-    if constexpr (PAGED) {
-      pages.resolve(a);
+    if constexpr (LAYOUT != kRows) pages.template resolve<__bf16>(a, key_hi);
+    auto piece = [&](const Head<__bf16, LAYOUT>& head, auto place, int u) {
+      const int p = tid + kThreads * u, key = p / kChunks;
+      const uint32_t bytes = (uint32_t)(p % kChunks) * 16;
+      if constexpr (LAYOUT != kRows) return head.template load<16>(from_lane(place, key), bytes);
+      else return head.template load<16>(key0 + key, bytes);
+    };
 #pragma unroll
-      for (int u = 0; u < kUnits; ++u) {
-        const int p = tid + kThreads * u, key = p / kChunks;
-        kreg[u] = *reinterpret_cast<const u32x4*>(kh + from_lane(pages.k, key) + p % kChunks * 8);
-        vreg[u] = *reinterpret_cast<const u32x4*>(vh + from_lane(pages.v, key) + p % kChunks * 8);
-      }
+    for (int u = 0; u < kUnits; ++u) kreg[u] = piece(kh, pages.k, u);
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) vreg[u] = piece(vh, pages.v, u);
+    if constexpr (LAYOUT == kPagedFar) {
       if (pages.ok != pages.kAll) {
 #pragma unroll
         for (int u = 0; u < kUnits; ++u)
           if (!(pages.ok >> ((tid + kThreads * u) / kChunks) & 1)) vreg[u] = u32x4{0, 0, 0, 0};
       }
-      pages.lookup(a, table, key0 + kTileKeys, key_hi, lane);
-      return;
     }
-#pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      const int p = tid + kThreads * u;
-      kreg[u] = __builtin_amdgcn_raw_buffer_load_b128(kr, (uint32_t)(key0 + p / kChunks) * krow + (uint32_t)(p % kChunks) * 16, 0, 0);
-    }
-#pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      const int p = tid + kThreads * u;
-      vreg[u] = __builtin_amdgcn_raw_buffer_load_b128(vr, (uint32_t)(key0 + p / kChunks) * vrow + (uint32_t)(p % kChunks) * 16, 0, 0);
-    }
+    if constexpr (LAYOUT != kRows) pages.lookup(a, table, key0 + kTileKeys, lane);
   };
   auto store = [&](int buf) {
 #pragma unroll
@@ -828,7 +826,6 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
   float m = -INFINITY, l = 0.f;
 
   if (key_lo < key_hi) {
-    if constexpr (PAGED) pages.lookup(a, table, key_lo, key_hi, lane);
     load(key_lo);
     store(0);
   }
@@ -837,7 +834,7 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
     __syncthreads();
     const int next = key0 + kTileKeys;
     const uint64_t ok = pages.ok;  // of this tile
-    const bool whole = PAGED ? ok == pages.kAll : next <= key_hi;
+    const bool whole = (LAYOUT != kRows) ? ok == pages.kAll : next <= key_hi;
     if (next < key_hi) load(next);
     if (!idle) {
       f32x16 s[2];
@@ -868,7 +865,7 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (32 * kt + 8 * (i / 4) + i % 4 >= lim || (PAGED && !(ok >> (32 * kt + 8 * (i / 4) + i % 4 + 4 * hl) & 1)))
+            if (32 * kt + 8 * (i / 4) + i % 4 >= lim || ((LAYOUT != kRows) && !(ok >> (32 * kt + 8 * (i / 4) + i % 4 + 4 * hl) & 1)))
               s[kt][i] = -INFINITY;
       }
       float mx = -INFINITY;
@@ -917,7 +914,7 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
   }
 
   if (causal && __syncthreads_or(odd)) {
-    odd_item<__bf16, D, PAGED>(a, it);
+    odd_item<__bf16, D, LAYOUT>(a, it);
     return;
   }
   auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
@@ -935,40 +932,55 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
 
 // What takes the prefix's items and the own caches' (rows per work-group: 16,
 // 32, 128 or 256).  The prefix's come first: they are the longer ones.
-template <typename T, int D, int ROWS, bool PAGED>
+template <typename T, int D, int ROWS, Layout LAYOUT>
 struct Part {
   using Shared = StreamShared<D, ROWS / 16>;
-  static __device__ __forceinline__ void run(const PrefixLaunch& a, const Item& it, Shared& sh) {
-    stream_item<T, D, ROWS / 16, PAGED>(a, it, sh);
+  using Pages = PageTile<Frag<T, D>::kKeys, LAYOUT>;
+  static constexpr int kWaveKeys = Frag<T, D>::kKeys;  // by which a wave's first key lies after the one's before
+  static __device__ __forceinline__ void run(const PrefixLaunch& a, const Item& it, Shared& sh, const Pages& pages = {}) {
+    stream_item<T, D, ROWS / 16, LAYOUT>(a, it, sh, pages);
   }
 };
-template <int D, bool PAGED>
-struct Part<__bf16, D, kTileRows, PAGED> {
+template <int D, Layout LAYOUT>
+struct Part<__bf16, D, kTileRows, LAYOUT> {
   using Shared = TileShared<D>;
-  static __device__ __forceinline__ void run(const PrefixLaunch& a, const Item& it, Shared& sh) {
-    tile_item<D, kTileRows, PAGED>(a, it, sh);
+  using Pages = PageTile<kTileKeys, LAYOUT>;
+  static constexpr int kWaveKeys = 0;
+  static __device__ __forceinline__ void run(const PrefixLaunch& a, const Item& it, Shared& sh, const Pages& pages = {}) {
+    tile_item<D, kTileRows, LAYOUT>(a, it, sh, pages);
   }
 };
 template <int D>
-struct Part<__bf16, D, kWideRows, false> {
+struct Part<__bf16, D, kWideRows, kRows> {
   using Shared = TileShared<D>;
   static __device__ __forceinline__ void run(const PrefixLaunch& a, const Item& it, Shared& sh) {
-    tile_item<D, kWideRows, false>(a, it, sh);
+    tile_item<D, kWideRows, kRows>(a, it, sh);
   }
 };
 constexpr int threads_of(int rows) { return rows >= kTileRows ? 2 * rows : kThreads; }
 
 // (0: none of them in this launch, so that the code of the other alone is there.)
-template <typename T, int D, int PREFIX, int OWN, bool PAGED = false>
-__global__ __launch_bounds__(threads_of(PREFIX > OWN ? PREFIX : OWN), 2) void prefix_kernel(PrefixLaunch a) {
-  using P = Part<T, D, PREFIX ? PREFIX : OWN, PAGED>;
-  using O = Part<T, D, OWN ? OWN : PREFIX, PAGED>;
+template <typename T, int D, int PREFIX, int OWN, Layout LAYOUT = kRows, int WAVES = LAYOUT == kPagedNear && OWN == 16 ? 3 : 2>
+__global__ __launch_bounds__(threads_of(PREFIX > OWN ? PREFIX : OWN), WAVES) void prefix_kernel(PrefixLaunch a) {
+  using P = Part<T, D, PREFIX ? PREFIX : OWN, LAYOUT>;
+  using O = Part<T, D, OWN ? OWN : PREFIX, LAYOUT>;
   union Shared {
     typename P::Shared p;
     typename O::Shared o;
   };
   __shared__ __attribute__((aligned(16))) unsigned char smem[sizeof(Shared)];
   Shared& sh = *reinterpret_cast<Shared*>(smem);
+  if constexpr (LAYOUT != kRows) {
+    const int blocks = a.own_blocks, slot = blockIdx.x >> 3;
+    const int unit = blocks == 1 ? 0 : (slot / blocks) * 8 + (blockIdx.x & 7);
+    if (unit >= a.own_units) return;
+    Item it = paged_item(a, OWN, unit, blocks == 1 ? 0 : slot % blocks);
+    typename O::Pages pages;
+    pages.lookup(a, a.table + (int64_t)it.owner * a.table_stride, it.key_lo + (int)(threadIdx.x >> 6) * O::kWaveKeys, threadIdx.x & 63);
+    paged_limit(a, it);
+    if (!it.nothing(a)) O::run(a, it, sh.o, pages);
+    return;
+  }
   // Work-groups are dealt to the 8 XCDs in turn.  The row blocks that read the
   // same chunk of K and V follow each other on one XCD, whose L2 they share; the
   // prefix's chunks come first.
@@ -1016,7 +1028,7 @@ __global__ __launch_bounds__(kThreads) void prefix_merge_kernel(PrefixLaunch a) 
       np = (n + c - 1) / c;
     }
     const int r0 = (t * a.G + e) / a.own_rows * a.own_rows, r1 = min(a.G * a.T, r0 + a.own_rows);
-    const int n = own_limit(a, b, last_real(a, b, r0 / a.G, (r1 - 1) / a.G)), c = chunk_of(n, a.own_split);
+    const int n = own_limit(a, b, last_real(a, b, r0 / a.G, (r1 - 1) / a.G)), c = a.chunk ? a.chunk : chunk_of(n, a.own_split);
     no = (n + c - 1) / c;
   }
   const int64_t base = row * (a.prefix_split + a.own_split);
@@ -1103,10 +1115,16 @@ hipError_t launch_merge(const PrefixLaunch& a, hipStream_t stream) {
 
 template <typename T, int D>
 hipError_t launch_paged_t(const PrefixLaunch& a, hipStream_t stream) {
-  const unsigned groups = 8u * (unsigned)a.own_slots;
-  if (a.own_rows == 16) prefix_kernel<T, D, 0, 16, true><<<groups, kThreads, 0, stream>>>(a);
-  else if (a.own_rows == 32) prefix_kernel<T, D, 0, 32, true><<<groups, kThreads, 0, stream>>>(a);
-  else if constexpr (std::is_same_v<T, __bf16>) prefix_kernel<T, D, 0, kTileRows, true><<<groups, kThreads, 0, stream>>>(a);
+  // (One row block: no two work-groups read the same keys, and the grid spares the divisions.)
+  const dim3 groups = a.own_blocks == 1 ? dim3(a.own_split, a.H, a.B) : dim3(8u * (unsigned)a.own_slots);
+  auto run = [&](auto layout) {
+    constexpr Layout kLayout = decltype(layout)::value;
+    if (a.own_rows == 16) prefix_kernel<T, D, 0, 16, kLayout><<<groups, kThreads, 0, stream>>>(a);
+    else if (a.own_rows == 32) prefix_kernel<T, D, 0, 32, kLayout><<<groups, kThreads, 0, stream>>>(a);
+    else if constexpr (std::is_same_v<T, __bf16>) prefix_kernel<T, D, 0, kTileRows, kLayout><<<groups, kThreads, 0, stream>>>(a);
+  };
+  if (a.near) run(std::integral_constant<Layout, kPagedNear>{});
+  else run(std::integral_constant<Layout, kPagedFar>{});
   if (hipError_t e = hipGetLastError()) return e;
   return launch_merge<T, D>(a, stream);
 }
