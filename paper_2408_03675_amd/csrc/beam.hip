@@ -110,16 +110,21 @@ struct Piece<float> {
 constexpr uint32_t kLeast = 0x00800000u;  // key of the lowest finite number
 constexpr float kLog2e = 1.44269504f;
 
-// kPer tokens per thread.
-template <typename T, int kPer>
-__global__ __launch_bounds__(kThreads) void beam_slices_kernel(BeamLaunch a) {
+// kPer tokens per thread, a.K at most kTop (so that eight work-groups fit a CU where
+// few are looked for).
+template <typename T, int kPer, int kTop>
+__global__ __launch_bounds__(kThreads, kTop < kMaxK ? 8 : 6) void beam_slices_kernel(BeamLaunch a) {
   using P = Piece<T>;
   constexpr int kPieces = kPer / P::kN, kSlice = kPer * kThreads;
-  __shared__ uint64_t list[most_of(kMaxK) * kPer];  // logits that reach the bound
+  // Threads whose maxima reach the bound, their logits, and those of them that reach it.
+  __shared__ int chosen[most_of(kTop)];
+  __shared__ f32x4 held[most_of(kTop) * kPer / 4];
+  __shared__ uint64_t list[most_of(kTop) * kPer];
   __shared__ uint32_t maxima[kThreads];
+  __shared__ uint32_t bounds[2];
   __shared__ float wave_max[kThreads / 64];
   __shared__ double wave_sum[kThreads / 64];
-  __shared__ int found;
+  __shared__ int n_chosen, found, n_reach;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int row = blockIdx.y, slice = blockIdx.x;
   if (a.ended && a.ended[row]) return;  // its one continuation needs no logits
@@ -149,7 +154,7 @@ __global__ __launch_bounds__(kThreads) void beam_slices_kernel(BeamLaunch a) {
         if (token(u, i) < a.V) x[u][i] = (float)x0[token(u, i)];
     }
   }
-  if (tid == 0) found = 0;
+  if (tid == 0) found = n_chosen = 0;
 
   // The thread's maximum and its exponentials' sum against it, of kPer terms in
   // fp32, as powers of two of x log2(e) - c with c = m log2(e) rounded, from which the
@@ -199,17 +204,23 @@ __global__ __launch_bounds__(kThreads) void beam_slices_kernel(BeamLaunch a) {
   for (int i = 1; i < 64; i *= 2) s += __shfl_xor(s, i);
   if (lane == 0) wave_sum[wave] = s;
 
-  // The bound of the threads' maxima; logits of a language model are a few units
-  // apart there, 2^20 steps each.
-  uint32_t key[kThreads / 64];
-#pragma unroll
-  for (int i = 0; i < kThreads / 64; ++i) key[i] = maxima[lane + 64 * i];
-  int reach;
-  const uint32_t top_key = top == -INFINITY ? 0 : float_order_key(top + 0.f);
+  // The bound of the threads' maxima, by one wave, as the others' instructions count
+  // too; logits of a language model are a few units apart there, 2^20 steps each.
   const int most = most_of(a.K);
-  const uint32_t bound = bound_of(key, top_key, 1u << 20, a.K, most, reach);
+  uint32_t key[kThreads / 64];
+  if (wave == 0) {
+    int reach;
+#pragma unroll
+    for (int i = 0; i < kThreads / 64; ++i) key[i] = maxima[lane + 64 * i];
+    const uint32_t x = bound_of(key, top == -INFINITY ? 0 : float_order_key(top + 0.f), 1u << 20, a.K, most, reach);
+    if (lane == 0) {
+      bounds[0] = x;
+      n_reach = reach;
+    }
+  }
+  __syncthreads();
+  const uint32_t bound = bounds[0];
   uint32_t tie = 0;  // of the logits equal to the bound, those whose ~token reaches it
-  __syncthreads();  // the maxima are read
   const int64_t slot = (int64_t)row * a.S + slice;
   if (tid == 0) {
     double t = 0.0;
@@ -218,7 +229,8 @@ __global__ __launch_bounds__(kThreads) void beam_slices_kernel(BeamLaunch a) {
     a.sums[2 * slot] = (double)top;
     a.sums[2 * slot + 1] = t;
   }
-  if (reach > most) {
+  bool take = mine >= bound;
+  if (n_reach > most) {
     // Equal maxima: the threads with the first tokens among them count.
     uint32_t k = mine > bound ? ~0u : 0;
     if (mine == bound) {
@@ -230,20 +242,36 @@ __global__ __launch_bounds__(kThreads) void beam_slices_kernel(BeamLaunch a) {
     }
     maxima[tid] = k;
     __syncthreads();
+    if (wave == 0) {
+      int reach;
 #pragma unroll
-    for (int i = 0; i < kThreads / 64; ++i) key[i] = maxima[lane + 64 * i];
-    tie = bound_of(key, ~0u, 1u << 12, a.K, a.K, reach);
+      for (int i = 0; i < kThreads / 64; ++i) key[i] = maxima[lane + 64 * i];
+      const uint32_t x = bound_of(key, ~0u, 1u << 12, a.K, a.K, reach);
+      if (lane == 0) bounds[1] = x;
+    }
+    __syncthreads();
+    tie = bounds[1];
+    take = k >= tie;
   }
-  if (mine >= bound) {
-    const float least = of_order_key(max(bound, kLeast));
+  // Their logits to all threads, which look for those that reach it.
+  if (take) {
+    const int at = atomicAdd(&n_chosen, 1);
+    chosen[at] = tid;
 #pragma unroll
     for (int u = 0; u < kPieces; ++u)
 #pragma unroll
-      for (int i = 0; i < P::kN; ++i)
-        if (x[u][i] >= least) {
-          const uint32_t t = ~(uint32_t)token(u, i);
-          if (x[u][i] > least || t >= tie) list[atomicAdd(&found, 1)] = (uint64_t)float_order_key(x[u][i] + 0.f) << 32 | t;
-        }
+      for (int i = 0; i < P::kN; i += 4)
+        held[(at * kPer + u * P::kN + i) / 4] = f32x4{x[u][i], x[u][i + 1], x[u][i + 2], x[u][i + 3]};
+  }
+  __syncthreads();
+  const float least = of_order_key(max(bound, kLeast));
+  for (int i = tid; i < n_chosen * kPer; i += kThreads) {
+    const float v = reinterpret_cast<const float*>(held)[i];
+    if (v >= least) {
+      const int e = i % kPer;
+      const uint32_t t = ~(uint32_t)(first + (e / P::kN * kThreads + chosen[i / kPer]) * P::kN + e % P::kN);
+      if (v > least || t >= tie) list[atomicAdd(&found, 1)] = (uint64_t)float_order_key(v + 0.f) << 32 | t;
+    }
   }
   __syncthreads();
   const int n = found;
@@ -450,12 +478,16 @@ __global__ __launch_bounds__(kThreads) void beam_finish_kernel(BeamLaunch a) {
 hipError_t launch_beam(const BeamLaunch& a, int dtype, hipStream_t stream) {
   const dim3 grid((unsigned)a.S, (unsigned)(a.B * a.W));
   auto run = [&](auto kernel) { kernel<<<grid, kThreads, 0, stream>>>(a); };
+  constexpr int kSmall = kBeamSmallSlice / kThreads, kLarge = kBeamSlice / kThreads, kFew = 16;
   if (a.slice == kBeamSmallSlice) {
-    if (dtype == NACL_F32) run(beam_slices_kernel<float, kBeamSmallSlice / kThreads>);
-    else run(beam_slices_kernel<__bf16, kBeamSmallSlice / kThreads>);
+    if (dtype == NACL_F32) run(beam_slices_kernel<float, kSmall, kMaxK>);
+    else run(beam_slices_kernel<__bf16, kSmall, kMaxK>);
+  } else if (a.K <= kFew) {
+    if (dtype == NACL_F32) run(beam_slices_kernel<float, kLarge, kFew>);
+    else run(beam_slices_kernel<__bf16, kLarge, kFew>);
   } else {
-    if (dtype == NACL_F32) run(beam_slices_kernel<float, kBeamSlice / kThreads>);
-    else run(beam_slices_kernel<__bf16, kBeamSlice / kThreads>);
+    if (dtype == NACL_F32) run(beam_slices_kernel<float, kLarge, kMaxK>);
+    else run(beam_slices_kernel<__bf16, kLarge, kMaxK>);
   }
   if (hipError_t e = hipGetLastError()) return e;
   beam_finish_kernel<<<a.B, kThreads, 0, stream>>>(a);
