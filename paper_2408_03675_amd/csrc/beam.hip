@@ -119,7 +119,8 @@ __global__ __launch_bounds__(kThreads, kTop < kMaxK ? 8 : 6) void beam_slices_ke
   // Threads whose maxima reach the bound, their logits, and those of them that reach it.
   __shared__ int chosen[most_of(kTop)];
   __shared__ f32x4 held[most_of(kTop) * kPer / 4];
-  __shared__ uint64_t list[most_of(kTop) * kPer];
+  __shared__ uint16_t places[most_of(kTop) * kPer];  // in held
+  __shared__ uint64_t list[kThreads];
   __shared__ uint32_t maxima[kThreads];
   __shared__ uint32_t bounds[2];
   __shared__ float wave_max[kThreads / 64];
@@ -264,24 +265,36 @@ __global__ __launch_bounds__(kThreads, kTop < kMaxK ? 8 : 6) void beam_slices_ke
         held[(at * kPer + u * P::kN + i) / 4] = f32x4{x[u][i], x[u][i + 1], x[u][i + 2], x[u][i + 3]};
   }
   __syncthreads();
+  // Logit i of held, as its key and ~token.
+  auto entry = [&](int i) {
+    const int e = i % kPer, at = first + (e / P::kN * kThreads + chosen[i / kPer]) * P::kN + e % P::kN;
+    return (uint64_t)float_order_key(reinterpret_cast<const float*>(held)[i] + 0.f) << 32 | ~(uint32_t)at;
+  };
   const float least = of_order_key(max(bound, kLeast));
   for (int i = tid; i < n_chosen * kPer; i += kThreads) {
     const float v = reinterpret_cast<const float*>(held)[i];
-    if (v >= least) {
-      const int e = i % kPer;
-      const uint32_t t = ~(uint32_t)(first + (e / P::kN * kThreads + chosen[i / kPer]) * P::kN + e % P::kN);
-      if (v > least || t >= tie) list[atomicAdd(&found, 1)] = (uint64_t)float_order_key(v + 0.f) << 32 | t;
-    }
+    if (v > least || (v == least && (uint32_t)entry(i) >= tie)) places[atomicAdd(&found, 1)] = (uint16_t)i;
   }
   __syncthreads();
   const int n = found;
   uint64_t* out = a.keys + slot * a.K;
-  for (int i = tid; i < n; i += kThreads) {
-    const uint64_t k = list[i];
-    int rank = 0;
+  if (n <= kThreads) {
+    const uint64_t k = tid < n ? entry(places[tid]) : 0;
+    list[tid] = k;
+    __syncthreads();
+    if (tid < n) {
+      int rank = 0;
 #pragma unroll 8
-    for (int j = 0; j < n; ++j) rank += list[j] > k;
-    if (rank < a.K) out[rank] = k;
+      for (int j = 0; j < n; ++j) rank += list[j] > k;
+      if (rank < a.K) out[rank] = k;
+    }
+  } else {  // few threads hold most of the largest
+    for (int i = tid; i < n; i += kThreads) {
+      const uint64_t k = entry(places[i]);
+      int rank = 0;
+      for (int j = 0; j < n; ++j) rank += entry(places[j]) > k;
+      if (rank < a.K) out[rank] = k;
+    }
   }
   for (int i = n + tid; i < a.K; i += kThreads) out[i] = 0;
 }
