@@ -885,6 +885,13 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, toke
 _ONE = torch.Size((1,))
 
 
+def _given(t, name, dev, shape, dtype):
+    """The address of a contiguous tensor that may be left out: not null, which would
+    mean that it was."""
+    _like(t, name, dev, shape, dtype)
+    return t.data_ptr() or _gpu(t, name, dev).data_ptr()
+
+
 def _table(t, name, dev, rows, entries=None):
     """A [B, entries] int32 table, rows of any stride; its row stride."""
     if not isinstance(t, torch.Tensor) or t.dim() != 2:
@@ -972,16 +979,14 @@ def pages_assign(step, page, table, held, free, n_free, shared=None, held_out=No
                                (held_out, "held_out", rows), (n_free_out, "n_free_out", _ONE), (slots, "slots", tokens),
                                (missing, "missing", _ONE)):
             _gpu(x, name, dev, shape, i32, contiguous=True)
-    if shared is not None:
-        _like(shared, "shared", dev, rows, i32)
     n_pages, entries = free.shape[0], table.shape[1]
     if not 0 <= page < 2 ** 31 or n_pages >= 2 ** 31 or entries >= 2 ** 31:
         raise ValueError("pages, their rows and the table's entries must fit 32 bits")
     x = _Pages(n_pages, page, entries, stride)
     x.table = table.data_ptr()
-    _launch(dev, lib.nacl_pages_assign, prob.ref(), step.c, x, held.data_ptr(), None if shared is None else shared.data_ptr(),
-            free.data_ptr(), n_free.data_ptr(), held_out.data_ptr(), n_free_out.data_ptr(), slots.data_ptr(),
-            missing.data_ptr())
+    shared = None if shared is None else _given(shared, "shared", dev, rows, i32)
+    _launch(dev, lib.nacl_pages_assign, prob.ref(), step.c, x, held.data_ptr(), shared, free.data_ptr(), n_free.data_ptr(),
+            held_out.data_ptr(), n_free_out.data_ptr(), slots.data_ptr(), missing.data_ptr() or _gpu(missing, "missing", dev).data_ptr())
     return held_out, n_free_out, slots, missing
 
 
@@ -1030,14 +1035,12 @@ def paged_attention(prob, step, q, pages, out=None, lse=None, ws=None):
         lse = torch.empty(step.q_shape[:3], dtype=torch.float32, device=dev)
     elif lse is False:
         lse = None
-    else:
-        _like(lse, "lse", dev, step.q_shape[:3], torch.float32)
     if ws is None:
         ws = paged_workspace(prob, step, pages, dev)
     n = ws.numel()
     _like(ws, "ws", dev, (n,), torch.uint8)
     _launch(dev, lib.nacl_paged_attention, prob.ref(), s, pages.c, q.data_ptr(), out.data_ptr(),
-            None if lse is None else lse.data_ptr(), ws.data_ptr(), n)
+            None if lse is None else _given(lse, "lse", dev, step.q_shape[:3], torch.float32), ws.data_ptr(), n)
     return out, lse
 
 
@@ -1084,10 +1087,9 @@ def beam_select(logits, scores, K, ended=None, end_token=0, parents=None, tokens
     _like(scores, "scores", dev, group, torch.float32)
     d = _Beams(B, W, V, K, NACL_F32 if logits.dtype is torch.float32 else NACL_BF16, stride if N > 1 else V)
     if ended is not None:
-        _like(ended, "ended", dev, group, torch.int32)
         if not 0 <= end_token < V:
             raise ValueError(f"end_token must lie in [0, {V})")
-        d.ended, d.end_token = ended.data_ptr(), end_token
+        d.ended, d.end_token = _given(ended, "ended", dev, group, torch.int32), end_token
     shape, i32, f32 = torch.Size((B, K)), torch.int32, torch.float32
     if parents is None:
         parents = torch.empty(shape, dtype=i32, device=dev)
@@ -1119,15 +1121,14 @@ def beam_reorder(prob, pages, parents, lens, held=None, table_out=None, lens_out
     i32, rows = torch.int32, torch.Size((prob.B,))
     _like(parents, "parents", dev, parents.shape, i32)
     _like(lens, "lens", dev, rows, i32)
-    if held is None:
-        if held_out is not None:
-            raise ValueError("held_out needs held")
-    else:
-        _like(held, "held", dev, rows, i32)
+    old = new = None  # addresses of held and held_out
+    if held is not None:
+        old = _given(held, "held", dev, rows, i32)
         if held_out is None:
             held_out = torch.empty_like(held)
-        else:
-            _like(held_out, "held_out", dev, rows, i32)
+        new = _given(held_out, "held_out", dev, rows, i32)
+    elif held_out is not None:
+        raise ValueError("held_out needs held")
     entries = pages.c.entries
     if table_out is None:
         table_out = torch.empty((prob.B, entries), dtype=i32, device=dev)
@@ -1136,7 +1137,6 @@ def beam_reorder(prob, pages, parents, lens, held=None, table_out=None, lens_out
         lens_out = torch.empty_like(lens)
     else:
         _like(lens_out, "lens_out", dev, rows, i32)
-    _launch(dev, lib.nacl_beam_reorder, prob.ref(), pages.c, parents.shape[1], parents.data_ptr(), lens.data_ptr(),
-            None if held is None else held.data_ptr(), table_out.data_ptr(), stride, lens_out.data_ptr(),
-            None if held_out is None else held_out.data_ptr())
+    _launch(dev, lib.nacl_beam_reorder, prob.ref(), pages.c, parents.shape[1], parents.data_ptr(), lens.data_ptr(), old,
+            table_out.data_ptr(), stride, lens_out.data_ptr(), new)
     return table_out, lens_out, held_out

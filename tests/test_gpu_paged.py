@@ -292,9 +292,11 @@ def test_no_logit_has_weight():
         assert (out == 0).all() and (lse == -math.inf).all()
 
 
-def test_far_pages():
-    """Pages whose places pass 32 bits of elements."""
-    H, page, D, n = 1, 16, 128, (1 << 32) // (16 * 128) + 64
+@pytest.mark.parametrize("n", [0xFFFFE000 // 4096, 0xFFFFE000 // 4096 + 1, (1 << 32) // (16 * 128) + 64])
+def test_far_pages(n):
+    """Pages of 4096 bytes whose places come near 32 bits of bytes, pass them, and pass
+    32 bits of elements."""
+    H, page, D = 1, 16, 128
     k = torch.zeros((n, H, page, D), dtype=torch.bfloat16, device=DEV)
     prob = nacl.Problem(1, H, 64, D, "bf16", [0])
     g = torch.Generator().manual_seed(0)

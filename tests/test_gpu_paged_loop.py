@@ -251,6 +251,23 @@ def test_pages_follow_their_tensors():
         nacl.paged_attention(p.prob, p.step, p.q[0], p.pages[0])
 
 
+@pytest.mark.parametrize("name", ["shared", "missing", "lse", "ended", "held", "held_out"])
+def test_an_optional_tensor_without_memory_is_refused(name):
+    """Its null address would mean that it was not given."""
+    p = Program(5)
+    t = dict(shared=p.shared, missing=p.missing, lse=p.out[0][1], ended=p.ended, held=p.held.clone(), held_out=p.next[2])[name]
+    t.untyped_storage().resize_(0)
+    with pytest.raises(ValueError, match="no memory"):
+        if name in ("shared", "missing"):
+            nacl.pages_assign(p.step, PAGE, p.table, p.held, p.free, p.n_free, **{name: t})
+        elif name == "lse":
+            nacl.paged_attention(p.prob, p.step, p.q[0], p.pages[0], lse=t)
+        elif name == "ended":
+            nacl.beam_select(torch.zeros((B, V), device=DEV), p.scores, W, ended=t, end_token=7)
+        else:
+            nacl.beam_reorder(p.prob, p.pages[0], p.best[0].zero_(), p.lens, **{"held": p.held, name: t})
+
+
 def test_a_used_workspace_of_any_contents():
     p = Program(4)
     p.prefill()
