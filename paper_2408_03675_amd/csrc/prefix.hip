@@ -604,11 +604,12 @@ __device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& i
     for (int q = 0; q < R; ++q) {
       if (!plain || !whole) {
         const int lim = limit[q] - key0 - 4 * g;
+        const uint32_t mine = ok >> (4 * g);  // the lane's keys
 #pragma unroll
         for (int e = 0; e < kE; ++e)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (16 * e + i >= lim || ((LAYOUT != kRows) && !(ok >> (16 * e + 4 * g + i) & 1))) s[q][e][i] = -INFINITY;
+            if (16 * e + i >= lim || ((LAYOUT != kRows) && !(mine >> (16 * e + i) & 1))) s[q][e][i] = -INFINITY;
       }
       float mx = -INFINITY;
 #pragma unroll
@@ -861,11 +862,12 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
       if (!plain || !whole) {
         asm volatile("");  // a branch: the comparisons cost as much as the exponentials' FMAs
         const int lim = limit - key0 - 4 * hl;
+        const uint32_t mine[2] = {(uint32_t)(hl ? ok >> 4 : ok), (uint32_t)((hl ? ok >> 4 : ok) >> 32)};  // the lane's keys
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (32 * kt + 8 * (i / 4) + i % 4 >= lim || ((LAYOUT != kRows) && !(ok >> (32 * kt + 8 * (i / 4) + i % 4 + 4 * hl) & 1)))
+            if (32 * kt + 8 * (i / 4) + i % 4 >= lim || ((LAYOUT != kRows) && !(mine[kt] >> (8 * (i / 4) + i % 4) & 1)))
               s[kt][i] = -INFINITY;
       }
       float mx = -INFINITY;
