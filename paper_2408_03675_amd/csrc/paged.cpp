@@ -30,16 +30,17 @@ PagedPlan paged_plan(const nacl_problem* p, const nacl_step* s, const nacl_pages
   const int64_t own = (int64_t)G * s->T;
   a.all_rows = (int64_t)p->B * p->H * own;
   // Up to 128 rows by 32, whose blocks read the same keys one after the other on one
-  // XCD (64 rows, 8 heads, 16000 keys: 21.4 + 4.6 us, as half a tile of 128 29.0 + 6.8; 128
-  // rows, 8000 keys: 20.6 + 4.9, 21.7 + 7.8).
+  // XCD (64 rows, 8 heads, 16000 keys: attention and merge 21.1 + 4.8 us, as half a tile of 128
+  // rows 21.9 + 5.7; 128 rows, 8000 keys: 20.5 + 4.6 and 19.4 + 7.7).
   a.rows = own <= 16 ? 16 : own <= kPrefixTileRows || p->dtype == NACL_F32 ? 32 : kPrefixTileRows;
   auto up = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
   a.blocks = (int)up(own, a.rows);
   const int64_t keys = (int64_t)p->B * p->H * a.blocks * a.L;
   // Five work-groups of 16 rows per CU if every sequence were as long as its table
   // (three run together; 3 caches of up to 131072 rows 173 us, by three per CU 221; 32 of up
-  // to 8256 129 and 137; 8 of up to 4000 19.9 and 20.4), two of more (4 caches of 8000 rows,
-  // 32 rows: 21.6 us, four 26.3; 64 rows above: four 27.0).
+  // to 8256 129 and 137; 8 of up to 4000 19.9 and 20.4), two of more (the 64 rows above: three
+  // 27.6; 4 caches of 8000 rows, 32 rows: 21.2 us, four 26.3; 512 tokens of 32 heads over
+  // 8192 rows: 125 us, three 135).
   const int per_cu = a.rows == 16 ? 5 : 2;
   const int64_t chunk = std::max<int64_t>(kPrefixMinChunk, up(keys, per_cu * kPlanCus));
   a.chunk = (int)(up(chunk, 32) * 32);

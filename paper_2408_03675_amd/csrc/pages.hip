@@ -14,6 +14,10 @@ namespace {
 // takes; a scan over the sequences gives each its run of the stack.  The pages are
 // moved by all threads together, a thread finding its page's sequence in the
 // scanned counts (a sequence that ended gives hundreds back, most take none).
+// Latency bounds it, the lengths' loads, the scan, the pages' loads one after the other: 64
+// sequences of one token 4.9 us, 256 that take up to 2048 tokens while 64 end (10000 pages,
+// 524288 slots of 4 bytes) 9.6 us; by one work-group and a second launch for the slots
+// 12.6 + 4.1.
 
 constexpr int kAssignSeqs = 1024;     // sequences of a work-group
 
