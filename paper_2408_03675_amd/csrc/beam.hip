@@ -13,7 +13,7 @@
 // 0 for nothing.
 //
 // 32 groups of 8 beams, 131072 tokens each (67 MB of bf16): slices 18.3 us (3.7 TB/s; vector
-// and scalar instructions bound them, some 300 and 200 a wave), finish 6.2 us; 4 beams of 32000
+// and scalar instructions bound them, some 300 and 150 a wave), finish 6.2 us; 4 beams of 32000
 // tokens 4.6 + 4.4 us, one chain of loads and barriers each.
 
 #include <type_traits>
