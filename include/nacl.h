@@ -452,7 +452,9 @@ size_t nacl_paged_workspace_bytes(const nacl_problem* p, const nacl_step* s, con
  * as the table goes (entries * page).  Rows of pages outside the pool (an entry
  * that is not in [0, n_pages)) are not seen.  q, out, lse and the results are
  * those of nacl_prefix_attention without a prefix, B * H * q_group * T below 2^26;
- * pages may be shared by sequences, and hold anything in rows that are not seen. */
+ * pages may be shared by sequences, and hold anything in rows that are not seen.
+ * Entries are followed as far as the lengths say, not as far as pages are held: a
+ * sequence that nacl_pages_assign gave no pages waits for them. */
 int nacl_paged_attention(const nacl_problem* p, const nacl_step* s, const nacl_pages* x, const void* q, void* out,
                          float* lse, void* ws, size_t ws_bytes, void* stream);
 
@@ -497,8 +499,9 @@ int nacl_beam_select(const nacl_beams* d, const void* logits, const float* score
  * touched).  A parent outside [0, W) is none: such a beam takes a table row that
  * is left, and holds no rows.
  * table_out [B, entries] (row stride out_stride, at least entries), lens_out [B]
- * (the parent's length, at most L and what the pages hold), held_out [B] (of the
- * table row taken; with held, else NULL): device int32, overlapping nothing else.
+ * (the parent's length, at most L and the rows that the parent's held pages and the
+ * beam's have room for), held_out [B] (of the table row taken; with held, else NULL):
+ * device int32, overlapping nothing else.
  * lens, held: device int32 [B]; without held every row of the table is taken to be
  * full.  A page that the beams of a group do not share belongs to one of them.
  * Entries outside [0, n_pages) are passed over.  The calls of a model's layers

@@ -89,7 +89,7 @@ def take_over(parents, lens, held, entries, page, L):
     out = []
     for i, p in enumerate(parents):
         takes = p if first[i] else spare.pop(0)
-        room = entries if held is None else max(0, min(entries, held[takes]))
+        room = entries if held is None or not ok[i] else max(0, min(entries, held[takes], held[p]))
         n = max(0, min(lens[p], L, room * page)) if ok[i] else 0
         out.append((takes, n, 0 if first[i] else n))
     return out

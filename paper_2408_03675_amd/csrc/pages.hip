@@ -287,10 +287,11 @@ __global__ __launch_bounds__(kReorderThreads) void reorder_kernel(ReorderLaunch 
   const int group = blockIdx.x / a.wgs, wg = blockIdx.x % a.wgs;
   const int lane = threadIdx.x & 63, base = group * a.W;
   const Beams x = beams_of(a, group);
-  // Rows that the beam holds afterwards: its parent's, as far as its pages go.
+  // Rows that the beam holds afterwards: its parent's, as far as the parent's pages go
+  // and its own.
   int len = 0;
   if (lane < a.W && x.parent >= 0) {
-    const int held = a.held ? max(0, min(a.entries, a.held[base + x.takes])) : a.entries;
+    const int held = a.held ? max(0, min(a.entries, min(a.held[base + x.takes], a.held[base + x.parent]))) : a.entries;
     len = (int)max((int64_t)0, min((int64_t)min(a.lens[base + x.parent], a.L), (int64_t)held * a.page));
   }
   // The tables.

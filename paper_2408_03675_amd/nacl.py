@@ -1060,10 +1060,10 @@ def beam_workspace(B, W, V, K, device="cuda"):
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def beam_select(logits, scores, K, ended=None, end_token=0, parents=None, tokens=None, out=None, ws=None):
+def beam_select(logits, scores, K, ended=None, end_token=None, parents=None, tokens=None, out=None, ws=None):
     """The K best continuations of every group's beams: logits [B * W, V] (fp32 or
-    bf16, any row stride), scores fp32 [B, W], ended (optional) int32 [B, W]
-    (include/nacl.h: nacl_beam_select).  Returns (parents int32 [B, K], tokens int32
+    bf16, any row stride), scores fp32 [B, W], ended (optional) int32 [B, W] with its
+    end_token (include/nacl.h: nacl_beam_select).  Returns (parents int32 [B, K], tokens int32
     [B, K], out fp32 [B, K])."""
     lib = _lib or load_library()
     if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16):
@@ -1076,7 +1076,7 @@ def beam_select(logits, scores, K, ended=None, end_token=0, parents=None, tokens
         raise ValueError("scores must be [B, W] for logits of [B * W, V]")
     group = scores.shape
     B, W = group
-    K, end_token = int(K), int(end_token)
+    K = int(K)
     if N >= 2 ** 31 or V >= 2 ** 31 or not 0 <= K < 2 ** 31:
         raise ValueError("B, W, V and K must fit 32 bits")
     stride, one = logits.stride()
@@ -1087,9 +1087,9 @@ def beam_select(logits, scores, K, ended=None, end_token=0, parents=None, tokens
     _like(scores, "scores", dev, group, torch.float32)
     d = _Beams(B, W, V, K, NACL_F32 if logits.dtype is torch.float32 else NACL_BF16, stride if N > 1 else V)
     if ended is not None:
-        if not 0 <= end_token < V:
-            raise ValueError(f"end_token must lie in [0, {V})")
-        d.ended, d.end_token = _given(ended, "ended", dev, group, torch.int32), end_token
+        if end_token is None or not 0 <= int(end_token) < V:
+            raise ValueError(f"ended needs an end_token in [0, {V})")
+        d.ended, d.end_token = _given(ended, "ended", dev, group, torch.int32), int(end_token)
     shape, i32, f32 = torch.Size((B, K)), torch.int32, torch.float32
     if parents is None:
         parents = torch.empty(shape, dtype=i32, device=dev)

@@ -251,6 +251,13 @@ def test_pages_follow_their_tensors():
         nacl.paged_attention(p.prob, p.step, p.q[0], p.pages[0])
 
 
+def test_ended_beams_need_an_end_token():
+    x, scores, ended = torch.zeros((2, 50), device=DEV), torch.zeros((1, 2), device=DEV), torch.zeros((1, 2), dtype=torch.int32, device=DEV)
+    for token in (None, -1, 50):
+        with pytest.raises(ValueError, match="end_token"):
+            nacl.beam_select(x, scores, 2, ended=ended, end_token=token)
+
+
 @pytest.mark.parametrize("name", ["shared", "missing", "lse", "ended", "held", "held_out"])
 def test_an_optional_tensor_without_memory_is_refused(name):
     """Its null address would mean that it was not given."""

@@ -45,3 +45,5 @@ def test_take_over():
     # Beam 1 goes on three times, 3 once; 0 and 2 end.
     assert take_over([1, 1, 3, 1], [5, 6, 7, 8], None, 4, 4, 16) == [(1, 6, 0), (0, 6, 6), (3, 8, 0), (2, 6, 6)]
     assert take_over([-1, 0, 9], [5, 6, 7], [1, 2, 2], 2, 4, 16) == [(1, 0, 0), (0, 4, 0), (2, 0, 0)]
+    # A copy ends where the parent's pages or the child's do.
+    assert take_over([0, 0, 2, 2], [9, 9, 9, 9], [2, 1, 1, 3], 3, 4, 16) == [(0, 8, 0), (1, 4, 4), (2, 4, 0), (3, 4, 4)]
