@@ -536,13 +536,17 @@ def evict_noalloc(prob, q, k, v, C, Cr, sampling=SAMPLE_SOFTMAX, seed=0, layer=0
 
 # The decoding step between two evictions (Algorithm 1, generation phase).
 
+_Tensor, _current_device, _raw_stream = torch.Tensor, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
 def _launch(dev, call, *args):
     """call(*args, stream) on dev's current stream, with dev the current device."""
-    if dev.index == torch._C._cuda_getDevice():
-        status = call(*args, _raw_stream(dev))
+    index = dev.index
+    if index == _current_device():
+        status = call(*args, _raw_stream(index))
     else:
         with torch.cuda.device(dev):
-            status = call(*args, _raw_stream(dev))
+            status = call(*args, _raw_stream(index))
     if status != NACL_OK:
         _check(status)
 
@@ -550,13 +554,13 @@ def _launch(dev, call, *args):
 def _like(t, name, dev, shape, dtype):
     """_gpu's checks of a contiguous tensor in one expression, for calls where
     the host's time counts; what does not pass is reported by _gpu."""
-    if not (isinstance(t, torch.Tensor) and t.device == dev and t.shape == shape and t.dtype is dtype and t.is_contiguous()):
+    if not (isinstance(t, _Tensor) and t.device == dev and t.shape == shape and t.dtype is dtype and t.is_contiguous()):
         _gpu(t, name, dev, shape, dtype, contiguous=True)
 
 
 def _rows4(t, name, dev, shape, dtype):
     """A [., ., ., D] tensor with a contiguous last dimension; its strides."""
-    if not (isinstance(t, torch.Tensor) and t.device == dev and t.shape == shape and t.dtype is dtype):
+    if not (isinstance(t, _Tensor) and t.device == dev and t.shape == shape and t.dtype is dtype):
         _gpu(t, name, dev, shape, dtype)
     st = t.stride()
     if st[3] != 1:
@@ -569,10 +573,6 @@ def _cache(t, name, dev, step, strides):
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device == dev and t.shape == step.cache_shape and
             t.dtype == step.dtype and t.stride() == strides):
         _gpu(t, name, dev, step.cache_shape, step.dtype, strides[:3])
-
-
-def _raw_stream(dev):
-    return torch._C._cuda_getCurrentRawStream(dev.index)
 
 
 class _Keeper:
@@ -608,7 +608,7 @@ class Step(_Keeper):
         self.dtype = prob.torch_dtype
         self.q_shape, self.new_shape = (B, Hq, self.T, D), (B, H, self.T, D)
         self.cache_shape = (B, H, L, D)
-        self.fits = (H, D, self.dtype)
+        self.fits, self.fits_rotation = (H, D, self.dtype), (D, self.dtype)
         self.rows, self.token_shape = torch.Size((B,)), torch.Size((B, self.T))
         self.k_stride, self.v_stride = tuple(prob.c.k_stride) + (1,), tuple(prob.c.v_stride) + (1,)
         s = _Step()
@@ -629,7 +629,7 @@ class Step(_Keeper):
         self.dev = next((t.device for t in (lens, n_new) if t is not None), None)
         self.c.lens = None if lens is None else lens.data_ptr()
         self.c.n_new = None if n_new is None else n_new.data_ptr()
-        self._strided = {}  # nacl_step by the strides of the call's tensors
+        self._strided, self._last = {}, (None, None)  # nacl_step by the strides of the call's tensors
         self._keep(lens, n_new)
 
     def on(self, prob, dev):
@@ -641,6 +641,9 @@ class Step(_Keeper):
 
     def strided(self, q, k=None, v=None, q_out=None):
         key = (q, k, v, q_out)
+        last, s = self._last  # (a program's strides are the same from step to step)
+        if last == key:
+            return s
         s = self._strided.get(key)
         if s is None:
             s = _Step.from_buffer_copy(self.c)
@@ -650,6 +653,7 @@ class Step(_Keeper):
             if len(self._strided) >= 64:
                 self._strided.clear()
             self._strided[key] = s
+        self._last = key, s
         return s
 
 
@@ -729,7 +733,7 @@ class Prefix(_Keeper):
 
 def _rotation(prob, step, rotation, positions, dev):
     """The call's nacl_rotation and its positions' address."""
-    if rotation.fits != step.fits[1:]:
+    if rotation.fits != step.fits_rotation:
         raise ValueError("the rotation was made for another head size or dtype")
     rotation.current()
     if rotation.dev is not None and rotation.dev != dev:
@@ -1001,8 +1005,18 @@ def paged_append(prob, step, rotation, positions, q_new, k_new, v_new, pages, sl
     _like(slots, "slots", dev, step.token_shape, torch.int32)
     if q_out is None:
         q_out = torch.empty(q_shape, dtype=dt, device=dev)
-    s = step.strided(_rows4(q_new, "q_new", dev, q_shape, dt), _rows4(k_new, "k_new", dev, new_shape, dt),
-                     _rows4(v_new, "v_new", dev, new_shape, dt), _rows4(q_out, "q_out", dev, q_shape, dt))
+    try:  # (one expression for what passes, for the host's time)
+        strides = q_new.stride(), k_new.stride(), v_new.stride(), q_out.stride()
+        good = (q_new.device == dev and q_new.shape == q_shape and q_new.dtype is dt and strides[0][3] == 1 and
+                k_new.device == dev and k_new.shape == new_shape and k_new.dtype is dt and strides[1][3] == 1 and
+                v_new.device == dev and v_new.shape == new_shape and v_new.dtype is dt and strides[2][3] == 1 and
+                q_out.device == dev and q_out.shape == q_shape and q_out.dtype is dt and strides[3][3] == 1)
+    except (AttributeError, IndexError):
+        good = False
+    if not good:
+        strides = (_rows4(q_new, "q_new", dev, q_shape, dt), _rows4(k_new, "k_new", dev, new_shape, dt),
+                   _rows4(v_new, "v_new", dev, new_shape, dt), _rows4(q_out, "q_out", dev, q_shape, dt))
+    s = step.strided(*strides)
     _launch(dev, lib.nacl_paged_append, prob.ref(), s, r, pos, q_new.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), pages.c,
             slots.data_ptr(), q_out.data_ptr())
     return q_out
