@@ -248,6 +248,29 @@ def test_hidden_rows_may_hold_anything(dtype, G, T, page):
         assert torch.isnan(out[b, hq, t]).any()
 
 
+def _check_seen(q, k, v, table, lens, out, lse, scale):
+    """Rows against the float64 attention to the rows of pages that are in the pool;
+    tolerances as for check_rows."""
+    B, Hq, T, D = q.shape
+    n, H, page, _ = k.shape
+    L = table.shape[1] * page
+    kd, vd = _f64(_dense(k, table, L)), _f64(_dense(v, table, L))
+    there = (table.cpu() >= 0) & (table.cpu() < n)
+    seen = there.repeat_interleave(page, dim=1).numpy()
+    u = 2.0 ** -8 if q.dtype == torch.bfloat16 else 0.0
+    for b, hq, t in _rows(B, Hq, T):
+        at = np.flatnonzero(seen[b, :int(lens[b]) + t + 1])
+        h = hq // (Hq // H)
+        ref, ref_l, size, S = attend_row(_f64(q[b, hq, t]), kd[b, h, at], vd[b, h, at], scale)
+        o, l = _f64(out[b, hq, t]), float(lse[b, hq, t])
+        if len(at) == 0:
+            assert l == -math.inf and (o == 0).all()
+            continue
+        gamma = (D + 8) * 2.0 ** -24 * S + (len(at) + 64) * 2.0 ** -24
+        tol = torch.finfo(q.dtype).eps / 2 * np.abs(ref) + (u + 2 * gamma) * 1.01 * size
+        assert (np.abs(o - ref) <= tol).all() and abs(l - ref_l) <= gamma + 2.0 ** -23 * abs(ref_l) + 2.0 ** -22
+
+
 @pytest.mark.parametrize("dtype,G,T,page", [("bf16", 2, 1, 16), ("f32", 2, 3, 5), ("bf16", 4, 40, 16), ("bf16", 2, 1, 64)])
 def test_pages_outside_the_pool_are_not_seen(dtype, G, T, page):
     B, H, L, D = 3, 2, 400, 64
@@ -257,29 +280,48 @@ def test_pages_outside_the_pool_are_not_seen(dtype, G, T, page):
     bad[0, 1], bad[0, 3], bad[1, :], bad[2, 0] = -1, k.shape[0], -9, 1 << 30
     bad[0, table.shape[1] - 1] = -1 << 31
     k[0, :, 0], v[0, :, 0] = math.nan, math.inf  # where nothing is to be read
-    k0 = k.clone()
+    bad[bad == 0] = -1  # (its NaN is nobody's)
     prob = nacl.Problem(B, H, L, D, dtype, [L - 1], q_group=G)
     step = nacl.Step(prob, T, lens=lens.to(DEV))
-    there = (bad.cpu() >= 0) & (bad.cpu() < k.shape[0])
-    # Page 0 is out of the way, so its NaN is nobody's.
-    there &= bad.cpu() != 0
-    bad[bad == 0] = -1
     out, lse = nacl.paged_attention(prob, step, q, nacl.Pages(prob, k, v, bad))
     torch.cuda.synchronize()
-    kd, vd = _f64(_dense(k0, bad, L)), _f64(_dense(v, bad, L))
-    seen = there.repeat_interleave(page, dim=1)[:, :L].numpy()
-    u = 2.0 ** -8 if dtype == "bf16" else 0.0
-    for b, hq, t in _rows(B, H * G, T):
-        n = int(lens[b]) + t + 1
-        at = np.flatnonzero(seen[b, :n])
-        ref, ref_l, size, S = attend_row(_f64(q[b, hq, t]), kd[b, hq // G, at], vd[b, hq // G, at], prob.c.sm_scale)
-        o, l = _f64(out[b, hq, t]), float(lse[b, hq, t])
-        if len(at) == 0:
-            assert l == -math.inf and (o == 0).all()
-            continue
-        gamma = (D + 8) * 2.0 ** -24 * S + (len(at) + 64) * 2.0 ** -24  # as for check_rows
-        tol = torch.finfo(q.dtype).eps / 2 * np.abs(ref) + (u + 2 * gamma) * 1.01 * size
-        assert (np.abs(o - ref) <= tol).all() and abs(l - ref_l) <= gamma + 2.0 ** -23 * abs(ref_l) + 2.0 ** -22
+    _check_seen(q, k, v, bad, lens, out, lse, prob.c.sm_scale)
+
+
+@pytest.fixture(scope="module")
+def wide():
+    """Buffers of which four pages span more than 4 GiB."""
+    yield [torch.zeros(4 * 1500 * 2 ** 20, dtype=torch.uint8, device=DEV) for _ in range(2)]
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("G,T", [(3, 1), (4, 5), (2, 12), (4, 60)])
+def test_every_form_of_the_far_layout(wide, dtype, D, G, T):
+    """Rows by 16, by 32 and by tiles of 128, pages outside the pool, tails inside a
+    page, NaN and infinities in rows that no query sees."""
+    H, page, B = 2, 75, 3
+    g = torch.Generator().manual_seed(D + T)
+    step_bytes = 1500 * 2 ** 20
+    k, v = (torch.as_strided(x.view(DT[dtype]), (4, H, page, D), (step_bytes // DT[dtype].itemsize, page * D, D, 1)) for x in wide)
+    for x in (k, v):
+        x.copy_(torch.randn((4, H, page, D), generator=g).to(DT[dtype]))
+    q = torch.randn((B, H * G, T, D), generator=g).to(DT[dtype]).to(DEV)
+    table = _i32([[3, 0, 2], [2, 4, 3], [-1, -7, 1 << 30]])
+    lens = torch.tensor([170 - T, 225 - T, 200 - T], dtype=torch.int32)
+    # Rows 170 and on of sequence 0, page 2 of which sequence 1 does see.
+    k[1], v[1] = math.nan, math.inf
+    prob = nacl.Problem(B, H, 225, D, dtype, [0], q_group=G)
+    step = nacl.Step(prob, T, lens=lens.to(DEV))
+    out, lse = nacl.paged_attention(prob, step, q, nacl.Pages(prob, k, v, table))
+    torch.cuda.synchronize()
+    _check_seen(q, k, v, table, lens, out, lse, prob.c.sm_scale)
+    # With its tail's hidden rows holding anything (of sequence 0 alone).
+    one = nacl.Problem(1, H, 225, D, dtype, [0], q_group=G)
+    k[2, :, 20:], v[2, :, 20:] = math.nan, math.inf
+    step = nacl.Step(one, T, lens=lens[:1].to(DEV))
+    again, lse1 = nacl.paged_attention(one, step, q[:1], nacl.Pages(one, k, v, table[:1]))
+    torch.cuda.synchronize()
+    assert torch.equal(again, out[:1]) and torch.equal(lse1, lse[:1])
 
 
 def test_no_logit_has_weight():
