@@ -51,6 +51,35 @@ __device__ __forceinline__ double row_turn(double x) {
   return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 
+// The wave's maximum and sum in lane 63, by row shifts and broadcasts.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float shifted(float x, float none) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(none), __float_as_int(x), CTRL, ROWS, 0xF, false));
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double shifted(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xF, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, ROWS, 0xF, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ float last_max(float x) {
+  x = fmaxf(x, shifted<0x111, 0xF>(x, -INFINITY));
+  x = fmaxf(x, shifted<0x112, 0xF>(x, -INFINITY));
+  x = fmaxf(x, shifted<0x114, 0xF>(x, -INFINITY));
+  x = fmaxf(x, shifted<0x118, 0xF>(x, -INFINITY));
+  x = fmaxf(x, shifted<0x142, 0xA>(x, -INFINITY));
+  return fmaxf(x, shifted<0x143, 0xC>(x, -INFINITY));
+}
+__device__ __forceinline__ double last_sum(double x) {
+  x += shifted<0x111, 0xF>(x);
+  x += shifted<0x112, 0xF>(x);
+  x += shifted<0x114, 0xF>(x);
+  x += shifted<0x118, 0xF>(x);
+  x += shifted<0x142, 0xA>(x);
+  return x + shifted<0x143, 0xC>(x);
+}
+
 // A bound that at least `want` of the wave's keys (N per lane) reach and at most
 // `most` of them, unless more are equal to it; 1 where fewer than `want` are not 0.
 // It is looked for downwards from the largest key, top, in steps that grow from
@@ -195,19 +224,15 @@ __global__ __launch_bounds__(kThreads, kTop < kMaxK ? 8 : 6) void beam_slices_ke
   }
   const uint32_t mine = m == -INFINITY ? 0 : float_order_key(m + 0.f);  // (-0 is 0)
   maxima[tid] = mine;
-  float wm = m;
-#pragma unroll
-  for (int i = 1; i < 64; i *= 2) wm = fmaxf(wm, __shfl_xor(wm, i));
-  if (lane == 0) wave_max[wave] = wm;
+  const float wm = last_max(m);
+  if (lane == 63) wave_max[wave] = wm;
   __syncthreads();
   float top = wave_max[0];
 #pragma unroll
   for (int i = 1; i < kThreads / 64; ++i) top = fmaxf(top, wave_max[i]);
   // The sums are joined in fp64.
-  double s = (double)(m == top ? sum : sum * __builtin_amdgcn_exp2f((m - top) * kLog2e));
-#pragma unroll
-  for (int i = 1; i < 64; i *= 2) s += __shfl_xor(s, i);
-  if (lane == 0) wave_sum[wave] = s;
+  const double s = last_sum((double)(m == top ? sum : sum * __builtin_amdgcn_exp2f((m - top) * kLog2e)));
+  if (lane == 63) wave_sum[wave] = s;
 
   // The bound of the threads' maxima, by one wave, as the others' instructions count
   // too; logits of a language model are a few units apart there, 2^20 steps each.
