@@ -411,7 +411,7 @@ __global__ __launch_bounds__(kThreads) void beam_finish_kernel(BeamLaunch a) {
       const bool finite = fabs(score) < INFINITY;
       mode[w] = !finite || (!ended && all == -INFINITY) ? kNone : ended ? kEnded : all == INFINITY ? kInfinite : kLogits;
       tops[w] = all;
-      shift[w] = ended ? score : score - log(sum);
+      shift[w] = (ended ? score : score - log(sum)) + 0.0;  // (-0 is 0)
       // The beam's best value: that of its largest logit.
       if (mode[w] != kNone) atomicMax((unsigned long long*)&best, (unsigned long long)order_key(shift[w]));
     }
