@@ -475,9 +475,10 @@ size_t nacl_beam_workspace_bytes(const nacl_beams* d);
 
 /* The best continuations of every group: of all beams w and tokens v the K largest
  *   value(w, v) = scores[b, w] + x[b * W + w, v] - ln sum over u of exp x[b * W + w, u],
- * largest first, equal ones by beam, then token.  An ended beam has one
- * continuation, end_token, with its score as the value, and its logits are not
- * read.  A beam whose score is infinite or NaN has none (so the first step of a
+ * largest first, equal ones by beam, then logit, then token: of one beam the order is
+ * that of its logits, also next to a score beside which their differences vanish.
+ * An ended beam has one continuation, end_token, with its score as the value, and its
+ * logits are not read.  A beam whose score is infinite or NaN has none (so the first step of a
  * search gives one beam a score and the others -infinity).  A NaN logit counts as
  * -infinity, which has no continuation; infinite logits share a row
  * evenly.  parents, tokens: device int32 [B, K]; out: device fp32 [B, K], the

@@ -337,15 +337,26 @@ enum Mode { kNone, kLogits, kInfinite, kEnded };
 constexpr int kHeads = kBeamLists / kThreads;  // of a thread, at most
 constexpr int kGroup = 16;                     // lanes per beam
 
+// Where a continuation comes from, larger for those that come first among equal values: by
+// beam, within it by logit, then by token.  (A beam's values may be equal where its
+// logits are not: next to a large score their differences are lost in fp64.)  Bits 52 ..
+// 57 hold the beam, 20 .. 51 the logit's key, the others the token.
+constexpr uint64_t kPlace = 1ull << 58;        // of every continuation: 0 is none
+__device__ __forceinline__ uint64_t place_of(int w, uint32_t logit, uint32_t inverse_token) {
+  return kPlace | (uint64_t)(kMaxK - 1 - w) << 52 | (uint64_t)logit << 20 | (inverse_token & 0xFFFFFu);
+}
+__device__ __forceinline__ int beam_at(uint64_t place) { return kMaxK - 1 - (int)(place >> 52 & (kMaxK - 1)); }
+__device__ __forceinline__ int token_at(uint64_t place) { return (int)(~(uint32_t)place & 0xFFFFFu); }
+
 __global__ __launch_bounds__(kThreads) void beam_finish_kernel(BeamLaunch a) {
   // A logit's value is (x - tops) + shift (kEnded, kInfinite: shift): a difference
   // that is exact next to a top of any size, then numbers of the values' size.
   __shared__ double tops[kMaxK], shift[kMaxK];
   __shared__ int mode[kMaxK];
-  __shared__ uint64_t head[kBeamLists];  // the lists' first values, and their places
-  __shared__ uint32_t head_at[kBeamLists];
-  __shared__ uint64_t list[kMaxK * kMaxK];
-  __shared__ uint32_t list_at[kMaxK * kMaxK];
+  // What reaches the bound, its values and their places; before that, the lists' first ones.
+  __shared__ uint64_t list[kMaxK * kMaxK], list_at[kMaxK * kMaxK];
+  uint64_t* head = list;
+  uint64_t* head_at = list_at;
   __shared__ uint64_t best;
   __shared__ int found;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -419,37 +430,38 @@ __global__ __launch_bounds__(kThreads) void beam_finish_kernel(BeamLaunch a) {
   __syncthreads();
 
   // Entry r of list l, whose key is k: its value and its place, beam and token.
-  auto entry = [&](int l, int r, uint64_t k, uint32_t& at) -> uint64_t {
+  auto entry = [&](int l, int r, uint64_t k, uint64_t& at) -> uint64_t {
     const int w = l / a.S, kind = mode[w];
     if (kind == kNone) return 0;
-    at = (uint32_t)w << 20 | (uint32_t)a.end_token;
+    at = place_of(w, 0, ~(uint32_t)a.end_token);
     if (kind == kEnded) return l == w * a.S && r == 0 ? order_key(shift[w]) : 0;
     if (!k) return 0;
-    at = (uint32_t)w << 20 | ~(uint32_t)k;
+    at = place_of(w, (uint32_t)(k >> 32), (uint32_t)k);
     const float x = of_order_key((uint32_t)(k >> 32));
     if (kind == kInfinite) return x == INFINITY ? order_key(shift[w]) : 0;
     return order_key(((double)x - tops[w]) + shift[w]);
   };
+  uint64_t mine[kHeads], mine_at[kHeads];
 #pragma unroll
   for (int c = 0; c < kHeads; ++c) {
     const int i = tid + c * kThreads;
+    mine[c] = mine_at[c] = 0;
     if (i >= n_kept) break;
-    uint32_t at = 0;
-    head[i] = entry(i / kept, i % kept, raw[c], at);
-    head_at[i] = at;
+    mine[c] = entry(i / kept, i % kept, raw[c], mine_at[c]);
+    head[i] = mine[c];
+    head_at[i] = mine_at[c];
   }
   __syncthreads();
   const uint64_t top = best;
 
-  // The bound of the heads (of equal values the first places).  Values are a few
+  // The bound of the heads (of equal values the largest places).  Values are a few
   // units apart, 2^48 steps each.  (The list holds what follows `most` heads.)
   uint64_t bound = 1;
-  uint32_t tie = 0;
+  uint64_t tie = 0;
   const int most = R > 1 || most_of(a.K) * a.K <= kMaxK * kMaxK ? most_of(a.K) : a.K;
   auto search = [&](auto n_c) {
     constexpr int N = decltype(n_c)::value;
-    uint64_t k[N];
-    uint32_t at[N];
+    uint64_t k[N], at[N];
     int reach;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -459,10 +471,10 @@ __global__ __launch_bounds__(kThreads) void beam_finish_kernel(BeamLaunch a) {
     }
     bound = bound_of(k, top, (uint64_t)1 << 48, a.K, most, reach);
     if (reach > most) {
-      uint32_t t[N];
+      uint64_t t[N];
 #pragma unroll
-      for (int i = 0; i < N; ++i) t[i] = k[i] > bound ? ~0u : k[i] == bound ? ~at[i] : 0;
-      tie = bound_of(t, ~0u, 1u << 20, a.K, a.K, reach);
+      for (int i = 0; i < N; ++i) t[i] = k[i] > bound ? 2 * kPlace - 1 : k[i] == bound ? at[i] : 0;
+      tie = bound_of(t, 2 * kPlace - 1, (uint64_t)1 << 52, a.K, a.K, reach);
     }
   };
   if (heads <= 64) search(std::integral_constant<int, 1>{});
@@ -470,18 +482,22 @@ __global__ __launch_bounds__(kThreads) void beam_finish_kernel(BeamLaunch a) {
   else search(std::integral_constant<int, kBeamLists / 64>{});
 
   // What reaches it, and of the lists whose entries here all do, what follows.
-  auto reaches = [&](uint64_t v, uint32_t at) { return v > bound || (v == bound && ~at >= tie); };
-  auto add = [&](uint64_t v, uint32_t at) {
+  __syncthreads();
+  auto reaches = [&](uint64_t v, uint64_t at) { return v > bound || (v == bound && at >= tie); };
+  auto add = [&](uint64_t v, uint64_t at) {
     const int i = atomicAdd(&found, 1);
     list[i] = v;
     list_at[i] = at;
   };
-  for (int i = tid; i < n_kept; i += kThreads) {
-    if (!reaches(head[i], head_at[i])) continue;
-    add(head[i], head_at[i]);
+#pragma unroll
+  for (int c = 0; c < kHeads; ++c) {
+    const int i = tid + c * kThreads;
+    if (i >= n_kept) break;
+    if (!reaches(mine[c], mine_at[c])) continue;
+    add(mine[c], mine_at[c]);
     if (i % kept != kept - 1) continue;
     for (int r = kept; r < a.K; ++r) {
-      uint32_t at = 0;
+      uint64_t at = 0;
       const uint64_t v = entry(i / kept, r, keys[(int64_t)(i / kept) * a.K + r], at);
       if (!reaches(v, at)) break;
       add(v, at);
@@ -491,21 +507,19 @@ __global__ __launch_bounds__(kThreads) void beam_finish_kernel(BeamLaunch a) {
   // Eight lanes rank one of them.
   const int n = found;
   for (int i = tid / 8; i < n; i += kThreads / 8) {
-    const uint64_t v = list[i];
-    const uint32_t at = list_at[i];
+    const uint64_t v = list[i], at = list_at[i];
     int rank = 0;
 #pragma unroll 4
     for (int j = tid % 8; j < n; j += 8) {
-      const uint64_t v2 = list[j];
-      const uint32_t at2 = list_at[j];
-      rank += (int)((v2 > v) | ((v2 == v) & (at2 < at)));
+      const uint64_t v2 = list[j], at2 = list_at[j];
+      rank += (int)((v2 > v) | ((v2 == v) & (at2 > at)));
     }
 #pragma unroll
     for (int x = 1; x < 8; x *= 2) rank += __shfl_xor(rank, x);
     if (rank < a.K && tid % 8 == 0) {
       const int64_t to = (int64_t)group * a.K + rank;
-      a.parents[to] = (int)(at >> 20);
-      a.tokens[to] = (int)(at & 0xFFFFFu);
+      a.parents[to] = beam_at(at);
+      a.tokens[to] = token_at(at);
       a.out[to] = (float)of_order_key(v);
     }
   }
