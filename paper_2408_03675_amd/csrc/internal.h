@@ -278,9 +278,8 @@ struct PrefixLaunch {
   // Paged caches: ks, vs are for page, h, row.
   const int32_t* table;          // [B, entries]
   int64_t table_stride;
-  int page, n_pages;
+  int page, n_pages;             // (not paged: 0)
   uint32_t page_inv;             // (2^32 - 1) / page
-  int chunk;                     // keys per chunk (not paged: 0)
   int near;                      // the pools' heads span less than kPagedNearBytes
 };
 hipError_t launch_prefix(const PrefixLaunch& a, int dtype, int D, hipStream_t stream);

@@ -15,10 +15,10 @@ namespace {
 using namespace nacl;
 
 // How a step's attention over pages is shared out, by sizes alone: blocks of rows
-// as for own caches, and chunks of a fixed number of keys, of which a sequence makes as
-// many as it is long.
+// as for own caches, and splits that take a sequence's blocks of keys in turn, so that all
+// of them are at work however short the sequence is beside its table.
 struct PagedPlan {
-  int L = 0, rows = 16, blocks = 0, chunk = 0, split = 0;
+  int L = 0, rows = 16, blocks = 0, split = 0;
   int64_t units = 0, slots = 0, all_rows = 0;
   bool direct = false;
   size_t ml = 0, total = 0;  // byte offset of part_ml, workspace bytes
@@ -30,21 +30,20 @@ PagedPlan paged_plan(const nacl_problem* p, const nacl_step* s, const nacl_pages
   const int64_t own = (int64_t)G * s->T;
   a.all_rows = (int64_t)p->B * p->H * own;
   // Up to 128 rows by 32, whose blocks read the same keys one after the other on one
-  // XCD (64 rows, 8 heads, 16000 keys: attention and merge 21.1 + 4.8 us, as half a tile of 128
-  // rows 21.9 + 5.7; 128 rows, 8000 keys: 20.5 + 4.6 and 19.4 + 7.7).
+  // XCD (64 rows, 8 heads, 16000 keys: 25.7 us, as half a tile of 128 rows 27.4; 128 rows,
+  // 8000 keys: 24.8 and 26.6; but 32000 keys 52.7 and 44.1).
   a.rows = own <= 16 ? 16 : own <= kPrefixTileRows || p->dtype == NACL_F32 ? 32 : kPrefixTileRows;
   auto up = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
   a.blocks = (int)up(own, a.rows);
   const int64_t keys = (int64_t)p->B * p->H * a.blocks * a.L;
-  // Five work-groups of 16 rows per CU if every sequence were as long as its table
-  // (three run together; 3 caches of up to 131072 rows 173 us, by three per CU 221; 32 of up
-  // to 8256 129 and 137; 8 of up to 4000 19.9 and 20.4), two of more (the 64 rows above: three
-  // 27.6; 4 caches of 8000 rows, 32 rows: 21.2 us, four 26.3; 512 tokens of 32 heads over
-  // 8192 rows: 125 us, three 135).
-  const int per_cu = a.rows == 16 ? 5 : 2;
+  // Six work-groups of 16 rows per CU if every sequence were as long as its table, two rounds
+  // of the three that run together (calls of 32 caches of up to 8256 rows, the mean over
+  // lengths: 138 us, three 140, five 140; of 3 caches of up to 131072 rows 228, 219, 238; of 32
+  // with lengths from 0 on 122, 127, 124), two of more (4 caches of 8000 rows, 32 rows: 31.7
+  // us, three 35, four 38; 512 tokens of 32 heads over 8192 rows 106, 121, 117).
+  const int per_cu = a.rows == 16 ? 6 : 2;
   const int64_t chunk = std::max<int64_t>(kPrefixMinChunk, up(keys, per_cu * kPlanCus));
-  a.chunk = (int)(up(chunk, 32) * 32);
-  a.split = (int)up(a.L, a.chunk);
+  a.split = (int)up(a.L, up(chunk, kPrefixMinChunk) * kPrefixMinChunk);
   a.units = (int64_t)p->B * p->H * a.split;
   a.slots = up(a.units, 8) * a.blocks;
   a.direct = a.split == 1;
@@ -212,7 +211,6 @@ int nacl_paged_attention(const nacl_problem* p, const nacl_step* s, const nacl_p
   a.page = x->page;
   a.n_pages = x->n_pages;
   a.page_inv = ~0u / (uint32_t)x->page;
-  a.chunk = plan.chunk;
   auto span = [&](const int64_t st[3]) { return ((x->n_pages - 1) * st[0] + (x->page - 1) * st[2] + p->D) * eb; };
   a.near = std::max(span(x->k_stride), span(x->v_stride)) <= kPagedNearBytes;
   return launched(nacl::launch_paged(a, p->dtype, p->D, static_cast<hipStream_t>(stream)), "paged attention kernels");

@@ -60,6 +60,11 @@ __device__ __forceinline__ int chunk_of(int n, int n_split) {
   return max(kPrefixMinChunk, (c + 31) & ~31);
 }
 
+// Of pages, split i of n_split takes the blocks of so many keys i, i + n_split, i + 2 n_split, ...
+// of those there are: blocks that its waves read at once (tiles: two of them).
+template <typename T>
+constexpr int kPagedBlock = sizeof(T) == 2 ? 128 : 64;
+
 // A query row of a block: its (sequence, query head, token), the keys it sees
 // (of padding, anything: its results are not taken).
 struct RowAt {
@@ -87,8 +92,9 @@ __device__ __forceinline__ RowAt row_at(const PrefixLaunch& a, bool prefix, int 
 // How a kernel's own caches are laid out: rows of a head behind each other, or pages;
 // pools that span less than 4 GiB (kPagedNear) are addressed as such rows are, by
 // buffer descriptors with 32-bit byte offsets: half the lane moves, and three
-// work-groups of 16 rows fit a CU's registers (by 64-bit addresses two; 3 caches of up to
-// 131072 rows 173 us and 179, 32 of 600 13.4 and 14.2, 32 of up to 8256 129 and 125).
+// work-groups of 16 rows fit a CU's registers (by 64-bit addresses two; calls of 32 caches of
+// up to 600 rows 13.8 us and 15.4, of 2 x 2000 tokens 132 and 141, of 32 caches of up to 8256
+// 137 and 136, of 3 of up to 131072 226 and 224).
 enum Layout { kRows, kPagedNear, kPagedFar };
 constexpr uint32_t kNowhere = 0xFFFFF000u;  // a byte offset past every near pool: loads give zeros
 
@@ -372,9 +378,12 @@ __device__ __forceinline__ Item item_of(const PrefixLaunch& a, bool prefix, int 
   return it;
 }
 
-// A paged work-group's share.  (One token of 32 query heads over 2112 rows 6.0 us, with the
-// key that a chunk starts at computed from the length 6.3; 32 of 600 rows 13.4 and 16.8.)  Its chunk starts at a key that the lengths do not move
-// (chunks of a.chunk keys), so that the first page is looked up while they are loaded.
+// A paged work-group's share.  Its first key depends on the split alone, so that the first
+// page is looked up while the lengths are loaded (32 caches of up to 600 rows 13.8 us, with
+// chunks that the lengths place 17.4), and all splits that there are blocks for are at
+// work, however much wider than the sequence its table is (8 of 4000 rows under a table of
+// 131072 29 us, by chunks of a fixed number of keys 100; under one of 4000 27.5 and 28).
+template <typename T>
 __device__ __forceinline__ Item paged_item(const PrefixLaunch& a, int rows, int unit, int block) {
   Item it;
   it.prefix = false;
@@ -390,7 +399,7 @@ __device__ __forceinline__ Item paged_item(const PrefixLaunch& a, int rows, int 
   }
   it.row0 = block * rows;
   it.row1 = min(a.G * a.T, it.row0 + rows);
-  it.key_lo = it.split * a.chunk;
+  it.key_lo = it.split * kPagedBlock<T>;
   return it;
 }
 __device__ __forceinline__ void paged_limit(const PrefixLaunch& a, Item& it) {
@@ -400,7 +409,7 @@ __device__ __forceinline__ void paged_limit(const PrefixLaunch& a, Item& it) {
     t1 = (it.row1 - 1) / a.G;
   }
   t1 = last_real(a, it.owner, t0, t1);
-  it.key_hi = min(t1 < t0 ? 0 : own_limit(a, it.owner, t1), it.key_lo + a.chunk);
+  it.key_hi = t1 < t0 ? 0 : own_limit(a, it.owner, t1);
 }
 
 // One head's K or V rows below the item's last key (what lies past them reads as
@@ -483,7 +492,7 @@ __device__ __forceinline__ void odd_item(const PrefixLaunch& a, const Item& it) 
     float m = -INFINITY, l = 0.f, o[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) o[i] = 0.f;
-    for (int key0 = it.key_lo; key0 < end; key0 += 64) {
+    auto keys = [&](int key0, int end) {
       float s = -INFINITY;
       int64_t at;
       const bool there = key0 + lane < end && place(key0 + lane, ks, at);
@@ -509,6 +518,12 @@ __device__ __forceinline__ void odd_item(const PrefixLaunch& a, const Item& it) 
 #pragma unroll
         for (int i = 0; i < kPer; ++i) o[i] = __builtin_fmaf(pj, (float)vh[at + kPer * lane + i], o[i]);
       }
+    };
+    if constexpr (LAYOUT == kRows) {
+      for (int key0 = it.key_lo; key0 < end; key0 += 64) keys(key0, end);
+    } else {
+      for (int block = it.key_lo; block < end; block += a.own_split * kPagedBlock<T>)
+        for (int key0 = block; key0 < min(end, block + kPagedBlock<T>); key0 += 64) keys(key0, end);
     }
 #pragma unroll
     for (int i = 1; i < 64; i *= 2) l += __shfl_xor(l, i);
@@ -538,13 +553,15 @@ __device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& i
                                             PageTile<Frag<T, D>::kKeys, LAYOUT> pages = {}) {
   using F = Frag<T, D>;
   constexpr int kE = F::kKeys / 16, kDt = F::kDt;
+  static_assert(kPagedBlock<T> == kWaves * F::kKeys);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int g = lane >> 4, r = lane & 15;
   const int key_lo = it.key_lo, key_hi = it.key_hi;
+  const int step = (LAYOUT != kRows) ? a.own_split * kPagedBlock<T> : kWaves * F::kKeys;
 
   typename F::Query qf[R];
   int limit[R];
-  bool plain = true;  // every row of the block sees every key of the chunk
+  bool plain = true;  // every row of the block sees every key of the item
 #pragma unroll
   for (int q = 0; q < R; ++q) {
     const int row = it.row0 + 16 * q + r;
@@ -558,6 +575,7 @@ __device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& i
     plain = plain && limit[q] >= key_hi;
   }
   plain = __all(plain);
+  const int least = __builtin_amdgcn_readfirstlane(limit[0]);  // (pages: the first row sees the fewest)
 
   const Head<T, LAYOUT> kh = head_of<T, LAYOUT>(a, it, it.prefix ? a.pk : a.k, it.prefix ? a.pks : a.ks);
   const Head<T, LAYOUT> vh = head_of<T, LAYOUT>(a, it, it.prefix ? a.pv : a.v, it.prefix ? a.pvs : a.vs);
@@ -578,7 +596,7 @@ __device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& i
     if constexpr (LAYOUT != kRows) {
       pages.template resolve<T>(a, key_hi);
       f.load_k(kh, [&](int i) { return from_lane(pages.k, i); }, g, r);
-      pages.lookup(a, table, key + kWaves * F::kKeys, lane);
+      pages.lookup(a, table, key + step, lane);
     } else {
       f.load_k(kh, [&](int i) { return key + i; }, g, r);
     }
@@ -587,23 +605,24 @@ __device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& i
     if constexpr (LAYOUT != kRows) f.load_v(vh, [&](int i) { return from_lane(pages.v, i); }, g, r);
     else f.load_v(vh, [&](int i) { return key + i; }, g, r);
   };
-  bool odd = false;  // an infinite or NaN value in a chunk that some rows see a part of
+  bool odd = false;  // an infinite or NaN value beside which some rows do not see all keys
   int key0 = key_lo + wave * F::kKeys;
   if (key0 < key_hi) {
     load_k(key0);
     load_v(key0);
   }
-  for (; key0 < key_hi; key0 += kWaves * F::kKeys) {
+  for (; key0 < key_hi; key0 += step) {
     f32x4 s[R][kE];
 #pragma unroll
     for (int q = 0; q < R; ++q) f.logits(qf[q], s[q]);
-    const int next = key0 + kWaves * F::kKeys;
+    const int next = key0 + step;
+    const bool seen = plain || ((LAYOUT != kRows) && key0 + F::kKeys <= least);  // the tile, by every row
     const uint32_t ok = (uint32_t)pages.ok;  // of this tile
     const bool whole = (LAYOUT != kRows) ? ok == (uint32_t)pages.kAll : key0 + F::kKeys <= key_hi;
     if (next < key_hi) load_k(next);
 #pragma unroll
     for (int q = 0; q < R; ++q) {
-      if (!plain || !whole) {
+      if (!seen || !whole) {
         const int lim = limit[q] - key0 - 4 * g;
         const uint32_t mine = ok >> (4 * g);  // the lane's keys
 #pragma unroll
@@ -643,7 +662,7 @@ __device__ __forceinline__ void stream_item(const PrefixLaunch& a, const Item& i
         for (int i = 0; i < 4; ++i)
           if (!(ok >> (16 * e + 4 * g + i) & 1)) f.zero_v(e, i);
     }
-    if (!plain) {
+    if (!seen) {
 #pragma unroll
       for (int e = 0; e < kE; ++e)
 #pragma unroll
@@ -748,6 +767,9 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
     qf[c] = real ? __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(query_of<__bf16>(a, at) + 16 * c + 8 * hl))
                  : __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
   const bool plain = __all(limit >= key_hi);
+  const int least = __builtin_amdgcn_readfirstlane(limit);  // (pages: the wave's first row sees the fewest)
+  static_assert(kPagedBlock<__bf16> == 2 * kTileKeys);
+  const int step = (LAYOUT != kRows) ? a.own_split * kPagedBlock<__bf16> : 2 * kTileKeys;
   const bool idle = it.row0 + 32 * wave >= it.row1;  // no row in this wave
 
   const Head<__bf16, LAYOUT> kh = head_of<__bf16, LAYOUT>(a, it, it.prefix ? a.pk : a.k, it.prefix ? a.pks : a.ks);
@@ -763,7 +785,7 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
   const bool causal = !it.prefix && a.T > 1;
   bool odd = false;  // as for few rows
   u32x4 kreg[kUnits], vreg[kUnits];
-  auto load = [&](int key0) {
+  auto load = [&](int key0, int after) {  // the tile after it
     if constexpr (LAYOUT != kRows) pages.template resolve<__bf16>(a, key_hi);
     auto piece = [&](const Head<__bf16, LAYOUT>& head, auto place, int u) {
       const int p = tid + kThreads * u, key = p / kChunks;
@@ -782,7 +804,7 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
           if (!(pages.ok >> ((tid + kThreads * u) / kChunks) & 1)) vreg[u] = u32x4{0, 0, 0, 0};
       }
     }
-    if constexpr (LAYOUT != kRows) pages.lookup(a, table, key0 + kTileKeys, lane);
+    if constexpr (LAYOUT != kRows) pages.lookup(a, table, after, lane);
   };
   auto store = [&](int buf) {
 #pragma unroll
@@ -828,16 +850,16 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
   float m = -INFINITY, l = 0.f;
 
   if (key_lo < key_hi) {
-    load(key_lo);
+    load(key_lo, key_lo + kTileKeys);
     store(0);
   }
-  auto tile = [&](auto buf_c, int key0) {
+  auto tile = [&](auto buf_c, int key0, int next, int after) {
     constexpr int buf = decltype(buf_c)::value;
     __syncthreads();
-    const int next = key0 + kTileKeys;
     const uint64_t ok = pages.ok;  // of this tile
-    const bool whole = (LAYOUT != kRows) ? ok == pages.kAll : next <= key_hi;
-    if (next < key_hi) load(next);
+    const bool seen = plain || ((LAYOUT != kRows) && key0 + kTileKeys <= least);
+    const bool whole = (LAYOUT != kRows) ? ok == pages.kAll : key0 + kTileKeys <= key_hi;
+    if (next < key_hi) load(next, after);
     if (!idle) {
       f32x16 s[2];
 #pragma unroll
@@ -860,7 +882,7 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
             s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[(c - kAhead) % (kAhead + 1)][kt], qf[c - kAhead], s[kt], 0, 0, 0);
         }
       }
-      if (!plain || !whole) {
+      if (!seen || !whole) {
         asm volatile("");  // a branch: the comparisons cost as much as the exponentials' FMAs
         const int lim = limit - key0 - 4 * hl;
         const uint32_t mine[2] = {(uint32_t)(hl ? ok >> 4 : ok), (uint32_t)((hl ? ok >> 4 : ok) >> 32)};  // the lane's keys
@@ -911,9 +933,9 @@ __device__ __forceinline__ void tile_item(const PrefixLaunch& a, const Item& it,
     }
     if (next < key_hi) store(buf ^ 1);
   };
-  for (int key0 = key_lo; key0 < key_hi; key0 += 2 * kTileKeys) {
-    tile(std::integral_constant<int, 0>{}, key0);
-    if (key0 + kTileKeys < key_hi) tile(std::integral_constant<int, 1>{}, key0 + kTileKeys);
+  for (int key0 = key_lo; key0 < key_hi; key0 += step) {
+    tile(std::integral_constant<int, 0>{}, key0, key0 + kTileKeys, key0 + step);
+    if (key0 + kTileKeys < key_hi) tile(std::integral_constant<int, 1>{}, key0 + kTileKeys, key0 + step, key0 + step + kTileKeys);
   }
 
   if (causal && __syncthreads_or(odd)) {
@@ -977,7 +999,7 @@ __global__ __launch_bounds__(threads_of(PREFIX > OWN ? PREFIX : OWN), WAVES) voi
     const int blocks = a.own_blocks, slot = blockIdx.x >> 3;
     const int unit = blocks == 1 ? 0 : (slot / blocks) * 8 + (blockIdx.x & 7);
     if (unit >= a.own_units) return;
-    Item it = paged_item(a, OWN, unit, blocks == 1 ? 0 : slot % blocks);
+    Item it = paged_item<T>(a, OWN, unit, blocks == 1 ? 0 : slot % blocks);
     typename O::Pages pages;
     pages.lookup(a, a.table + (int64_t)it.owner * a.table_stride, it.key_lo + (int)(threadIdx.x >> 6) * O::kWaveKeys, threadIdx.x & 63);
     paged_limit(a, it);
@@ -1031,8 +1053,8 @@ __global__ __launch_bounds__(kThreads) void prefix_merge_kernel(PrefixLaunch a) 
       np = (n + c - 1) / c;
     }
     const int r0 = (t * a.G + e) / a.own_rows * a.own_rows, r1 = min(a.G * a.T, r0 + a.own_rows);
-    const int n = own_limit(a, b, last_real(a, b, r0 / a.G, (r1 - 1) / a.G)), c = a.chunk ? a.chunk : chunk_of(n, a.own_split);
-    no = (n + c - 1) / c;
+    const int n = own_limit(a, b, last_real(a, b, r0 / a.G, (r1 - 1) / a.G)), c = a.page ? kPagedBlock<T> : chunk_of(n, a.own_split);
+    no = min((n + c - 1) / c, a.own_split);
   }
   const int64_t base = row * (a.prefix_split + a.own_split);
   const int total = np + no;
