@@ -393,6 +393,12 @@ int nacl_sample(const nacl_draw* d, const void* logits, const float* u, int32_t*
  * tokens into them (nacl_paged_append) and attends (nacl_paged_attention); where
  * sequences are beams, the best continuations are picked (nacl_beam_select) and
  * the beams take over what their parents hold (nacl_beam_reorder).
+ * The eviction itself takes contiguous caches and no table.  A sequence in pages is
+ * evicted by way of one: its rows gathered by the caller in the table's order, evicted
+ * (nacl_evict, of one sequence), and the C kept rows written back as C new tokens of a
+ * sequence without rows (lens 0, n_new C; the others' lens with n_new 0), for which
+ * nacl_pages_assign gives the slots and takes the other pages back, by nacl_paged_append
+ * with a rotation of nothing (rot 0, no weights), whose queries may hold anything.
  * The problem describes the caches as for the decoding step; L is the most rows
  * that a sequence may hold, and the problem's k_stride and v_stride are validated
  * and not used.
@@ -423,8 +429,8 @@ typedef struct nacl_pages {
  * missing (optional): the pages by which the stack fell short, 0 if none.
  *   slots[b, t] = table[b, j / page] * page + j mod page,  j = row0 + lens[b] + t,
  * and -1 for padding (t >= n_new[b]), for rows outside [0, L) and for rows without
- * a page of the pool.  (A program that finds missing above 0 frees memory, by an
- * eviction or by ending a sequence, and calls again with held_out and n_free_out.)
+ * a page of the pool.  (A program that finds missing above 0 frees memory, by evicting
+ * or ending a sequence, and calls again with held_out and n_free_out.)
  * x->k, x->v and their strides are not used.  held, held_out, shared (optional):
  * int32 [B]; n_free, n_free_out, missing: int32 [1]; slots: int32 [B, T]; all
  * DEVICE and contiguous.  held_out may be held and n_free_out n_free; what is
