@@ -16,8 +16,8 @@ namespace {
 // scanned counts (a sequence that ended gives hundreds back, most take none).
 // Latency bounds it, the lengths' loads, the scan, the pages' loads one after the other: 64
 // sequences of one token 4.9 us, 256 that take up to 2048 tokens while 64 end (10000 pages,
-// 524288 slots of 4 bytes) 9.6 us; by one work-group and a second launch for the slots
-// 12.6 + 4.1.
+// 524288 slots of 4 bytes) 9.6 us; in place, by one work-group and a second launch for the
+// slots, 14.9 together.  1500 sequences of one token 15.5 us, 4000 of eight 28.8.
 
 constexpr int kAssignSeqs = 1024;     // sequences of a work-group
 
@@ -353,7 +353,9 @@ hipError_t launch_assign(const AssignLaunch& a, int cus, hipStream_t stream) {
   // (In place, held and n_free are not there to be read by other work-groups.)
   const bool in_place = a.held_out == a.held || a.n_free_out == a.n_free;
   if (a.B <= kAssignSeqs) {
-    const int n = a.B <= 256 ? 256 : kAssignSeqs;
+    // (In place all threads of the one work-group move pages: the 256 sequences above 14.9
+    // us, by 256 threads 31.5; 64 of one token 5.5 and 6.3.)
+    const int n = a.B <= 256 && !in_place ? 256 : kAssignSeqs;
     // A work-group takes a slot per thread, and up to 32 pages per thread if
     // every page of the tables changes hands.
     const bool with_slots = !in_place || slots <= 4 * n;
