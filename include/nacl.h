@@ -457,7 +457,9 @@ size_t nacl_paged_workspace_bytes(const nacl_problem* p, const nacl_step* s, con
  * sees the rows j < row0 + lens[b] + t + 1 of its sequence, at most L and as far
  * as the table goes (entries * page).  Rows of pages outside the pool (an entry
  * that is not in [0, n_pages)) are not seen.  q, out, lse and the results are
- * those of nacl_prefix_attention without a prefix, B * H * q_group * T below 2^26;
+ * those of nacl_prefix_attention without a prefix (for bf16 the probabilities are rounded
+ * to bf16 for the value product where q_group * T exceeds 128), B * H * q_group * T below
+ * 2^26;
  * pages may be shared by sequences, and hold anything in rows that are not seen.
  * Entries are followed as far as the lengths say, not as far as pages are held: a
  * sequence that nacl_pages_assign gave no pages waits for them. */

@@ -12,10 +12,10 @@
 // K-th largest of all, and few pass it.  Keys are unsigned with the numbers' order,
 // 0 for nothing.
 //
-// 32 groups of 8 beams, 131072 tokens each (67 MB of bf16), 16 wanted: slices 17.2 us (3.9
-// TB/s; vector and scalar instructions bound them, some 300 and 150 a wave), finish 6.8 us
-// (slices of 4096 tokens 21.6 + 8.2); 64 wanted: 23.7 + 10; 4 beams of 32000 tokens 4.7 + 4.4 us,
-// one chain of loads and barriers each.
+// 32 groups of 8 beams, 131072 tokens each (67 MB of bf16), 16 wanted: slices 16.4 us (4.1
+// TB/s; vector and scalar instructions bound them, some 300 and 150 a wave), finish 6.5 us
+// (slices of 4096 tokens 21.6 + 8.2); 64 wanted: 22.5 + 10.2; 4 beams of 32000 tokens 4.4 + 4.3
+// us, one chain of loads and barriers each.
 
 #include <type_traits>
 

@@ -7,10 +7,11 @@
 // queries of every sequence, query head and token of a group (rows of one K/V
 // head: ((i * G) + e) * T + t for sequence i of the group), for the own cache
 // those of one sequence ((t * G) + e, so that a block's causal limits rise).
-// A work-group takes a block of rows and a chunk of keys, its waves the chunk's
-// tiles in turn, each with a softmax of its own (running maximum and sum); the
-// waves' results are joined in LDS and either are the output (one chunk in all)
-// or go to the workspace, where merge_kernel joins a row's chunks.
+// A work-group takes a block of rows and a chunk of keys (of pages: blocks of keys that lie
+// as many blocks apart as there are splits), its waves the chunk's tiles in turn, each
+// with a softmax of its own (running maximum and sum); the waves' results are joined in
+// LDS and either are the output (one chunk in all) or go to the workspace, where
+// prefix_merge_kernel joins a row's chunks.
 
 #include <type_traits>
 
